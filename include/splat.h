@@ -157,11 +157,15 @@ splat_status splat_acsr_build(const splat_pattern_desc* desc, splat_acsr_t* out)
  *   `columns` reports the outcome.  A mask whose columns are not single runs
  *   still builds (columns = 0).  O(nnz) host time; UNSUPPORTED above 2^28
  *   non-zeros per head.
+ * SPLAT_PLAN_GRAD -- also plans the transposed mask (groups of keys, tiles of
+ *   query rows), which splat_sparse_mhsa_bwd works from.  Any mask; about as
+ *   much host time and device memory again as the plan itself.
  *
  * Returns INVALID_ARG for unknown flag bits; otherwise as splat_acsr_build.
  */
 #define SPLAT_PLAN_NO_SPAN 1u
 #define SPLAT_PLAN_COLUMNS 2u
+#define SPLAT_PLAN_GRAD 8u
 #define SPLAT_NO_SPAN_MAX_L 16384
 splat_status splat_acsr_build_ex(const splat_pattern_desc* desc, uint32_t flags, splat_acsr_t* out);
 
@@ -175,6 +179,10 @@ splat_status splat_acsr_build_ex(const splat_pattern_desc* desc, uint32_t flags,
  * one built from an equivalent descriptor.
  */
 splat_status splat_acsr_from_mask(int32_t L, const uint8_t* mask, splat_acsr_t* out);
+
+/* splat_acsr_from_mask with planning options: `flags` is 0 or SPLAT_PLAN_GRAD
+ * (INVALID_ARG for any other bit). */
+splat_status splat_acsr_from_mask_ex(int32_t L, const uint8_t* mask, uint32_t flags, splat_acsr_t* out);
 
 void splat_acsr_destroy(splat_acsr_t h); /* NULL is a no-op */
 
@@ -192,7 +200,7 @@ typedef struct {
   int64_t computed;        /* rows x keys of the 32-row x 64-key tiles the kernels compute (>= nnz) */
   int32_t columns;         /* column-wise analysis: -1 not requested, 0 some column is not one
                               affine run, 1 every column is (column-major layout available) */
-  int32_t reserved;
+  int32_t grad;            /* 1 if the handle was built with SPLAT_PLAN_GRAD */
 } splat_acsr_info_t;
 
 splat_status splat_acsr_info(splat_acsr_t h, splat_acsr_info_t* out);
@@ -224,6 +232,19 @@ splat_status splat_acsr_row_runs(splat_acsr_t h, int32_t row, int32_t* runs, int
  * Sizes come from splat_acsr_info (n_groups, n_tiles).
  */
 splat_status splat_acsr_export_plan(splat_acsr_t h, int32_t* groups, int32_t* rows, int32_t* tiles);
+
+/*
+ * Host copy of the transposed mask's work plan (SPLAT_PLAN_GRAD; INVALID_ARG
+ * without it).  sizes = {groups, tiles, mask words}; the other arrays may be
+ * NULL, to ask for the sizes.  groups and tiles as splat_acsr_export_plan with
+ * keys and query rows exchanged: keys[L] lists every key once (grouped), a
+ * tile is query rows first + step * u.  masks[128 * block + m] = the tile's
+ * query rows that have the group's key m; lone[t] = the query rows of tile t
+ * that have a single key.
+ */
+splat_status splat_acsr_export_grad_plan(splat_acsr_t h, int32_t sizes[3], int32_t* groups,
+                                         int32_t* keys, int32_t* tiles, uint64_t* masks,
+                                         uint64_t* lone);
 
 /*
  * Mask bits of one row inside one planned tile: bit u is set iff key

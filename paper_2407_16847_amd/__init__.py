@@ -32,6 +32,7 @@ MAX_TERMS = 8
 MAX_RUNS = 4
 PLAN_NO_SPAN = 1          # SPLAT_PLAN_NO_SPAN
 PLAN_COLUMNS = 2          # SPLAT_PLAN_COLUMNS
+PLAN_GRAD = 8             # SPLAT_PLAN_GRAD
 DENSE_ALPHA = 0.10        # SPLAT_DENSE_ALPHA
 NO_SPAN_MAX_L = 16384     # SPLAT_NO_SPAN_MAX_L
 F32, BF16 = 0, 1
@@ -60,7 +61,7 @@ class AcsrInfo(ctypes.Structure):
                 ("on_device", ctypes.c_int32), ("device", ctypes.c_int32), ("bm", ctypes.c_int32),
                 ("bn", ctypes.c_int32), ("n_groups", ctypes.c_int32), ("n_tiles", ctypes.c_int32),
                 ("n_full_tiles", ctypes.c_int32), ("nnz", ctypes.c_int64), ("computed", ctypes.c_int64),
-                ("columns", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+                ("columns", ctypes.c_int32), ("grad", ctypes.c_int32)]
 
 
 class TilingStats(ctypes.Structure):
@@ -117,10 +118,12 @@ def _open(path: str) -> ctypes.CDLL:
         "splat_acsr_build": [P(PatternDesc), P(vp)],
         "splat_acsr_build_ex": [P(PatternDesc), ctypes.c_uint32, P(vp)],
         "splat_acsr_from_mask": [i32, vp, P(vp)],
+        "splat_acsr_from_mask_ex": [i32, vp, ctypes.c_uint32, P(vp)],
         "splat_acsr_info": [vp, P(AcsrInfo)],
         "splat_acsr_export": [vp, vp, vp],
         "splat_acsr_row_runs": [vp, i32, vp, P(i32)],
         "splat_acsr_export_plan": [vp, vp, vp, vp],
+        "splat_acsr_export_grad_plan": [vp, P(i32), vp, vp, vp, vp, vp],
         "splat_acsr_tile_row_mask": [vp, i32, i32, P(ctypes.c_uint64)],
         "splat_rsddmm": [vp, i32, i32, i32, i32, vp, vp, f32, vp, vp],
         "splat_row_softmax": [vp, i32, i32, vp, vp, vp],
@@ -237,22 +240,24 @@ class Acsr:
     """An ACSR handle: per-row affine runs + work plan, on the current device."""
 
     def __init__(self, pattern: Optional[Pattern] = None, *, mask: Optional[np.ndarray] = None,
-                 span: bool = True, columns: bool = False):
+                 span: bool = True, columns: bool = False, grad: bool = False):
         """span=False plans without span specialisation (every group walks all
         of [0, L); an ablation).  columns=True adds the column-wise analysis
         (the column-major layout when every column is one affine run).  Both
-        need a pattern, not a mask."""
+        need a pattern, not a mask.  grad=True adds the plan of the transposed
+        mask, which the backward pass needs."""
         lib = load()
         h = ctypes.c_void_p()
-        flags = (0 if span else PLAN_NO_SPAN) | (PLAN_COLUMNS if columns else 0)
+        flags = ((0 if span else PLAN_NO_SPAN) | (PLAN_COLUMNS if columns else 0)
+                 | (PLAN_GRAD if grad else 0))
         if mask is not None:
-            if flags:
+            if flags & ~PLAN_GRAD:
                 raise ValueError("span=False and columns=True need a pattern, not a mask")
             m = np.ascontiguousarray(np.asarray(mask, dtype=np.uint8))
             if m.ndim != 2 or m.shape[0] != m.shape[1]:
                 raise ValueError("mask must be a square [L, L] array")
-            _check(lib.splat_acsr_from_mask(int(m.shape[0]), m.ctypes.data_as(ctypes.c_void_p),
-                                            ctypes.byref(h)))
+            _check(lib.splat_acsr_from_mask_ex(int(m.shape[0]), m.ctypes.data_as(ctypes.c_void_p),
+                                               flags, ctypes.byref(h)))
         else:
             if pattern is None:
                 raise ValueError("need a pattern or a mask")
@@ -342,6 +347,19 @@ class Acsr:
                                                 rows.ctypes.data_as(ctypes.c_void_p),
                                                 t.ctypes.data_as(ctypes.c_void_p)))
         return g, rows, t[: inf["n_tiles"]]
+
+    def export_grad_plan(self):
+        """(groups, keys, tiles, masks, lone) of the transposed mask's plan."""
+        n = (ctypes.c_int32 * 3)()
+        call, at = self._lib.splat_acsr_export_grad_plan, ctypes.c_void_p
+        _check(call(self.handle, n, None, None, None, None, None))
+        g = np.zeros((n[0], 4), dtype=np.int32)
+        keys = np.zeros(self.L, dtype=np.int32)
+        t = np.zeros((max(n[1], 1), 5), dtype=np.int32)
+        masks = np.zeros((n[2] // 128 + 1, 128), dtype=np.uint64)
+        lone = np.zeros(max(n[1], 1), dtype=np.uint64)
+        _check(call(self.handle, n, *(x.ctypes.data_as(at) for x in (g, keys, t, masks, lone))))
+        return g, keys, t[: n[1]], masks[: n[2] // 128], lone[: n[1]]
 
     def tile_row_mask(self, tile: int, row: int) -> int:
         b = ctypes.c_uint64()

@@ -31,6 +31,7 @@ struct Bits {
   explicit Bits(int32_t n_) : w((n_ + 63) / 64, 0ull), n(n_) {}
   void clear() { std::fill(w.begin(), w.end(), 0ull); }
   void set(int32_t j) { w[j >> 6] |= 1ull << (j & 63); }
+  bool has(int32_t j) const { return (w[j >> 6] >> (j & 63)) & 1; }
   void set_range(int32_t lo, int32_t hi) {  // inclusive, lo <= hi
     int32_t wl = lo >> 6, wh = hi >> 6;
     if (wl == wh) {
@@ -230,10 +231,12 @@ splat_status build_from_desc(const splat_pattern_desc& d, HostAcsr& a, std::stri
   }
   splat_status s = finish_rows(a, err);
   if (s == SPLAT_OK && (plan_flags & SPLAT_PLAN_COLUMNS)) s = analyse_columns(a, err);
+  if (s == SPLAT_OK && (plan_flags & SPLAT_PLAN_GRAD)) plan_grad(a);
   return s;
 }
 
-splat_status build_from_mask(int32_t L, const uint8_t* mask, HostAcsr& a, std::string& err) {
+splat_status build_from_mask(int32_t L, const uint8_t* mask, HostAcsr& a, std::string& err,
+                             uint32_t plan_flags) {
   if (L < 1 || L > SPLAT_MAX_L) {
     err = "L must be in [1, " + std::to_string(SPLAT_MAX_L) + "]";
     return SPLAT_ERR_INVALID_ARG;
@@ -271,10 +274,44 @@ splat_status build_from_mask(int32_t L, const uint8_t* mask, HostAcsr& a, std::s
     rr.r[0] = Run{cols[0], stride, n, 0};
     a.nruns[i] = 1;
   }
-  return finish_rows(a, err);
+  a.plan_flags = plan_flags;
+  const splat_status s = finish_rows(a, err);
+  if (s == SPLAT_OK && (plan_flags & SPLAT_PLAN_GRAD)) plan_grad(a);
+  return s;
 }
 
 // ---------------------------------------------------------------------------
+namespace {
+
+// The next tile over the set U, whose first member not yet in a tile is c:
+// the kBN places from c on, or, where that takes in more of U, the members at
+// c's gap to its successor (if step_ok(gap)).  Returns the last place taken.
+template <typename F>
+int32_t cut_tile(const Bits& U, int32_t c, F&& step_ok, Tile& t) {
+  const int32_t dense_end = std::min(U.n - 1, c + kBN - 1);
+  const int32_t k1 = U.count_range(c, dense_end);
+  int32_t k2 = 0, last = c, step = 1;
+  const int32_t nx = U.next(c + 1);
+  if (nx > 0 && nx - c > 1 && step_ok(nx - c)) {
+    step = nx - c;
+    k2 = 1;
+    while (k2 < kBN) {
+      const int32_t y = U.next(last + 1);
+      if (y < 0 || y - last != step) break;
+      last = y;
+      ++k2;
+    }
+  }
+  if (k2 > k1) {
+    t.kb = c, t.ks = step, t.nk = k2;
+    return last;
+  }
+  t.kb = c, t.ks = 1, t.nk = dense_end - c + 1;
+  return dense_end;
+}
+
+}  // namespace
+
 void plan_work(HostAcsr& a) {
   const int32_t L = a.L;
   // 1. group rows by affine signature: (stride, start mod stride) of a row
@@ -337,27 +374,7 @@ void plan_work(HostAcsr& a) {
           t.kb = c, t.ks = 1, t.nk = std::min(kBN, L - c);
           pos = c + t.nk;
         } else {
-          const int32_t dense_end = std::min(L - 1, c + kBN - 1);
-          const int32_t k1 = U.count_range(c, dense_end);
-          int32_t k2 = 0, last = c, step = 1;
-          const int32_t nx = U.next(c + 1);
-          if (nx > 0 && nx - c > 1 && gather_ok(nx - c)) {
-            step = nx - c;
-            k2 = 1;
-            while (k2 < kBN) {
-              const int32_t y = U.next(last + 1);
-              if (y < 0 || y - last != step) break;
-              last = y;
-              ++k2;
-            }
-          }
-          if (k2 > k1) {
-            t.kb = c, t.ks = step, t.nk = k2;
-            pos = last + 1;
-          } else {
-            t.kb = c, t.ks = 1, t.nk = dense_end - c + 1;
-            pos = dense_end + 1;
-          }
+          pos = cut_tile(U, c, gather_ok, t) + 1;
         }
         t.mask_block = -1;
         // per-row membership, per-wavefront state
@@ -405,6 +422,159 @@ void plan_work(HostAcsr& a) {
     p.g.tile_end = (int32_t)a.tiles.size();
     a.groups.push_back(p.g);
   }
+}
+
+// ---------------------------------------------------------------------------
+// Plan of the transposed mask.
+namespace {
+
+// word k, bit u <-> word u, bit k
+void transpose64(uint64_t (&x)[64]) {
+  uint64_t m = 0x00000000ffffffffull;
+  for (int j = 32; j != 0; j >>= 1, m ^= m << j)
+    for (int k = 0; k < 64; k = (k + j + 1) & ~j) {
+      const uint64_t t = ((x[k] >> j) ^ x[k + j]) & m;
+      x[k] ^= t << j;
+      x[k + j] ^= t;
+    }
+}
+
+// A group's keys as arithmetic progressions, none of them across the group's
+// key 64: a row's membership in each is O(1) per run.
+struct KeyPiece {
+  int32_t at, kb, ks, n;
+};
+
+std::vector<KeyPiece> key_pieces(const int32_t* keys, int32_t n) {
+  std::vector<KeyPiece> out;
+  for (int32_t p = 0; p < n;) {
+    const int32_t end = std::min(n, (p / 64 + 1) * 64);
+    KeyPiece k{p, keys[p], p + 1 < end ? keys[p + 1] - keys[p] : 1, 1};
+    while (p + k.n < end && keys[p + k.n] == k.kb + k.ks * k.n) ++k.n;
+    out.push_back(k);
+    p += k.n;
+  }
+  return out;
+}
+
+}  // namespace
+
+void plan_grad(HostAcsr& a) {
+  const int32_t L = a.L;
+  GradPlan& g = a.grad;
+  g = GradPlan();
+  // 1. Group the keys.  Where every row of several keys is one run of the same
+  //    stride s > 1, keys of one residue mod s share their rows.  Otherwise the
+  //    keys that many more rows have than the others (global columns) form
+  //    groups of their own, so that their rows cost the others nothing.
+  int32_t step = 0;   // 0: no row of several keys yet, 1: no common stride
+  std::vector<int32_t> diff(L + 1, 0), count(L, 0);
+  for (int32_t i = 0; i < L; ++i) {
+    for (int r = 0; r < SPLAT_MAX_RUNS; ++r) {
+      const Run& q = a.runs[i].r[r];
+      if (q.count <= 0) continue;
+      if (q.stride == 1) {
+        ++diff[q.start], --diff[q.start + q.count];
+      } else {
+        for (int32_t k = 0; k < q.count; ++k) ++count[q.start + q.stride * k];
+      }
+    }
+    if (a.row_ptr[i + 1] - a.row_ptr[i] > 1) {
+      const int32_t s = a.nruns[i] == 1 ? a.runs[i].r[0].stride : 1;
+      step = step == 0 || step == s ? s : 1;
+    }
+  }
+  for (int32_t j = 0, n = 0; j < L; ++j) n += diff[j], count[j] += n;
+  std::map<int32_t, std::vector<int32_t>> classes;
+  if (step > 1) {
+    for (int32_t j = 0; j < L; ++j) classes[j % step].push_back(j);
+  } else {
+    std::vector<int32_t> sorted(count);
+    std::nth_element(sorted.begin(), sorted.begin() + L / 2, sorted.end());
+    const int32_t many = 2 * sorted[L / 2] + kBM;
+    for (int32_t j = 0; j < L; ++j) classes[count[j] > many ? 0 : 1].push_back(j);
+  }
+  // 2. Cut each group's query rows into tiles.
+  struct Pending {
+    Group g;
+    std::vector<Tile> t;
+  };
+  std::vector<Pending> pend;
+  Bits U(L), one(L);
+  for (int32_t i = 0; i < L; ++i)
+    if (a.row_ptr[i + 1] - a.row_ptr[i] == 1) one.set(i);
+  std::vector<uint64_t> in(2 * (size_t)L, 0ull);   // each row's keys of the group
+  auto any_step = [](int32_t) { return true; };    // masks are not evaluated on the device
+  for (auto& kv : classes) {
+    const std::vector<int32_t>& keys = kv.second;
+    for (size_t off = 0; off < keys.size(); off += kBM) {
+      const int32_t nk = (int32_t)std::min<size_t>(kBM, keys.size() - off);
+      Pending p;
+      p.g = Group{(int32_t)g.rows.size(), nk, 0, 0};
+      g.rows.insert(g.rows.end(), keys.begin() + off, keys.begin() + off + nk);
+      const std::vector<KeyPiece> pieces = key_pieces(keys.data() + off, nk);
+      U.clear();
+      for (int32_t i = 0; i < L; ++i) {
+        uint64_t w[2] = {0, 0};
+        for (int r = 0; r < SPLAT_MAX_RUNS; ++r) {
+          const Run& q = a.runs[i].r[r];
+          if (q.count <= 0 || q.start > keys[off + nk - 1] ||
+              q.start + q.stride * (q.count - 1) < keys[off])
+            continue;
+          for (const KeyPiece& k : pieces)
+            w[k.at >> 6] |= run_tile_bits(q, k.kb, k.ks, k.n) << (k.at & 63);
+        }
+        in[2 * (size_t)i] = w[0], in[2 * (size_t)i + 1] = w[1];
+        if (w[0] | w[1]) U.set(i);
+      }
+      int32_t pos = 0;
+      for (int32_t c = U.next(0); c >= 0; c = U.next(pos)) {
+        Tile t{};
+        pos = cut_tile(U, c, any_step, t) + 1;
+        uint64_t rb[kBM], lone = 0;
+        for (int w = 0; w < 2; ++w) {
+          uint64_t x[64];
+          for (int32_t u = 0; u < 64; ++u)
+            x[u] = u < t.nk ? in[2 * (size_t)(t.kb + t.ks * u) + w] : 0ull;
+          transpose64(x);
+          std::memcpy(rb + 64 * w, x, sizeof(x));
+        }
+        for (int32_t u = 0; u < t.nk; ++u)
+          if (one.has(t.kb + t.ks * u)) lone |= 1ull << u;
+        t.pad[0] = (int32_t)(uint32_t)lone, t.pad[1] = (int32_t)(uint32_t)(lone >> 32);
+        t.mask_block = -1;
+        bool group_full = t.nk == kBN && lone == 0, any_partial = false;
+        for (int32_t w = 0; w < kWavesPerGroup && w * kWaveRows < nk; ++w) {
+          bool full = t.nk == kBN && lone == 0, empty = true;
+          for (int32_t m = w * kWaveRows; m < (w + 1) * kWaveRows && m < nk; ++m) {
+            full = full && rb[m] == ~0ull;
+            empty = empty && rb[m] == 0;
+          }
+          const int32_t st = empty ? kWaveEmpty : (full ? kWaveFull : kWavePartial);
+          t.flags |= st << (kWaveShift + 2 * w);
+          group_full = group_full && st == kWaveFull;
+          any_partial = any_partial || st == kWavePartial;
+        }
+        if (group_full) t.flags |= kTileFull;
+        if (any_partial) {
+          t.mask_block = (int32_t)(g.masks.size() / kBM);
+          g.masks.insert(g.masks.end(), rb, rb + kBM);
+        }
+        p.t.push_back(t);
+      }
+      pend.push_back(std::move(p));
+    }
+  }
+  // 3. heaviest groups first
+  std::stable_sort(pend.begin(), pend.end(),
+                   [](const Pending& x, const Pending& y) { return x.t.size() > y.t.size(); });
+  for (Pending& p : pend) {
+    p.g.tile_begin = (int32_t)g.tiles.size();
+    g.tiles.insert(g.tiles.end(), p.t.begin(), p.t.end());
+    p.g.tile_end = (int32_t)g.tiles.size();
+    g.groups.push_back(p.g);
+  }
+  a.has_grad = true;
 }
 
 // ---------------------------------------------------------------------------

@@ -67,6 +67,11 @@ void plan_sizes(splat_acsr* h) {
         n += ((a.tiles[t].flags >> (splat::kWaveShift + 2 * w)) & 3) != splat::kWaveEmpty;
       h->dev.max_slice_tiles = std::max(h->dev.max_slice_tiles, n);
     }
+  h->dev.grad_groups = (int32_t)a.grad.groups.size();
+  h->dev.grad_tiles = (int32_t)a.grad.tiles.size();
+  h->dev.grad_max_tiles = 0;
+  for (const splat::Group& g : a.grad.groups)
+    h->dev.grad_max_tiles = std::max(h->dev.grad_max_tiles, g.tile_end - g.tile_begin);
 }
 
 // One allocation holds every metadata array, each 256-byte aligned.
@@ -85,15 +90,23 @@ splat_status upload(splat_acsr* h) {
     return fail(SPLAT_ERR_HIP, "hipFuncSetAttribute (fused kernel LDS): %s", hipGetErrorString(e));
   const HostAcsr& a = h->host;
   auto al = [](size_t x) { return (x + 255) & ~size_t(255); };
-  const size_t s_rowptr = al(sizeof(int32_t) * (a.L + 1));
-  const size_t s_runs = al(sizeof(splat::RowRuns) * a.L);
-  const size_t s_rows = al(sizeof(int32_t) * a.L);
-  const size_t s_groups = al(sizeof(splat::Group) * a.groups.size());
-  const size_t s_tiles = al(sizeof(splat::Tile) * (a.tiles.size() + 1));
-  // one extra zero block: tiles without masks still issue (unused) mask loads
-  const size_t s_masks = al(sizeof(uint64_t) * (a.masks.size() + splat::kBM));
-  const size_t s_cols = al(sizeof(splat::ColRun) * a.cols.size());
-  const size_t total = s_rowptr + s_runs + s_rows + s_groups + s_tiles + s_masks + s_cols;
+  struct Part {
+    const void* src;
+    size_t n, sz;   // bytes to copy, bytes to take up
+  };
+  auto part = [&](const auto& v, size_t more = 0) {
+    const size_t e = sizeof(v[0]);
+    return Part{v.data(), e * v.size(), al(e * (v.size() + more))};
+  };
+  // one extra zero tile and mask block: descriptors are read one ahead, and
+  // tiles without masks still issue (unused) mask loads
+  const Part parts[] = {part(a.row_ptr),     part(a.runs),         part(a.rows),
+                        part(a.groups),      part(a.tiles, 1),     part(a.masks, splat::kBM),
+                        part(a.cols),        part(a.grad.rows),    part(a.grad.groups),
+                        part(a.grad.tiles, 1), part(a.grad.masks, splat::kBM)};
+  constexpr int kParts = sizeof(parts) / sizeof(parts[0]);
+  size_t total = 0;
+  for (const Part& q : parts) total += q.sz;
   void* mem = nullptr;
   e = hipMalloc(&mem, total);
   if (e != hipSuccess) {
@@ -106,18 +119,8 @@ splat_status upload(splat_acsr* h) {
     return fail(SPLAT_ERR_HIP, "hipMemset of ACSR metadata: %s", hipGetErrorString(e));
   }
   char* p = (char*)mem;
-  struct Part {
-    const void* src;
-    size_t n, sz;
-  } parts[] = {{a.row_ptr.data(), sizeof(int32_t) * (a.L + 1), s_rowptr},
-               {a.runs.data(), sizeof(splat::RowRuns) * a.L, s_runs},
-               {a.rows.data(), sizeof(int32_t) * a.L, s_rows},
-               {a.groups.data(), sizeof(splat::Group) * a.groups.size(), s_groups},
-               {a.tiles.data(), sizeof(splat::Tile) * a.tiles.size(), s_tiles},
-               {a.masks.data(), sizeof(uint64_t) * a.masks.size(), s_masks},
-               {a.cols.data(), sizeof(splat::ColRun) * a.cols.size(), s_cols}};
-  char* dst[7];
-  for (int k = 0; k < 7; ++k) {
+  char* dst[kParts];
+  for (int k = 0; k < kParts; ++k) {
     dst[k] = p;
     if (parts[k].n) {
       e = hipMemcpy(p, parts[k].src, parts[k].n, hipMemcpyHostToDevice);
@@ -137,6 +140,12 @@ splat_status upload(splat_acsr* h) {
   h->dev.tiles = (const splat::Tile*)dst[4];
   h->dev.masks = (const uint64_t*)dst[5];
   h->dev.cols = a.cols.empty() ? nullptr : (const splat::ColRun*)dst[6];
+  if (a.has_grad) {
+    h->dev.grad_rows = (const int32_t*)dst[7];
+    h->dev.grad_group = (const splat::Group*)dst[8];
+    h->dev.grad_tile = (const splat::Tile*)dst[9];
+    h->dev.grad_masks = (const uint64_t*)dst[10];
+  }
   return SPLAT_OK;
 }
 
@@ -362,6 +371,24 @@ splat_status scratch_on(int dev, char** out) {
   return ok();
 }
 
+// groups[4 * g + ..] and tiles[5 * t + ..] of a plan, where not NULL
+void export_plan(const std::vector<splat::Group>& gs, const std::vector<splat::Tile>& ts,
+                 int32_t* groups, int32_t* tiles) {
+  for (size_t g = 0; groups && g < gs.size(); ++g) {
+    groups[4 * g] = gs[g].row_off;
+    groups[4 * g + 1] = gs[g].nrows;
+    groups[4 * g + 2] = gs[g].tile_begin;
+    groups[4 * g + 3] = gs[g].tile_end;
+  }
+  for (size_t t = 0; tiles && t < ts.size(); ++t) {
+    tiles[5 * t] = ts[t].kb;
+    tiles[5 * t + 1] = ts[t].ks;
+    tiles[5 * t + 2] = ts[t].nk;
+    tiles[5 * t + 3] = ts[t].flags;
+    tiles[5 * t + 4] = ts[t].mask_block;
+  }
+}
+
 }  // namespace
 
 extern "C" {
@@ -391,7 +418,7 @@ splat_status splat_pattern_full(int32_t L, splat_pattern_desc* out) {
 
 splat_status splat_acsr_build_ex(const splat_pattern_desc* desc, uint32_t flags, splat_acsr_t* out) {
   if (!desc || !out) return fail(SPLAT_ERR_INVALID_ARG, "desc and out must be non-NULL");
-  if (flags & ~(SPLAT_PLAN_NO_SPAN | SPLAT_PLAN_COLUMNS))
+  if (flags & ~(SPLAT_PLAN_NO_SPAN | SPLAT_PLAN_COLUMNS | SPLAT_PLAN_GRAD))
     return fail(SPLAT_ERR_INVALID_ARG, "unknown plan flags 0x%x", flags);
   if ((flags & SPLAT_PLAN_NO_SPAN) && desc->L > SPLAT_NO_SPAN_MAX_L)
     return fail(SPLAT_ERR_UNSUPPORTED, "SPLAT_PLAN_NO_SPAN needs L <= %d, got %d", SPLAT_NO_SPAN_MAX_L,
@@ -413,19 +440,26 @@ splat_status splat_acsr_build(const splat_pattern_desc* desc, splat_acsr_t* out)
   return splat_acsr_build_ex(desc, 0u, out);
 }
 
-splat_status splat_acsr_from_mask(int32_t L, const uint8_t* mask, splat_acsr_t* out) {
+splat_status splat_acsr_from_mask_ex(int32_t L, const uint8_t* mask, uint32_t flags,
+                                     splat_acsr_t* out) {
+  if (flags & ~SPLAT_PLAN_GRAD)
+    return fail(SPLAT_ERR_INVALID_ARG, "unknown plan flags 0x%x for a mask", flags);
   if (!out) return fail(SPLAT_ERR_INVALID_ARG, "out must be non-NULL");
   splat_acsr* h = new (std::nothrow) splat_acsr();
   if (!h) return fail(SPLAT_ERR_OOM, "host allocation failed");
   std::string err;
   splat_status s;
   try {
-    s = splat::build_from_mask(L, mask, h->host, err);
+    s = splat::build_from_mask(L, mask, h->host, err, flags);
   } catch (const std::bad_alloc&) {
     s = SPLAT_ERR_OOM;
     err = "host allocation failed during the analysis";
   }
   return finish_build(h, s, err, out);
+}
+
+splat_status splat_acsr_from_mask(int32_t L, const uint8_t* mask, splat_acsr_t* out) {
+  return splat_acsr_from_mask_ex(L, mask, 0u, out);
 }
 
 void splat_acsr_destroy(splat_acsr_t h) {
@@ -451,6 +485,7 @@ splat_status splat_acsr_info(splat_acsr_t h, splat_acsr_info_t* out) {
   out->nnz = a.nnz;
   out->computed = a.computed;
   out->columns = a.col_regular;
+  out->grad = a.has_grad;
   return ok();
 }
 
@@ -530,20 +565,27 @@ splat_status splat_acsr_row_runs(splat_acsr_t h, int32_t row, int32_t* runs, int
 splat_status splat_acsr_export_plan(splat_acsr_t h, int32_t* groups, int32_t* rows, int32_t* tiles) {
   if (!h || !groups || !rows || !tiles) return fail(SPLAT_ERR_INVALID_ARG, "NULL argument");
   const HostAcsr& a = h->host;
-  for (size_t g = 0; g < a.groups.size(); ++g) {
-    groups[4 * g] = a.groups[g].row_off;
-    groups[4 * g + 1] = a.groups[g].nrows;
-    groups[4 * g + 2] = a.groups[g].tile_begin;
-    groups[4 * g + 3] = a.groups[g].tile_end;
-  }
   std::memcpy(rows, a.rows.data(), sizeof(int32_t) * a.L);
-  for (size_t t = 0; t < a.tiles.size(); ++t) {
-    tiles[5 * t] = a.tiles[t].kb;
-    tiles[5 * t + 1] = a.tiles[t].ks;
-    tiles[5 * t + 2] = a.tiles[t].nk;
-    tiles[5 * t + 3] = a.tiles[t].flags;
-    tiles[5 * t + 4] = a.tiles[t].mask_block;
-  }
+  export_plan(a.groups, a.tiles, groups, tiles);
+  return ok();
+}
+
+splat_status splat_acsr_export_grad_plan(splat_acsr_t h, int32_t sizes[3], int32_t* groups,
+                                         int32_t* keys, int32_t* tiles, uint64_t* masks,
+                                         uint64_t* lone) {
+  if (!h || !sizes) return fail(SPLAT_ERR_INVALID_ARG, "handle and sizes must be non-NULL");
+  if (!h->host.has_grad)
+    return fail(SPLAT_ERR_INVALID_ARG, "the handle was built without SPLAT_PLAN_GRAD");
+  const splat::GradPlan& g = h->host.grad;
+  sizes[0] = (int32_t)g.groups.size();
+  sizes[1] = (int32_t)g.tiles.size();
+  sizes[2] = (int32_t)g.masks.size();
+  if (keys) std::memcpy(keys, g.rows.data(), sizeof(int32_t) * g.rows.size());
+  export_plan(g.groups, g.tiles, groups, tiles);
+  if (masks && !g.masks.empty())
+    std::memcpy(masks, g.masks.data(), sizeof(uint64_t) * g.masks.size());
+  for (size_t t = 0; lone && t < g.tiles.size(); ++t)
+    lone[t] = (uint64_t)(uint32_t)g.tiles[t].pad[0] | (uint64_t)(uint32_t)g.tiles[t].pad[1] << 32;
   return ok();
 }
 

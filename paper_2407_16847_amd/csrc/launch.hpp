@@ -28,6 +28,14 @@ struct DevAcsr {
   const Tile* tiles;
   const uint64_t* masks;    // kBM row masks per tile that has a PARTIAL wavefront
   const ColRun* cols;       // L single-run column descriptors, or null (no column-major layout)
+  // the transposed mask's plan (groups of keys, tiles of query rows), or null
+  int32_t grad_groups;
+  int32_t grad_tiles;
+  int32_t grad_max_tiles;   // tiles of the key group that has the most
+  const int32_t* grad_rows;
+  const Group* grad_group;
+  const Tile* grad_tile;
+  const uint64_t* grad_masks;
 };
 
 // Position of `row` in the column-major value array of one head, for a row
