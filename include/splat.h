@@ -431,6 +431,43 @@ splat_status splat_sparse_mhsa_fwd(splat_acsr_t h, splat_dtype dtype, int32_t B,
                                    void* O, splat_dtype out_dtype, void* stream);
 
 /*
+ * Training: the fused forward that keeps what its backward pass needs, and the
+ * backward pass.  With s_ij = scale q_i.k_j on the mask:
+ *
+ *     lse_i = ln sum_j exp(s_ij)            p_ij  = exp(s_ij - lse_i)
+ *     dP_ij = dO_i.v_j                      dS_ij = p_ij (dP_ij - dO_i.O_i)
+ *     dQ_i = scale sum_j dS_ij k_j    dK_j = scale sum_i dS_ij q_i    dV_j = sum_i p_ij dO_i
+ *
+ * splat_sparse_mhsa_fwd_lse -- splat_sparse_mhsa_fwd that also writes the rows'
+ * log-sum-exp: lse is fp32 [B,H,L], -inf for a row without keys (whose O is 0).
+ * O has `dtype`.  With bf16 inputs the scores are scaled in fp32 (the other call
+ * rounds scale * Q to bf16 first), so O may differ from that call's by roundings
+ * of that size.  Only a row's own keys count, whatever the others hold: a row
+ * whose products over its tiles are not finite is formed again from its keys
+ * alone.  O and lse share no memory with Q, K, V or each other (INVALID_ARG).
+ *
+ * splat_sparse_mhsa_bwd -- dQ, dK, dV [B,H,L,d] of `dtype` from Q, K, V, the O and
+ * lse of splat_sparse_mhsa_fwd_lse and the gradient dO of O, all [B,H,L,d] of
+ * `dtype`.  The probabilities are recomputed, in fp32; with bf16 inputs p and dS
+ * are rounded to nearest even bf16 for the products that sum them, which run in
+ * fp32.  Sums have a fixed order: equal calls give equal bits.  A row with one
+ * key has p = 1 whatever its score: its dS is 0, and so its dQ.  Rows without keys
+ * have dQ = 0, keys without rows dK = dV = 0.  An infinity or a NaN reaches only
+ * the gradients that the mask connects it with.
+ * workspace: 2*B*H*L floats of device memory that the call writes and reads (calls
+ * that may run at the same time need one each).  The gradients and the workspace
+ * share no memory with the inputs or each other (INVALID_ARG).  The handle must
+ * have been built with SPLAT_PLAN_GRAD (INVALID_ARG).
+ */
+splat_status splat_sparse_mhsa_fwd_lse(splat_acsr_t h, splat_dtype dtype, int32_t B, int32_t H,
+                                       int32_t d, const void* Q, const void* K, const void* V,
+                                       float scale, void* O, float* lse, void* stream);
+splat_status splat_sparse_mhsa_bwd(splat_acsr_t h, splat_dtype dtype, int32_t B, int32_t H, int32_t d,
+                                   const void* Q, const void* K, const void* V, const void* O,
+                                   const float* lse, const void* dO, float scale, void* dQ, void* dK,
+                                   void* dV, float* workspace, void* stream);
+
+/*
  * splat_debug_bounds -- index checks of a checked build (built with
  * -DSPLAT_DEBUG_BOUNDS: libsplat_checked.so beside libsplat.so; a debugging
  * aid, not part of the method).  In a checked build every kernel checks the

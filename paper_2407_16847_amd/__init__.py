@@ -26,6 +26,7 @@ __all__ = [
     "SplatError", "Pattern", "Acsr", "load", "lib_path", "rsddmm", "row_softmax", "rspmm",
     "sparse_mhsa_fwd", "MAX_RUNS", "MAX_TERMS", "PLAN_NO_SPAN", "NO_SPAN_MAX_L", "PLAN_COLUMNS",
     "DENSE_ALPHA", "transpose_colmajor", "rspmm_colmajor", "sparse_mhsa_unfused",
+    "sparse_mhsa_fwd_lse", "sparse_mhsa_bwd", "PLAN_GRAD",
 ]
 
 MAX_TERMS = 8
@@ -129,6 +130,9 @@ def _open(path: str) -> ctypes.CDLL:
         "splat_row_softmax": [vp, i32, i32, vp, vp, vp],
         "splat_rspmm": [vp, i32, i32, i32, i32, vp, vp, vp, i32, vp],
         "splat_sparse_mhsa_fwd": [vp, i32, i32, i32, i32, vp, vp, vp, f32, vp, i32, vp],
+        "splat_sparse_mhsa_fwd_lse": [vp, i32, i32, i32, i32, vp, vp, vp, f32, vp, vp, vp],
+        "splat_sparse_mhsa_bwd": [vp, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, f32, vp, vp, vp, vp,
+                                  vp],
         "splat_sparse_mhsa_unfused_noalloc": [vp, i32, i32, i32, i32, vp, vp, vp, f32, vp, i32, f32,
                                               P(i32), vp],
         "splat_acsr_export_csc": [vp, vp, vp],
@@ -515,6 +519,69 @@ def sparse_mhsa_fwd(acsr: Acsr, Q: torch.Tensor, K: torch.Tensor, V: torch.Tenso
                                         V.data_ptr(), float(scale), O.data_ptr(), _DT[O.dtype],
                                         _stream()))
     return O
+
+
+def sparse_mhsa_fwd_lse(acsr: Acsr, Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, scale: float,
+                        O: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None
+                        ) -> Tuple[torch.Tensor, torch.Tensor]:
+    """The fused forward that keeps the rows' log-sum-exp for sparse_mhsa_bwd:
+    (O in the inputs' dtype, lse fp32 [B, H, L])."""
+    _dense(Q, "Q", acsr)
+    B, H, L, d = Q.shape
+    _like(K, "K", Q, acsr)
+    _like(V, "V", Q, acsr)
+    O = _result(O, "O", Q, acsr)
+    if lse is None:
+        lse = torch.empty((B, H, L), dtype=torch.float32, device=Q.device)
+    else:
+        _rows(lse, "lse", Q)
+    _check(load().splat_sparse_mhsa_fwd_lse(acsr.handle, _DT[Q.dtype], B, H, d, Q.data_ptr(),
+                                            K.data_ptr(), V.data_ptr(), float(scale), O.data_ptr(),
+                                            lse.data_ptr(), _stream()))
+    return O, lse
+
+
+def sparse_mhsa_bwd(acsr: Acsr, Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, O: torch.Tensor,
+                    lse: torch.Tensor, dO: torch.Tensor, scale: float,
+                    dQ: Optional[torch.Tensor] = None, dK: Optional[torch.Tensor] = None,
+                    dV: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None
+                    ) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+    """(dQ, dK, dV) of sparse_mhsa_fwd_lse from the gradient dO of its O.  Needs a
+    handle built with grad=True.  workspace: fp32 [2, B, H, L], made by the call
+    unless given."""
+    _dense(Q, "Q", acsr)
+    B, H, L, d = Q.shape
+    for x, name in ((K, "K"), (V, "V"), (O, "O"), (dO, "dO")):
+        _like(x, name, Q, acsr)
+    _rows(lse, "lse", Q)
+    dQ, dK, dV = (_result(x, name, Q, acsr) for x, name in ((dQ, "dQ"), (dK, "dK"), (dV, "dV")))
+    if workspace is None:
+        workspace = torch.empty((2, B, H, L), dtype=torch.float32, device=Q.device)
+    else:
+        _rows(workspace, "workspace", Q, 2)
+    _check(load().splat_sparse_mhsa_bwd(acsr.handle, _DT[Q.dtype], B, H, d, Q.data_ptr(),
+                                        K.data_ptr(), V.data_ptr(), O.data_ptr(), lse.data_ptr(),
+                                        dO.data_ptr(), float(scale), dQ.data_ptr(), dK.data_ptr(),
+                                        dV.data_ptr(), workspace.data_ptr(), _stream()))
+    return dQ, dK, dV
+
+
+def _result(x: Optional[torch.Tensor], name: str, Q: torch.Tensor, acsr: Acsr) -> torch.Tensor:
+    """x, of Q's shape and dtype, or a new tensor of them."""
+    if x is None:
+        return _new(Q, Q.dtype)
+    _like(x, name, Q, acsr)
+    return x
+
+
+def _rows(x: torch.Tensor, name: str, Q: torch.Tensor, *lead: int) -> None:
+    """x is fp32, a value (or `lead` of them) for every query row."""
+    if not isinstance(x, torch.Tensor) or not x.is_cuda:
+        raise TypeError(f"{name} must be a CUDA (HIP) tensor")
+    shape = (*lead, *Q.shape[:3])
+    if x.dtype != torch.float32 or x.shape != shape or not x.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous float32 {list(shape)} tensor")
+    _on(x, name, Q)
 
 
 def _values(x: torch.Tensor, name: str, acsr: Acsr, B: int, H: int) -> None:

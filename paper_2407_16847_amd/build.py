@@ -27,7 +27,7 @@ BUILD_DIR_CHECKED = os.path.join(HERE, "_build_checked")
 ARCH = "gfx950"
 
 SOURCES = ["acsr_host.cpp", "tiling.cpp", "api.hip", "kernels_mfma.hip", "kernels_tiles.hip",
-           "kernels_slices.hip"]
+           "kernels_slices.hip", "kernels_grad.hip"]
 
 COMMON = ["-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function", "-Wno-unknown-pragmas"]
 # Packed fp32 instructions stay off: plain float code must not be turned into

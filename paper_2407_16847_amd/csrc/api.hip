@@ -88,6 +88,9 @@ splat_status upload(splat_acsr* h) {
   e = splat::prepare_fused_mfma();
   if (e != hipSuccess)
     return fail(SPLAT_ERR_HIP, "hipFuncSetAttribute (fused kernel LDS): %s", hipGetErrorString(e));
+  if (h->host.has_grad && (e = splat::prepare_bwd()) != hipSuccess)
+    return fail(SPLAT_ERR_HIP, "hipFuncSetAttribute (backward kernels' LDS): %s",
+                hipGetErrorString(e));
   const HostAcsr& a = h->host;
   auto al = [](size_t x) { return (x + 255) & ~size_t(255); };
   struct Part {
@@ -292,6 +295,27 @@ bool use_colmajor(const HostAcsr& a, float alpha) {
 // Do the byte ranges [a, a + na) and [b, b + nb) meet?
 bool meet(const void* a, size_t na, const void* b, size_t nb) {
   return a && b && (uintptr_t)a < (uintptr_t)b + nb && (uintptr_t)b < (uintptr_t)a + na;
+}
+
+// A call's tensors: each a valid pointer, and no output meets anything else.
+struct Span {
+  const void* p;
+  size_t bytes;
+  const char* name;
+};
+splat_status check_spans(const Span* in, int n_in, const Span* out, int n_out) {
+  for (int k = 0; k < n_in; ++k) CHECK(check_ptr(in[k].p, in[k].name));
+  for (int k = 0; k < n_out; ++k) CHECK(check_ptr(out[k].p, out[k].name));
+  for (int k = 0; k < n_out; ++k) {
+    auto apart = [&](const Span& x) {
+      if (meet(out[k].p, out[k].bytes, x.p, x.bytes))
+        return fail(SPLAT_ERR_INVALID_ARG, "%s must not overlap %s", out[k].name, x.name);
+      return SPLAT_OK;
+    };
+    for (int i = 0; i < n_in; ++i) CHECK(apart(in[i]));
+    for (int i = 0; i < k; ++i) CHECK(apart(out[i]));
+  }
+  return SPLAT_OK;
 }
 
 // The unfused chain.  keep_values: the caller reads P in S (and Pt) afterwards;
@@ -661,10 +685,51 @@ splat_status splat_sparse_mhsa_fwd(splat_acsr_t h, splat_dtype dtype, int32_t B,
   hipStream_t st = (hipStream_t)stream;
   if (dtype == SPLAT_BF16) CHECK(check_tile_grid(h, B, H));
   if (dtype == SPLAT_BF16)
-    return launched(splat::launch_fused_mfma(h->dev, B * H, d, Q, K, V, scale, O, out_dtype, st),
+    return launched(splat::launch_fused_mfma(h->dev, B * H, d, Q, K, V, scale, O, out_dtype,
+                                              nullptr, st),
                     "sparse_mhsa_fwd");
-  return launched(splat::launch_fused_f32(h->dev, B * H, d, Q, K, V, scale, O, out_dtype, st),
+  return launched(splat::launch_fused_f32(h->dev, B * H, d, Q, K, V, scale, O, out_dtype,
+                                           nullptr, st),
                   "sparse_mhsa_fwd");
+}
+
+splat_status splat_sparse_mhsa_fwd_lse(splat_acsr_t h, splat_dtype dtype, int32_t B, int32_t H,
+                                       int32_t d, const void* Q, const void* K, const void* V,
+                                       float scale, void* O, float* lse, void* stream) {
+  CHECK(check_handle(h, B, H));
+  CHECK(check_dtype(dtype, "dtype"));
+  CHECK(check_d(d));
+  const size_t rows = (size_t)B * H * h->host.L, dense = rows * d * (dtype == SPLAT_BF16 ? 2 : 4);
+  const Span in[] = {{Q, dense, "Q"}, {K, dense, "K"}, {V, dense, "V"}};
+  const Span out[] = {{O, dense, "O"}, {lse, rows * 4, "lse"}};
+  CHECK(check_spans(in, 3, out, 2));
+  hipStream_t st = (hipStream_t)stream;
+  if (dtype == SPLAT_BF16) CHECK(check_tile_grid(h, B, H));
+  return launched(dtype == SPLAT_BF16
+                      ? splat::launch_fused_mfma(h->dev, B * H, d, Q, K, V, scale, O, 1, lse, st)
+                      : splat::launch_fused_f32(h->dev, B * H, d, Q, K, V, scale, O, 0, lse, st),
+                  "sparse_mhsa_fwd_lse");
+}
+
+splat_status splat_sparse_mhsa_bwd(splat_acsr_t h, splat_dtype dtype, int32_t B, int32_t H, int32_t d,
+                                   const void* Q, const void* K, const void* V, const void* O,
+                                   const float* lse, const void* dO, float scale, void* dQ, void* dK,
+                                   void* dV, float* workspace, void* stream) {
+  CHECK(check_handle(h, B, H));
+  CHECK(check_dtype(dtype, "dtype"));
+  CHECK(check_d(d));
+  if (!h->host.has_grad)
+    return fail(SPLAT_ERR_INVALID_ARG, "the handle was built without SPLAT_PLAN_GRAD");
+  const size_t rows = (size_t)B * H * h->host.L, dense = rows * d * (dtype == SPLAT_BF16 ? 2 : 4);
+  const Span in[] = {{Q, dense, "Q"}, {K, dense, "K"},      {V, dense, "V"},
+                     {O, dense, "O"}, {lse, rows * 4, "lse"}, {dO, dense, "dO"}};
+  const Span out[] = {{dQ, dense, "dQ"}, {dK, dense, "dK"}, {dV, dense, "dV"},
+                      {workspace, rows * 8, "workspace"}};
+  CHECK(check_spans(in, 6, out, 4));
+  if (dtype == SPLAT_BF16) CHECK(check_tile_grid(h, B, H));
+  const splat::BwdArgs x{Q, K, V, O, dO, lse, workspace, dQ, dK, dV};
+  return launched(splat::launch_bwd(h->dev, dtype, B * H, d, x, scale, (hipStream_t)stream),
+                  "sparse_mhsa_bwd");
 }
 
 splat_status splat_sparse_mhsa_unfused(splat_acsr_t h, splat_dtype dtype, int32_t B, int32_t H,
@@ -731,6 +796,7 @@ splat_status splat_debug_bounds(uint32_t* flags, int32_t clear) {
   if (e == hipSuccess) e = splat::bounds_collect_mfma(&bits, clear != 0);
   if (e == hipSuccess) e = splat::bounds_collect_tiles(&bits, clear != 0);
   if (e == hipSuccess) e = splat::bounds_collect_slices(&bits, clear != 0);
+  if (e == hipSuccess) e = splat::bounds_collect_grad(&bits, clear != 0);
   if (e != hipSuccess) return fail(SPLAT_ERR_HIP, "splat_debug_bounds: %s", hipGetErrorString(e));
   *flags = bits;
   return SPLAT_OK;

@@ -42,11 +42,10 @@
 #include "bounds.hpp"
 #include "launch.hpp"
 #include "mfma_util.hpp"
+#include "slice_ops.hpp"
 
 namespace splat {
 namespace {
-
-using namespace mfma;
 
 constexpr int kThreads = 256;           // 4 waves
 constexpr float kSumLimit = 4096.f;   // largest tile row sum the fast pass accepts
@@ -110,10 +109,11 @@ __device__ __forceinline__ void issue_tile(char* slot, const Tile tl, const __bf
 // pass, whose factor 2^-m is applied afterwards by scale_pairs, only when some
 // row of the wavefront has m > 0).  Each p goes to the P^T operand rounded to
 // nearest even bf16 (one v_cvt_pk_bf16_f32 per pair); returns the sum of the
-// rounded p (v_dot2c_f32_bf16 against ones, fp32 accumulation).
-template <bool REF>
-__device__ __forceinline__ float tile_exp(const f32x16_t* s, float m, bf16x8_t* pf) {
-  float l0 = 0.f, l1 = 0.f;
+// rounded p (v_dot2c_f32_bf16 against ones, fp32 accumulation).  SUM: lx = the
+// sum of the p before their rounding.
+template <bool REF, bool SUM>
+__device__ __forceinline__ float tile_exp(const f32x16_t* s, float m, bf16x8_t* pf, float& lx) {
+  float l0 = 0.f, l1 = 0.f, x0 = 0.f, x1 = 0.f;
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     float e8[8];
@@ -121,6 +121,10 @@ __device__ __forceinline__ float tile_exp(const f32x16_t* s, float m, bf16x8_t* 
     for (int e = 0; e < 8; ++e) {
       const float t = s[j >> 1][(j & 1) * 8 + e];
       e8[e] = exp2_hw(REF ? t - m : t);
+    }
+    if constexpr (SUM) {
+      x0 += (e8[0] + e8[1]) + (e8[2] + e8[3]);
+      x1 += (e8[4] + e8[5]) + (e8[6] + e8[7]);
     }
     // the row sum adds exactly the rounded values the MFMA multiplies; the
     // dot products take the packed pairs as scalars (taken back out of a
@@ -133,6 +137,7 @@ __device__ __forceinline__ float tile_exp(const f32x16_t* s, float m, bf16x8_t* 
     l1 = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, u3), kOnes2, l1, false);
     pf[j] = __builtin_bit_cast(bf16x8_t, u32x4_t{u0, u1, u2, u3});
   }
+  if constexpr (SUM) lx = x0 + x1;
   return l0 + l1;
 }
 
@@ -169,12 +174,24 @@ __device__ __forceinline__ void mask_scores(f32x16_t* s, uint64_t mk, int h) {
 // taking tiles s, s + NSET, .. with a ring of its own; at the end set 0 takes
 // the others' O, sums and references over through LDS.  The references are
 // integers, so the factors between them are powers of two.
-template <int D, typename OutT, int NSET>
-__global__ __launch_bounds__(kThreads * NSET, D == 64 ? 4 : 2) void k_fused_mfma(
+//
+// LSE, for the backward pass, which recomputes the scores from Q itself: Q is
+// not scaled and rounded beforehand, the scores are scaled in fp32 (so that
+// both passes see the same scores), the rows' log-sum-exp adds the p before
+// their rounding, and rows that are not finite are formed again from their own
+// keys alone.
+struct LseArgs {
+  float* lse;
+  const int32_t* row_ptr;
+  const RowRuns* runs;
+  float scale;
+};
+template <int D, typename OutT, int NSET, bool LSE>
+__device__ __forceinline__ void fused_tiles(
     const Group* __restrict__ groups, const int32_t* __restrict__ rows,
     const Tile* __restrict__ tiles, const uint64_t* __restrict__ masks, int L, int BH,
     const __bf16* __restrict__ Q, const __bf16* K, const __bf16* V, float sl2,
-    OutT* __restrict__ O) {
+    OutT* __restrict__ O, const LseArgs x) {
   using G = Geo<D>;
   constexpr int NKS = G::NKS, NDB = G::NDB, NSLOT = G::NSLOT, RB = G::RB;
   extern __shared__ __attribute__((aligned(16))) char smem_all[];
@@ -203,7 +220,7 @@ __global__ __launch_bounds__(kThreads * NSET, D == 64 ? 4 : 2) void k_fused_mfma
       if (row_valid) {
         const bf16x8_t q = *(const bf16x8_t*)(qrow + ks * 16 + h * 8);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) qf[ks][e] = (__bf16)((float)q[e] * sl2);
+        for (int e = 0; e < 8; ++e) qf[ks][e] = LSE ? q[e] : (__bf16)((float)q[e] * sl2);
       } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e) qf[ks][e] = (__bf16)0.f;
@@ -228,7 +245,7 @@ __global__ __launch_bounds__(kThreads * NSET, D == 64 ? 4 : 2) void k_fused_mfma
   // and the reference as the fast pass applies it
   // (l_run holds this lane's half of the row's keys; acc says whether the
   // whole row has accumulated any weight, identical in both halves)
-  float m_run = 0.f, l_run = 0.f;
+  float m_run = 0.f, l_run = 0.f, lx_run = 0.f;
   unsigned msub = 0u;
   float mscale = 1.f;
   bool fast_ok = true, acc = false;
@@ -274,6 +291,9 @@ __global__ __launch_bounds__(kThreads * NSET, D == 64 ? 4 : 2) void k_fused_mfma
             for (int r = 0; r < 16; ++r) sacc[kb2][r] = 0.f;
 #pragma unroll
             for (int ks = 0; ks < NKS; ++ks) sacc[kb2] = mfma32(ka[kb2][ks], qf[ks], sacc[kb2]);
+            if constexpr (LSE)
+#pragma unroll
+              for (int r = 0; r < 16; ++r) sacc[kb2][r] *= sl2;
           }
         };
         f32x16_t sacc[2];
@@ -284,10 +304,12 @@ __global__ __launch_bounds__(kThreads * NSET, D == 64 ? 4 : 2) void k_fused_mfma
           mask_scores(sacc, mk, h);
         }
         bf16x8_t pf[4];
-        float lt = tile_exp<false>(sacc, 0.f, pf);
+        float lx = 0.f;
+        float lt = tile_exp<false, LSE>(sacc, 0.f, pf, lx);
         if (__any(msub != 0u)) {
           scale_pairs(pf, msub);
           lt *= mscale;   // 2^-m: the sum of the scaled pairs, exactly
+          if constexpr (LSE) lx *= mscale;
         }
         float lrow = lt + lane_xor32(lt);
         // the slow pass takes the tile when, for some row, the fast pass
@@ -317,9 +339,10 @@ __global__ __launch_bounds__(kThreads * NSET, D == 64 ? 4 : 2) void k_fused_mfma
           // a power of two, 1 if unchanged; a row with nothing accumulated
           // has nothing to rescale (and its reference may fall)
           const float alpha = acc ? exp2_hw(m_run - m_new) : 0.f;
-          lt = tile_exp<true>(sacc, m_new, pf);
+          lt = tile_exp<true, LSE>(sacc, m_new, pf, lx);
           lrow = lt + lane_xor32(lt);
           l_run *= alpha;
+          if constexpr (LSE) lx_run *= alpha;
           m_run = m_new;
           fast_ok = m_run >= 0.f && m_run <= kRefMax;
           msub = fast_ok ? 0x00800080u * (unsigned)m_run : 0u;
@@ -330,6 +353,7 @@ __global__ __launch_bounds__(kThreads * NSET, D == 64 ? 4 : 2) void k_fused_mfma
             for (int r = 0; r < 16; ++r) oacc[b][r] *= alpha;
         }
         l_run += lt;
+        if constexpr (LSE) lx_run += lx;
         acc = acc || lrow > 0.f;
         // O^T[d][query] += V^T[d][key] P^T[key][query]; k-step j, element e of
         // lane half h is key 16*j + 8*(e/4) + 4*h + e%4
@@ -353,6 +377,10 @@ __global__ __launch_bounds__(kThreads * NSET, D == 64 ? 4 : 2) void k_fused_mfma
     char* const states = smem_all + G::LDS;
     float* const ml = (float*)(states + (NSET - 1) * 4 * kState);
     static_assert(G::LDS + (NSET - 1) * 4 * (kState + 512) <= NSET * G::LDS, "states fit");
+    // ... and LSE's sums behind the staged output
+    float* const sums = (float*)(smem_all + 4 * 32 * (D * (int)sizeof(OutT) + 16));
+    static_assert(!LSE || 4 * 32 * (D * (int)sizeof(OutT) + 16) + (NSET - 1) * 4 * 256 <= G::LDS,
+                  "sums fit");
     if (set > 0) {
       char* const mine = states + ((set - 1) * 4 + wave) * kState;
 #pragma unroll
@@ -365,6 +393,7 @@ __global__ __launch_bounds__(kThreads * NSET, D == 64 ? 4 : 2) void k_fused_mfma
       float* const st = ml + ((set - 1) * 4 + wave) * 128;
       st[lane] = acc ? m_run : -INFINITY;
       st[64 + lane] = l_run;
+      if constexpr (LSE) sums[((set - 1) * 4 + wave) * 64 + lane] = lx_run;
     }
     __syncthreads();
     if (set > 0) return;
@@ -375,6 +404,7 @@ __global__ __launch_bounds__(kThreads * NSET, D == 64 ? 4 : 2) void k_fused_mfma
     auto factor = [&](float mq) { return mq == -INFINITY ? 0.f : exp2_hw(mq - mt); };
     const float f0 = factor(acc ? m_run : -INFINITY);
     l_run *= f0;
+    if constexpr (LSE) lx_run *= f0, m_run = mt;
 #pragma unroll
     for (int b = 0; b < NDB; ++b)
 #pragma unroll
@@ -384,6 +414,7 @@ __global__ __launch_bounds__(kThreads * NSET, D == 64 ? 4 : 2) void k_fused_mfma
       const float* const st = ml + (q * 4 + wave) * 128;
       const float f = factor(st[lane]);
       l_run = fmaf(st[64 + lane], f, l_run);
+      if constexpr (LSE) lx_run = fmaf(sums[(q * 4 + wave) * 64 + lane], f, lx_run);
       const char* const other = states + (q * 4 + wave) * kState;
 #pragma unroll
       for (int b = 0; b < NDB; ++b)
@@ -400,6 +431,20 @@ __global__ __launch_bounds__(kThreads * NSET, D == 64 ? 4 : 2) void k_fused_mfma
 
   const float l_tot = l_run + lane_xor32(l_run);
   const float inv = l_tot > 0.f ? 1.f / l_tot : 0.f;
+  uint64_t bad = 0;                    // LSE: rows to form again, by their lanes
+  if constexpr (LSE) {
+    const float lx = lx_run + lane_xor32(lx_run);
+    if (h == 0 && row_valid)
+      x.lse[(size_t)bh * L + row] =
+          lx == 0.f ? -INFINITY : (m_run + log2f(lx)) * 0.6931471805599453f;
+    float z = 0.f;
+#pragma unroll
+    for (int b = 0; b < NDB; ++b)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) z = fmaf(oacc[b][r] * inv, 0.f, z);
+    bad = __ballot(row_valid && z != z);
+    bad = (bad | bad >> 32) & 0xffffffffu;
+  }
   // O leaves through LDS: each wavefront stages its 32 rows (rows padded by
   // 16 bytes; after the loop's last barrier no wavefront reads the ring), then
   // writes whole rows, 16 bytes per lane with consecutive lanes along a row,
@@ -426,8 +471,31 @@ __global__ __launch_bounds__(kThreads * NSET, D == 64 ? 4 : 2) void k_fused_mfma
     const int r = idx / CPRO, c = idx % CPRO;
     const int orow = __shfl(row, r);           // lane r holds query row r of the wavefront
     const u32x4_t v = *(const u32x4_t*)(stage + r * RS + c * 16);
-    if (r < nrows_w) store16_nt(ohead + (size_t)orow * (D * SZ) + c * 16, v);
+    if (r < nrows_w && (!LSE || !((bad >> r) & 1)))
+      store16_nt(ohead + (size_t)orow * (D * SZ) + c * 16, v);
   }
+  if constexpr (LSE)
+    for (; bad; bad &= bad - 1)
+      fused_row<D>(__builtin_amdgcn_readlane(row, __builtin_ctzll(bad)), lane, x.runs, x.row_ptr, L,
+                   Q + head, Kh, Vh, x.scale, O + head, x.lse + (size_t)bh * L);
+}
+
+template <int D, typename OutT, int NSET>
+__global__ __launch_bounds__(kThreads * NSET, D == 64 ? 4 : 2) void k_fused_mfma(
+    const Group* __restrict__ groups, const int32_t* __restrict__ rows,
+    const Tile* __restrict__ tiles, const uint64_t* __restrict__ masks, int L, int BH,
+    const __bf16* __restrict__ Q, const __bf16* K, const __bf16* V, float sl2,
+    OutT* __restrict__ O) {
+  fused_tiles<D, OutT, NSET, false>(groups, rows, tiles, masks, L, BH, Q, K, V, sl2, O, LseArgs{});
+}
+
+template <int D, int NSET>
+__global__ __launch_bounds__(kThreads * NSET, D == 64 ? 4 : 2) void k_fused_mfma_lse(
+    const Group* __restrict__ groups, const int32_t* __restrict__ rows,
+    const Tile* __restrict__ tiles, const uint64_t* __restrict__ masks, int L, int BH,
+    const __bf16* __restrict__ Q, const __bf16* K, const __bf16* V, float sl2,
+    __bf16* __restrict__ O, const LseArgs x) {
+  fused_tiles<D, __bf16, NSET, true>(groups, rows, tiles, masks, L, BH, Q, K, V, sl2, O, x);
 }
 
 }  // namespace
@@ -471,6 +539,31 @@ hipError_t fused_launch(const DevAcsr& a, int BH, const void* Q, const void* K, 
   return hipGetLastError();
 }
 
+template <int D, int NSET>
+hipError_t allow_lds_lse() {
+  return hipFuncSetAttribute((const void*)k_fused_mfma_lse<D, NSET>,
+                             hipFuncAttributeMaxDynamicSharedMemorySize, NSET * Geo<D>::LDS);
+}
+
+template <int D, int NSET>
+hipError_t lse_launch(const DevAcsr& a, int BH, const void* Q, const void* K, const void* V,
+                      float sl2, void* O, const LseArgs& x, hipStream_t st) {
+  hipLaunchKernelGGL((k_fused_mfma_lse<D, NSET>), dim3(a.n_groups * BH), dim3(kThreads * NSET),
+                     NSET * Geo<D>::LDS, st, a.groups, a.rows, a.tiles, a.masks, a.L, BH,
+                     (const __bf16*)Q, (const __bf16*)K, (const __bf16*)V, sl2, (__bf16*)O, x);
+  return hipGetLastError();
+}
+
+template <int D>
+hipError_t fused_lse(const DevAcsr& a, int BH, const void* Q, const void* K, const void* V,
+                     float sl2, void* O, const LseArgs& x, hipStream_t st) {
+  const int sets = fused_mfma_sets(a, BH, D);
+  if constexpr (D == 64)
+    if (sets == 4) return lse_launch<D, 4>(a, BH, Q, K, V, sl2, O, x, st);
+  return sets >= 2 ? lse_launch<D, 2>(a, BH, Q, K, V, sl2, O, x, st)
+                   : lse_launch<D, 1>(a, BH, Q, K, V, sl2, O, x, st);
+}
+
 template <int D, typename OutT>
 hipError_t fused_out(const DevAcsr& a, int BH, const void* Q, const void* K, const void* V,
                      float sl2, void* O, hipStream_t st) {
@@ -500,12 +593,20 @@ hipError_t prepare_fused_mfma() {
   also(allow_lds<64, float, 4>()), also(allow_lds<64, __bf16, 4>());
   also(allow_lds<128, float, 1>()), also(allow_lds<128, __bf16, 1>());
   also(allow_lds<128, float, 2>()), also(allow_lds<128, __bf16, 2>());
+  also(allow_lds_lse<64, 1>()), also(allow_lds_lse<64, 2>()), also(allow_lds_lse<64, 4>());
+  also(allow_lds_lse<128, 1>()), also(allow_lds_lse<128, 2>());
   return e;
 }
 
 hipError_t launch_fused_mfma(const DevAcsr& a, int BH, int d, const void* Q, const void* K,
-                             const void* V, float scale, void* O, int out_dtype, hipStream_t st) {
+                             const void* V, float scale, void* O, int out_dtype, float* lse,
+                             hipStream_t st) {
   const float sl2 = (float)((double)scale * 1.4426950408889634074);  // scale * log2(e)
+  if (lse) {
+    const LseArgs x{lse, a.row_ptr, a.runs, scale};
+    return d == 64 ? fused_lse<64>(a, BH, Q, K, V, sl2, O, x, st)
+                   : fused_lse<128>(a, BH, Q, K, V, sl2, O, x, st);
+  }
   if (d == 64) return fused_d<64>(a, BH, Q, K, V, sl2, O, out_dtype, st);
   return fused_d<128>(a, BH, Q, K, V, sl2, O, out_dtype, st);
 }

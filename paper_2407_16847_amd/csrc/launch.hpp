@@ -60,9 +60,12 @@ Route unfused_route(const DevAcsr& a, int dtype, int BH, int d, bool colmajor, b
 // Every launcher enqueues on `st` and returns the launch status.
 // dtype / out dtype: 0 = fp32, 1 = bf16.
 
+// The fused forward.  lse: also the rows' log-sum-exp [BH, L] (O then has the
+// inputs' dtype), or null.
 // fp32: on the matrix cores, a workgroup per 32 rows, or a wavefront per row.
 hipError_t launch_fused_f32(const DevAcsr& a, int BH, int d, const void* Q, const void* K,
-                            const void* V, float scale, void* O, int out_dtype, hipStream_t st);
+                            const void* V, float scale, void* O, int out_dtype, float* lse,
+                            hipStream_t st);
 // The single steps, either dtype: the kernel that suits the launch.
 // colmajor: P holds the column-major values (requires a.cols).
 hipError_t launch_rsddmm(const DevAcsr& a, int dtype, int BH, int d, const void* Q, const void* K,
@@ -89,10 +92,22 @@ hipError_t launch_transpose_colmajor(const DevAcsr& a, int BH, const float* P, f
 // Row softmax, any row length (rows of up to 2048 values in registers).
 hipError_t launch_softmax(const DevAcsr& a, int BH, const float* S, float* P, hipStream_t st);
 
+// The backward pass: O, dO and the gradients have Q's dtype; ws holds two floats
+// per query row (2 * BH * L).
+struct BwdArgs {
+  const void *Q, *K, *V, *O, *dO;
+  const float* lse;
+  float* ws;
+  void *dQ, *dK, *dV;
+};
+hipError_t launch_bwd(const DevAcsr& a, int dtype, int BH, int d, const BwdArgs& x, float scale,
+                      hipStream_t st);
+
 // Allows the fused kernels their dynamic LDS (above the default limit at
 // d = 128) on the current device.  Called once per handle at build time, on
 // the handle's device, so launches never change kernel attributes.
 hipError_t prepare_fused_mfma();
+hipError_t prepare_bwd();   // ... and the backward kernels, for handles with the transposed plan
 
 // Index checks of a build with -DSPLAT_DEBUG_BOUNDS (no-ops otherwise): each
 // kernel file's flags on the current device, OR-ed into *bits (bit k = kind
@@ -100,11 +115,13 @@ hipError_t prepare_fused_mfma();
 hipError_t bounds_collect_mfma(uint32_t* bits, bool clear);
 hipError_t bounds_collect_tiles(uint32_t* bits, bool clear);
 hipError_t bounds_collect_slices(uint32_t* bits, bool clear);
+hipError_t bounds_collect_grad(uint32_t* bits, bool clear);
 // One check of `index` against [0, n) as kind `kind`, run on the device
 // (allocates and frees one int); *result = the checked index.
 hipError_t bounds_probe(int kind, int index, int n, int* result);
 
 hipError_t launch_fused_mfma(const DevAcsr& a, int BH, int d, const void* Q, const void* K,
-                             const void* V, float scale, void* O, int out_dtype, hipStream_t st);
+                             const void* V, float scale, void* O, int out_dtype, float* lse,
+                             hipStream_t st);
 
 }  // namespace splat
