@@ -468,6 +468,114 @@ splat_status splat_sparse_mhsa_bwd(splat_acsr_t h, splat_dtype dtype, int32_t B,
                                    void* dV, float* workspace, void* stream);
 
 /*
+ * Rotary positions: features t of a head form pairs, and pair t of the token at
+ * position m turns by the angle m f_t:
+ *
+ *     (x, y) -> (x cos - y sin, y cos + x sin) * magnitude
+ *
+ * The first rot_dim features take part, the others stay as they are.  Pair t is
+ * features (t, t + rot_dim/2), or (2t, 2t + 1) if interleaved.  The frequency of
+ * pair t is f_t = base^(-2t/rot_dim), for longer contexts divided by `factor`;
+ * with a ramp (ramp_lo < ramp_hi) only as far as the pair turns seldom in
+ * original_len positions: with n = original_len f_t / 2 pi turns and
+ * k = (n - ramp_lo)/(ramp_hi - ramp_lo) clamped to [0, 1], f_t becomes
+ * k f_t + (1 - k) f_t / factor.
+ *
+ * splat_rotary_build -- a handle with the cosines and sines of positions
+ * 0 .. max_len - 1: fp32, from angles in 64 bits, max_len * rot_dim * 4 bytes on
+ * the current device (host-only without a GPU).  INVALID_ARG for a bad
+ * descriptor.  Handles are immutable and may be used by several host threads.
+ * splat_rotary_export -- a host copy of the table [max_len, rot_dim/2, 2].
+ */
+#define SPLAT_ROTARY_MAX_LEN 1048576
+typedef struct {
+  int32_t max_len;         /* positions, 1 .. SPLAT_ROTARY_MAX_LEN */
+  int32_t rot_dim;         /* features that turn: a multiple of 16 up to d */
+  int32_t interleaved;     /* 0 or 1 */
+  int32_t original_len;    /* with a ramp: >= 1 */
+  double base;             /* > 1 */
+  double factor;           /* >= 1 */
+  double ramp_lo, ramp_hi; /* 0, 0: no ramp */
+  double magnitude;        /* > 0 */
+} splat_rotary_desc;
+
+typedef struct splat_rotary* splat_rotary_t;
+splat_status splat_rotary_build(const splat_rotary_desc* desc, splat_rotary_t* out);
+void splat_rotary_destroy(splat_rotary_t r); /* NULL is a no-op */
+splat_status splat_rotary_export(splat_rotary_t r, float* table);
+
+/* A [B, heads, T, d] tensor by its strides in elements: feature stride 1, the
+ * others >= 0 and multiples of 16 bytes.  data: 16-byte aligned device memory. */
+typedef struct {
+  void* data;
+  int64_t stride_b, stride_h, stride_t;
+  int32_t heads;
+} splat_heads;
+
+/*
+ * splat_rotary_apply -- y = the rotation of x, for one tensor or two (a layer's Q
+ * and K; x2 and y2 NULL for one) of `dtype`.  positions: int32 [B, T] on the
+ * device, NULL for 0 .. T-1.  inverse: the transposed rotation, which is the
+ * gradient (and, at magnitude 1, the inverse).  A token whose position lies
+ * outside [0, max_len) gets NaN in its rotated features.  fp32 arithmetic, one
+ * rounding.  y may be x itself (same strides) and otherwise shares no memory
+ * with either input or the other output (INVALID_ARG).
+ */
+splat_status splat_rotary_apply(splat_rotary_t r, splat_dtype dtype, int32_t B, int32_t T, int32_t d,
+                                const int32_t* positions, const splat_heads* x1, const splat_heads* y1,
+                                const splat_heads* x2, const splat_heads* y2, int32_t inverse,
+                                void* stream);
+
+/*
+ * The paged cache: keys and values in pages of `page` tokens, k and v
+ * [n_pages, heads, page, d] contiguous device memory of `dtype`; sequence b's
+ * token at position m lies in page table[b * max_pages + m / page], at place
+ * m % page.  page is a power of two up to 65536.  The tables live on the device
+ * and are not seen by the host: the kernels check what they use.
+ */
+typedef struct {
+  void *k, *v;
+  const int32_t* table; /* [B, max_pages] */
+  int32_t n_pages, heads, page, max_pages;
+} splat_cache;
+
+/*
+ * splat_cache_append -- writes T new tokens of each sequence into the cache, the
+ * first of sequence b at position start[b], with the position rotation of K on
+ * the way (r NULL: none).  K, V: [B, cache heads, T, d].  counts[b] (NULL: T)
+ * tokens of sequence b are new, the rest padding: padding is not written, and
+ * neither is a token whose position is negative or past the table, or whose page
+ * lies outside [0, n_pages); everything else in the cache stays as it was.  Two
+ * tokens of one call must not share a place.  Q, Qr (both NULL: none): the step's
+ * queries [B, heads, T, d] and their rotation at the same positions, 0 in padding
+ * rows; Qr may be Q itself, otherwise it shares no memory with another argument.
+ * Positions past r's max_len give NaN, as in splat_rotary_apply.
+ */
+splat_status splat_cache_append(splat_rotary_t r, splat_dtype dtype, int32_t B, int32_t T, int32_t d,
+                                const splat_cache* cache, const int32_t* start,
+                                const int32_t* counts, const splat_heads* K, const splat_heads* V,
+                                const splat_heads* Q, const splat_heads* Qr, void* stream);
+
+/*
+ * splat_sparse_mhsa_decode -- the attention of one query token a sequence over the
+ * paged cache: sequence b, of lengths[b] tokens, has the mask's row
+ * lengths[b] - 1, of which the columns below lengths[b] count.
+ * Q, O: [B, H, 1, d] contiguous, of `dtype`.  H is a multiple of the cache's heads:
+ * query head h reads head h / (H / heads).  Length 0, or a row without columns:
+ * O = 0.  A length outside [0, L] or past the table, or a page outside
+ * [0, n_pages) among the row's keys: NaN in that sequence's O.  fp32 arithmetic,
+ * one rounding, a fixed order of sums.  O shares no memory with the inputs.
+ * workspace: splat_decode_workspace() bytes, 16-byte aligned, that the call writes
+ * and reads (calls that may run at the same time need one each); NULL if 0.
+ */
+splat_status splat_decode_workspace(splat_acsr_t h, int32_t B, int32_t H, int32_t heads, int32_t d,
+                                    int64_t* bytes);
+splat_status splat_sparse_mhsa_decode(splat_acsr_t h, splat_dtype dtype, int32_t B, int32_t H,
+                                      int32_t d, const void* Q, const splat_cache* cache,
+                                      const int32_t* lengths, float scale, void* O, void* workspace,
+                                      void* stream);
+
+/*
  * splat_debug_bounds -- index checks of a checked build (built with
  * -DSPLAT_DEBUG_BOUNDS: libsplat_checked.so beside libsplat.so; a debugging
  * aid, not part of the method).  In a checked build every kernel checks the

@@ -26,7 +26,8 @@ __all__ = [
     "SplatError", "Pattern", "Acsr", "load", "lib_path", "rsddmm", "row_softmax", "rspmm",
     "sparse_mhsa_fwd", "MAX_RUNS", "MAX_TERMS", "PLAN_NO_SPAN", "NO_SPAN_MAX_L", "PLAN_COLUMNS",
     "DENSE_ALPHA", "transpose_colmajor", "rspmm_colmajor", "sparse_mhsa_unfused",
-    "sparse_mhsa_fwd_lse", "sparse_mhsa_bwd", "PLAN_GRAD",
+    "sparse_mhsa_fwd_lse", "sparse_mhsa_bwd", "PLAN_GRAD", "Rotary", "rotary", "cache_append",
+    "sparse_mhsa_decode", "decode_workspace",
 ]
 
 MAX_TERMS = 8
@@ -70,6 +71,24 @@ class TilingStats(ctypes.Structure):
                 ("redundant", ctypes.c_int64), ("reuse", ctypes.c_double),
                 ("coalesced", ctypes.c_double), ("cost", ctypes.c_double),
                 ("stretch", ctypes.c_int32), ("iterations", ctypes.c_int32)]
+
+
+class RotaryDesc(ctypes.Structure):
+    _fields_ = [("max_len", ctypes.c_int32), ("rot_dim", ctypes.c_int32),
+                ("interleaved", ctypes.c_int32), ("original_len", ctypes.c_int32),
+                ("base", ctypes.c_double), ("factor", ctypes.c_double), ("ramp_lo", ctypes.c_double),
+                ("ramp_hi", ctypes.c_double), ("magnitude", ctypes.c_double)]
+
+
+class Heads(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("stride_b", ctypes.c_int64), ("stride_h", ctypes.c_int64),
+                ("stride_t", ctypes.c_int64), ("heads", ctypes.c_int32)]
+
+
+class Cache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("table", ctypes.c_void_p),
+                ("n_pages", ctypes.c_int32), ("heads", ctypes.c_int32), ("page", ctypes.c_int32),
+                ("max_pages", ctypes.c_int32)]
 
 
 TILING_METHODS = {"poset": 0, "grid": 1, "naive": 2}
@@ -133,6 +152,14 @@ def _open(path: str) -> ctypes.CDLL:
         "splat_sparse_mhsa_fwd_lse": [vp, i32, i32, i32, i32, vp, vp, vp, f32, vp, vp, vp],
         "splat_sparse_mhsa_bwd": [vp, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, f32, vp, vp, vp, vp,
                                   vp],
+        "splat_rotary_build": [P(RotaryDesc), P(vp)],
+        "splat_rotary_export": [vp, vp],
+        "splat_rotary_apply": [vp, i32, i32, i32, i32, vp, P(Heads), P(Heads), P(Heads), P(Heads), i32,
+                               vp],
+        "splat_cache_append": [vp, i32, i32, i32, i32, P(Cache), vp, vp, P(Heads), P(Heads), P(Heads),
+                               P(Heads), vp],
+        "splat_decode_workspace": [vp, i32, i32, i32, i32, P(i64)],
+        "splat_sparse_mhsa_decode": [vp, i32, i32, i32, i32, vp, P(Cache), vp, f32, vp, vp, vp],
         "splat_sparse_mhsa_unfused_noalloc": [vp, i32, i32, i32, i32, vp, vp, vp, f32, vp, i32, f32,
                                               P(i32), vp],
         "splat_acsr_export_csc": [vp, vp, vp],
@@ -151,6 +178,8 @@ def _open(path: str) -> ctypes.CDLL:
         fn.restype = ctypes.c_int
     lib.splat_acsr_destroy.argtypes = [vp]
     lib.splat_acsr_destroy.restype = None
+    lib.splat_rotary_destroy.argtypes = [vp]
+    lib.splat_rotary_destroy.restype = None
     lib.splat_last_error.restype = ctypes.c_char_p
     lib.splat_version.restype = ctypes.c_char_p
     return lib
@@ -564,6 +593,207 @@ def sparse_mhsa_bwd(acsr: Acsr, Q: torch.Tensor, K: torch.Tensor, V: torch.Tenso
                                         dO.data_ptr(), float(scale), dQ.data_ptr(), dK.data_ptr(),
                                         dV.data_ptr(), workspace.data_ptr(), _stream()))
     return dQ, dK, dV
+
+
+class Rotary:
+    """Rotary positions (see splat_rotary_build): the cosines and sines of
+    positions 0 .. max_len - 1 on the current device."""
+
+    def __init__(self, max_len: int, rot_dim: int, *, base: float = 10000.0, interleaved: bool = False,
+                 factor: float = 1.0, ramp: Optional[Tuple[float, float]] = None,
+                 original_len: int = 0, magnitude: float = 1.0):
+        """The first rot_dim features turn: pairs (t, t + rot_dim/2), or (2t,
+        2t + 1) if interleaved.  factor divides the frequencies; with ramp = (lo,
+        hi) only those of pairs that turn fewer than lo times in original_len
+        positions, fading out until hi.  magnitude multiplies the result."""
+        lo, hi = (0.0, 0.0) if ramp is None else ramp
+        self.desc = RotaryDesc(int(max_len), int(rot_dim), int(bool(interleaved)), int(original_len),
+                               float(base), float(factor), float(lo), float(hi), float(magnitude))
+        self._h = ctypes.c_void_p()
+        self._lib = load()
+        if ramp is not None and not hi > lo:
+            raise ValueError("ramp must be (lo, hi) with lo < hi")
+        _check(self._lib.splat_rotary_build(ctypes.byref(self.desc), ctypes.byref(self._h)))
+
+    def close(self) -> None:
+        if getattr(self, "_h", None) is not None and self._h.value:
+            self._lib.splat_rotary_destroy(self._h)
+            self._h = ctypes.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    @property
+    def handle(self) -> ctypes.c_void_p:
+        if not self._h.value:
+            raise ValueError("rotary handle is closed")
+        return self._h
+
+    def export(self) -> np.ndarray:
+        """The table [max_len, rot_dim/2, 2] of cosines and sines (times magnitude)."""
+        t = np.zeros((self.desc.max_len, self.desc.rot_dim // 2, 2), dtype=np.float32)
+        _check(self._lib.splat_rotary_export(self.handle, t.ctypes.data_as(ctypes.c_void_p)))
+        return t
+
+
+def _heads(x: torch.Tensor, name: str, ref: Optional[torch.Tensor] = None) -> Heads:
+    """x [B, heads, T, d] by its strides; dtype, device, B, T and d of ref."""
+    if not isinstance(x, torch.Tensor) or not x.is_cuda:
+        raise TypeError(f"{name} must be a CUDA (HIP) tensor")
+    if x.dtype not in _DT:
+        raise TypeError(f"{name} must be float32 or bfloat16, got {x.dtype}")
+    if x.dim() != 4 or 0 in x.shape:
+        raise ValueError(f"{name} must be [B, heads, T, d] with no empty axis, got {tuple(x.shape)}")
+    if x.stride(3) != 1:
+        raise ValueError(f"{name}'s features must be contiguous")
+    if ref is not None and ref is not x:
+        if x.dtype != ref.dtype or (x.shape[0], *x.shape[2:]) != (ref.shape[0], *ref.shape[2:]):
+            raise ValueError(f"{name} must match {tuple(ref.shape)} {ref.dtype} in dtype, B, T and d, "
+                             f"got {tuple(x.shape)} {x.dtype}")
+        _on(x, name, ref)
+    sb, sh, st, _ = x.stride()
+    return Heads(x.data_ptr(), sb, sh, st, x.shape[1])
+
+
+def _ints(x: torch.Tensor, name: str, shape, ref: torch.Tensor) -> int:
+    """The address of x, contiguous int32 of `shape` on ref's device."""
+    if not isinstance(x, torch.Tensor) or not x.is_cuda:
+        raise TypeError(f"{name} must be a CUDA (HIP) tensor")
+    if x.dtype != torch.int32 or tuple(x.shape) != tuple(shape) or not x.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous int32 {list(shape)} tensor, "
+                         f"got {x.dtype} {list(x.shape)}")
+    _on(x, name, ref)
+    return x.data_ptr()
+
+
+def _turned(x: torch.Tensor, y: Optional[torch.Tensor], name: str) -> Tuple[torch.Tensor, Heads]:
+    """The output for x: y, or a new contiguous tensor."""
+    if y is None:
+        y = torch.empty(tuple(x.shape), dtype=x.dtype, device=x.device)
+    h = _heads(y, name, x)
+    if y.shape != x.shape:
+        raise ValueError(f"{name} must be {tuple(x.shape)}, got {tuple(y.shape)}")
+    return y, h
+
+
+def rotary(rot: Rotary, X: torch.Tensor, X2: Optional[torch.Tensor] = None, *,
+           positions: Optional[torch.Tensor] = None, inverse: bool = False,
+           Y: Optional[torch.Tensor] = None, Y2: Optional[torch.Tensor] = None):
+    """X [B, H, T, d] (any strides, contiguous features) rotated to its tokens'
+    positions -- int32 [B, T], or 0 .. T-1 -- as a contiguous tensor, or into Y,
+    which may be X.  With X2 (its own number of heads; a layer's Q and K in one
+    launch) returns both.  inverse=True: the transposed rotation, its gradient."""
+    x, (Y, y) = _heads(X, "X"), _turned(X, Y, "Y")
+    pair = X2 is not None
+    x2, y2 = None, None
+    if pair:
+        x2 = _heads(X2, "X2", X)
+        Y2, y2 = _turned(X2, Y2, "Y2")
+    elif Y2 is not None:
+        raise ValueError("Y2 needs X2")
+    B, _, T, d = X.shape
+    pos = None if positions is None else _ints(positions, "positions", (B, T), X)
+    _check(load().splat_rotary_apply(rot.handle, _DT[X.dtype], B, T, d, pos, ctypes.byref(x),
+                                     ctypes.byref(y), ctypes.byref(x2) if pair else None,
+                                     ctypes.byref(y2) if pair else None, int(bool(inverse)), _stream()))
+    return (Y, Y2) if pair else Y
+
+
+def _cache(k_cache: torch.Tensor, v_cache: torch.Tensor, table: torch.Tensor, ref: torch.Tensor) -> Cache:
+    """The paged cache, checked against ref [B, heads, T, d]."""
+    for x, name in ((k_cache, "k_cache"), (v_cache, "v_cache")):
+        if not isinstance(x, torch.Tensor) or not x.is_cuda:
+            raise TypeError(f"{name} must be a CUDA (HIP) tensor")
+        if x.dim() != 4 or x.dtype != ref.dtype or x.shape[3] != ref.shape[3] or not x.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous {ref.dtype} [pages, heads, page, "
+                             f"{ref.shape[3]}] tensor, got {x.dtype} {list(x.shape)}")
+        _on(x, name, ref)
+    if v_cache.shape != k_cache.shape:
+        raise ValueError("k_cache and v_cache must have one shape")
+    if not isinstance(table, torch.Tensor) or table.dim() != 2:
+        raise ValueError("table must be [B, max_pages]")
+    at = _ints(table, "table", (ref.shape[0], table.shape[1]), ref)
+    n, heads, page, _ = k_cache.shape
+    return Cache(k_cache.data_ptr(), v_cache.data_ptr(), at, n, heads, page, table.shape[1])
+
+
+def cache_append(k_cache: torch.Tensor, v_cache: torch.Tensor, table: torch.Tensor,
+                 start: torch.Tensor, K: torch.Tensor, V: torch.Tensor, *,
+                 counts: Optional[torch.Tensor] = None, rot: Optional[Rotary] = None,
+                 Q: Optional[torch.Tensor] = None, Qr: Optional[torch.Tensor] = None
+                 ) -> Optional[torch.Tensor]:
+    """Writes K and V [B, heads, T, d] into the paged cache ([pages, heads, page,
+    d] each; table int32 [B, max_pages]), the first token of sequence b at
+    position start[b], K rotated on the way; only the first counts[b] tokens, if
+    given.  With Q [B, H, T, d] returns its rotation at the same positions (in Qr,
+    if given; padding rows 0)."""
+    k = _heads(K, "K")
+    v = _heads(V, "V", K)
+    B, _, T, d = K.shape
+    c = _cache(k_cache, v_cache, table, K)
+    first = _ints(start, "start", (B,), K)
+    n = None if counts is None else _ints(counts, "counts", (B,), K)
+    q, qr = None, None
+    if Q is not None:
+        q = _heads(Q, "Q", K)
+        Qr, qr = _turned(Q, Qr, "Qr")
+    elif Qr is not None:
+        raise ValueError("Qr needs Q")
+    _check(load().splat_cache_append(rot.handle if rot is not None else None, _DT[K.dtype], B, T, d,
+                                     ctypes.byref(c), first, n, ctypes.byref(k), ctypes.byref(v),
+                                     ctypes.byref(q) if q is not None else None,
+                                     ctypes.byref(qr) if q is not None else None, _stream()))
+    return Qr
+
+
+def decode_workspace(acsr: Acsr, B: int, H: int, heads: int, d: int) -> int:
+    """Bytes of workspace that sparse_mhsa_decode takes (0: none)."""
+    n = ctypes.c_int64()
+    _check(acsr._lib.splat_decode_workspace(acsr.handle, B, H, heads, d, ctypes.byref(n)))
+    return int(n.value)
+
+
+def sparse_mhsa_decode(acsr: Acsr, Q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor,
+                       table: torch.Tensor, lengths: torch.Tensor, scale: float,
+                       O: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None
+                       ) -> torch.Tensor:
+    """One query token a sequence, Q [B, H, 1, d], over the paged cache: the
+    mask's row lengths[b] - 1, its columns below lengths[b] (int32 [B]).  The
+    cache's heads divide H.  workspace: at least decode_workspace() bytes, made by
+    the call unless given."""
+    if not isinstance(Q, torch.Tensor) or not Q.is_cuda:
+        raise TypeError("Q must be a CUDA (HIP) tensor")
+    if Q.dtype not in _DT:
+        raise TypeError(f"Q must be float32 or bfloat16, got {Q.dtype}")
+    if Q.dim() != 4 or Q.shape[2] != 1 or not Q.is_contiguous():
+        raise ValueError(f"Q must be a contiguous [B, H, 1, d] tensor, got {tuple(Q.shape)}")
+    B, H, _, d = Q.shape
+    c = _cache(k_cache, v_cache, table, Q)
+    at = _ints(lengths, "lengths", (B,), Q)
+    if O is None:
+        O = _new(Q, Q.dtype)
+    else:
+        if not isinstance(O, torch.Tensor) or not O.is_cuda:
+            raise TypeError("O must be a CUDA (HIP) tensor")
+        if O.dtype != Q.dtype or O.shape != Q.shape or not O.is_contiguous():
+            raise ValueError(f"O must be a contiguous {Q.dtype} {list(Q.shape)} tensor")
+        _on(O, "O", Q)
+    need = decode_workspace(acsr, B, H, c.heads, d)
+    if workspace is not None:
+        if not isinstance(workspace, torch.Tensor) or not workspace.is_cuda:
+            raise TypeError("workspace must be a CUDA (HIP) tensor")
+        if workspace.numel() * workspace.element_size() < need or not workspace.is_contiguous():
+            raise ValueError(f"workspace must be contiguous and hold {need} bytes")
+        _on(workspace, "workspace", Q)
+    elif need:
+        workspace = torch.empty(need // 4, dtype=torch.float32, device=Q.device)
+    _check(load().splat_sparse_mhsa_decode(acsr.handle, _DT[Q.dtype], B, H, d, Q.data_ptr(),
+                                           ctypes.byref(c), at, float(scale), O.data_ptr(),
+                                           workspace.data_ptr() if need else None, _stream()))
+    return O
 
 
 def _result(x: Optional[torch.Tensor], name: str, Q: torch.Tensor, acsr: Acsr) -> torch.Tensor:

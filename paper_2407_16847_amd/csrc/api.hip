@@ -13,6 +13,7 @@
 #include "../../include/splat.h"
 #include "acsr_host.hpp"
 #include "launch.hpp"
+#include "rotary_host.hpp"
 #include "tiling.hpp"
 
 using splat::DevAcsr;
@@ -23,6 +24,12 @@ struct splat_acsr {
   int device = -1;
   void* dmem = nullptr;
   DevAcsr dev{};
+};
+
+struct splat_rotary {
+  splat::HostRotary host;
+  int device = -1;
+  float* dmem = nullptr;
 };
 
 namespace {
@@ -88,6 +95,8 @@ splat_status upload(splat_acsr* h) {
   e = splat::prepare_fused_mfma();
   if (e != hipSuccess)
     return fail(SPLAT_ERR_HIP, "hipFuncSetAttribute (fused kernel LDS): %s", hipGetErrorString(e));
+  if ((e = splat::prepare_decode()) != hipSuccess)
+    return fail(SPLAT_ERR_HIP, "hipFuncSetAttribute (decode kernel LDS): %s", hipGetErrorString(e));
   if (h->host.has_grad && (e = splat::prepare_bwd()) != hipSuccess)
     return fail(SPLAT_ERR_HIP, "hipFuncSetAttribute (backward kernels' LDS): %s",
                 hipGetErrorString(e));
@@ -176,19 +185,23 @@ splat_status check_batch(int32_t B, int32_t H) {
   return SPLAT_OK;
 }
 
+// A handle's device is there and is the current one.
+splat_status check_device(int device, const char* what) {
+  if (device < 0) return fail(SPLAT_ERR_NO_DEVICE, "the %s handle was built without a GPU", what);
+  int dev = -1;
+  hipError_t e = hipGetDevice(&dev);
+  if (e != hipSuccess) return fail(SPLAT_ERR_HIP, "hipGetDevice: %s", hipGetErrorString(e));
+  if (dev != device)
+    return fail(SPLAT_ERR_INVALID_ARG, "current device %d differs from the handle's device %d", dev,
+                device);
+  return SPLAT_OK;
+}
+
 splat_status check_handle(splat_acsr_t h, int32_t B, int32_t H) {
   if (!h) return fail(SPLAT_ERR_INVALID_ARG, "ACSR handle is NULL");
   splat_status s = check_batch(B, H);
   if (s != SPLAT_OK) return s;
-  if (h->device < 0)
-    return fail(SPLAT_ERR_NO_DEVICE, "the ACSR handle was built without a GPU");
-  int dev = -1;
-  hipError_t e = hipGetDevice(&dev);
-  if (e != hipSuccess) return fail(SPLAT_ERR_HIP, "hipGetDevice: %s", hipGetErrorString(e));
-  if (dev != h->device)
-    return fail(SPLAT_ERR_INVALID_ARG, "current device %d differs from the handle's device %d", dev,
-                h->device);
-  return SPLAT_OK;
+  return check_device(h->device, "ACSR");
 }
 
 // The bf16 kernels run one 256-thread workgroup per (row group, batch*head)
@@ -316,6 +329,124 @@ splat_status check_spans(const Span* in, int n_in, const Span* out, int n_out) {
     for (int i = 0; i < k; ++i) CHECK(apart(out[i]));
   }
   return SPLAT_OK;
+}
+
+// ---- tensors by strides, the paged cache
+// A call's heads: [B, heads, T, d] places of e bytes.
+struct View {
+  const splat_heads* x;
+  const char* name;
+  int32_t B, T, d, e;
+  const char* at() const { return (const char*)x->data; }
+  // bytes from the first place of a token (of the tensor) to past its last
+  int64_t token() const { return ((x->heads - 1) * x->stride_h + d) * e; }
+  int64_t extent() const { return token() + ((B - 1) * x->stride_b + (T - 1) * x->stride_t) * e; }
+  bool same(const View& o) const {
+    return x->data == o.x->data && x->heads == o.x->heads && x->stride_b == o.x->stride_b &&
+           x->stride_h == o.x->stride_h && x->stride_t == o.x->stride_t;
+  }
+};
+
+splat_status check_view(const View& v, bool output) {
+  const splat_heads& x = *v.x;
+  CHECK(check_ptr(x.data, v.name));
+  CHECK(check_batch(v.B, x.heads));
+  const int64_t unit = 16 / v.e, most = int64_t(1) << 40;
+  struct Dim {
+    int64_t n, stride;
+  } dim[3] = {{v.B, x.stride_b}, {x.heads, x.stride_h}, {v.T, x.stride_t}};
+  for (Dim& k : dim) {
+    if (k.n == 1) k.stride = 0;   // never used
+    if (k.stride < 0 || k.stride % unit != 0 || k.stride > most / k.n)
+      return fail(SPLAT_ERR_INVALID_ARG,
+                  "%s: strides must be multiples of 16 bytes, 0 or more", v.name);
+  }
+  if (!output) return SPLAT_OK;
+  // no two places of an output may be one
+  std::sort(dim, dim + 3, [](const Dim& a, const Dim& b) { return a.stride < b.stride; });
+  int64_t reach = v.d;
+  for (const Dim& k : dim) {
+    if (k.n == 1) continue;
+    if (k.stride < reach)
+      return fail(SPLAT_ERR_INVALID_ARG, "%s: an output's places must not overlap", v.name);
+    reach = k.stride * (k.n - 1) + reach;
+  }
+  return SPLAT_OK;
+}
+
+// Whether two views share no memory; views of one buffer that take turns, as Q, K
+// and V of a joint projection, are told apart by their tokens' places.
+bool apart(const View& a, const View& b) {
+  if (!meet(a.at(), a.extent(), b.at(), b.extent())) return true;
+  const int64_t st = a.x->stride_t * a.e;
+  if (a.T == 1 || b.T == 1 || b.x->stride_t * b.e != st || a.token() > st || b.token() > st)
+    return false;
+  for (const View* v : {&a, &b})
+    if (v->B > 1 && (v->x->stride_b * v->e) % st != 0) return false;
+  const int64_t off = ((b.at() - a.at()) % st + st) % st;
+  return off >= a.token() && off + b.token() <= st;
+}
+
+splat_status check_apart(const View& out, const View& in) {
+  if (!apart(out, in))
+    return fail(SPLAT_ERR_INVALID_ARG, "%s must not overlap %s", out.name, in.name);
+  return SPLAT_OK;
+}
+
+splat::HeadsJob heads_job(const View& x, const View* y, bool rotate) {
+  splat::HeadsJob j{};
+  j.x = x.at();
+  j.xb = x.x->stride_b * x.e, j.xh = x.x->stride_h * x.e, j.xt = x.x->stride_t * x.e;
+  j.heads = x.x->heads;
+  j.rotate = rotate;
+  if (y) {
+    j.y = (char*)y->x->data;
+    j.yb = y->x->stride_b * y->e, j.yh = y->x->stride_h * y->e, j.yt = y->x->stride_t * y->e;
+  }
+  return j;
+}
+
+splat_status check_tokens(int32_t B, int32_t T) {
+  if (B < 1 || T < 1 || (int64_t)B * T > INT32_MAX)
+    return fail(SPLAT_ERR_INVALID_ARG, "B and T must be >= 1 with B*T < 2^31 (got B=%d, T=%d)", B, T);
+  return SPLAT_OK;
+}
+
+splat_status check_rotary(splat_rotary_t r, int32_t d) {
+  if (!r) return fail(SPLAT_ERR_INVALID_ARG, "rotary handle is NULL");
+  CHECK(check_device(r->device, "rotary"));
+  if (r->host.desc.rot_dim > d)
+    return fail(SPLAT_ERR_INVALID_ARG, "the rotation takes %d features, the heads have %d",
+                r->host.desc.rot_dim, d);
+  return SPLAT_OK;
+}
+
+void use_rotary(splat::HeadsArgs& a, splat_rotary_t r) {
+  const splat_rotary_desc& d = r->host.desc;
+  a.angles = (const float2*)r->dmem;
+  a.max_len = d.max_len, a.rot = d.rot_dim, a.interleaved = d.interleaved != 0;
+}
+
+splat_status check_cache(const splat_cache* c, int32_t B) {
+  if (!c) return fail(SPLAT_ERR_INVALID_ARG, "cache is NULL");
+  CHECK(check_ptr(c->k, "the cache's k"));
+  CHECK(check_ptr(c->v, "the cache's v"));
+  if (!c->table) return fail(SPLAT_ERR_INVALID_ARG, "the cache's table is NULL");
+  CHECK(check_batch(B, c->heads));
+  if (c->n_pages < 1 || c->max_pages < 1)
+    return fail(SPLAT_ERR_INVALID_ARG, "n_pages and max_pages must be >= 1");
+  if (c->page < 1 || c->page > 65536 || (c->page & (c->page - 1)) != 0)
+    return fail(SPLAT_ERR_INVALID_ARG, "page must be a power of two up to 65536, got %d", c->page);
+  // rows of the cache are counted in 32 bits
+  if ((int64_t)c->n_pages * c->heads > (int64_t)UINT32_MAX / c->page)
+    return fail(SPLAT_ERR_UNSUPPORTED, "the cache holds 2^32 rows or more");
+  return SPLAT_OK;
+}
+
+int32_t log2_of(int32_t page) {
+  int32_t s = 0;
+  while ((1 << s) < page) ++s;
+  return s;
 }
 
 // The unfused chain.  keep_values: the caller reads P in S (and Pt) afterwards;
@@ -732,6 +863,202 @@ splat_status splat_sparse_mhsa_bwd(splat_acsr_t h, splat_dtype dtype, int32_t B,
                   "sparse_mhsa_bwd");
 }
 
+splat_status splat_rotary_build(const splat_rotary_desc* desc, splat_rotary_t* out) {
+  if (!desc || !out) return fail(SPLAT_ERR_INVALID_ARG, "desc and out must be non-NULL");
+  splat_rotary* r = new (std::nothrow) splat_rotary();
+  if (!r) return fail(SPLAT_ERR_OOM, "host allocation failed");
+  auto drop = [&](splat_status s, const char* what, const char* why) {
+    if (r->dmem) (void)hipFree(r->dmem);
+    delete r;
+    return fail(s, "%s%s%s", what, *why ? ": " : "", why);
+  };
+  try {
+    std::string err;
+    const splat_status s = splat::rotary_build(*desc, r->host, err);
+    if (s != SPLAT_OK) return drop(s, err.c_str(), "");
+    int n = 0;
+    if (hipGetDeviceCount(&n) != hipSuccess || n == 0) {
+      (void)hipGetLastError();   // a missing GPU is not an error for a host-only handle
+      *out = r;
+      return ok();
+    }
+    const std::vector<float> table = splat::rotary_table(r->host);
+    hipError_t e = hipGetDevice(&r->device);
+    if (e != hipSuccess) return drop(SPLAT_ERR_HIP, "hipGetDevice", hipGetErrorString(e));
+    e = hipMalloc((void**)&r->dmem, table.size() * sizeof(float));
+    if (e != hipSuccess) {
+      (void)hipGetLastError();
+      r->dmem = nullptr;
+      return drop(SPLAT_ERR_OOM, "hipMalloc for the rotary table", hipGetErrorString(e));
+    }
+    e = hipMemcpy(r->dmem, table.data(), table.size() * sizeof(float), hipMemcpyHostToDevice);
+    if (e != hipSuccess)
+      return drop(SPLAT_ERR_HIP, "hipMemcpy of the rotary table", hipGetErrorString(e));
+  } catch (const std::bad_alloc&) {
+    return drop(SPLAT_ERR_OOM, "host allocation failed", "");
+  }
+  *out = r;
+  return ok();
+}
+
+void splat_rotary_destroy(splat_rotary_t r) {
+  if (!r) return;
+  if (r->dmem) (void)hipFree(r->dmem);
+  delete r;
+}
+
+splat_status splat_rotary_export(splat_rotary_t r, float* table) {
+  if (!r || !table) return fail(SPLAT_ERR_INVALID_ARG, "handle and table must be non-NULL");
+  try {
+    const std::vector<float> t = splat::rotary_table(r->host);
+    std::memcpy(table, t.data(), t.size() * sizeof(float));
+  } catch (const std::bad_alloc&) {
+    return fail(SPLAT_ERR_OOM, "host allocation failed");
+  }
+  return ok();
+}
+
+splat_status splat_rotary_apply(splat_rotary_t r, splat_dtype dtype, int32_t B, int32_t T, int32_t d,
+                                const int32_t* positions, const splat_heads* x1, const splat_heads* y1,
+                                const splat_heads* x2, const splat_heads* y2, int32_t inverse,
+                                void* stream) {
+  CHECK(check_dtype(dtype, "dtype"));
+  CHECK(check_d(d));
+  CHECK(check_tokens(B, T));
+  CHECK(check_rotary(r, d));
+  if (!x1 || !y1) return fail(SPLAT_ERR_INVALID_ARG, "x1 and y1 must be non-NULL");
+  if (!x2 != !y2) return fail(SPLAT_ERR_INVALID_ARG, "x2 and y2 go together");
+  if (inverse != 0 && inverse != 1) return fail(SPLAT_ERR_INVALID_ARG, "inverse must be 0 or 1");
+  const int32_t e = dtype == SPLAT_BF16 ? 2 : 4;
+  const View x[2] = {{x1, "x1", B, T, d, e}, {x2, "x2", B, T, d, e}};
+  const View y[2] = {{y1, "y1", B, T, d, e}, {y2, "y2", B, T, d, e}};
+  const int n = x2 ? 2 : 1;
+  for (int k = 0; k < n; ++k) {
+    CHECK(check_view(x[k], false));
+    CHECK(check_view(y[k], true));
+    if (x[k].x->heads != y[k].x->heads)
+      return fail(SPLAT_ERR_INVALID_ARG, "%s and %s differ in heads", x[k].name, y[k].name);
+  }
+  const size_t pos_bytes = (size_t)B * T * 4;
+  for (int k = 0; k < n; ++k) {
+    for (int i = 0; i < n; ++i)
+      if (!(i == k && y[k].same(x[k]))) CHECK(check_apart(y[k], x[i]));
+    if (k == 1) CHECK(check_apart(y[1], y[0]));
+    if (meet(positions, pos_bytes, y[k].at(), y[k].extent()))
+      return fail(SPLAT_ERR_INVALID_ARG, "%s must not overlap positions", y[k].name);
+  }
+  splat::HeadsArgs a{};
+  a.n_jobs = n, a.B = B, a.T = T;
+  for (int k = 0; k < n; ++k) a.job[k] = heads_job(x[k], &y[k], true);
+  use_rotary(a, r);
+  a.inverse = inverse != 0;
+  a.positions = positions;
+  return launched(splat::launch_heads(a, dtype, d, (hipStream_t)stream), "rotary_apply");
+}
+
+splat_status splat_cache_append(splat_rotary_t r, splat_dtype dtype, int32_t B, int32_t T, int32_t d,
+                                const splat_cache* cache, const int32_t* start,
+                                const int32_t* counts, const splat_heads* K, const splat_heads* V,
+                                const splat_heads* Q, const splat_heads* Qr, void* stream) {
+  CHECK(check_dtype(dtype, "dtype"));
+  CHECK(check_d(d));
+  CHECK(check_tokens(B, T));
+  if (r) CHECK(check_rotary(r, d));
+  CHECK(check_cache(cache, B));
+  if (!start) return fail(SPLAT_ERR_INVALID_ARG, "start is NULL");
+  if (!K || !V) return fail(SPLAT_ERR_INVALID_ARG, "K and V must be non-NULL");
+  if (!Q != !Qr) return fail(SPLAT_ERR_INVALID_ARG, "Q and Qr go together");
+  const int32_t e = dtype == SPLAT_BF16 ? 2 : 4;
+  const View k{K, "K", B, T, d, e}, v{V, "V", B, T, d, e};
+  const View q{Q, "Q", B, T, d, e}, qr{Qr, "Qr", B, T, d, e};
+  CHECK(check_view(k, false));
+  CHECK(check_view(v, false));
+  if (K->heads != cache->heads || V->heads != cache->heads)
+    return fail(SPLAT_ERR_INVALID_ARG, "K and V must have the cache's %d heads", cache->heads);
+  const size_t bytes = (size_t)cache->n_pages * cache->heads * cache->page * d * e;
+  const Span own[] = {{cache->k, bytes, "the cache's k"}, {cache->v, bytes, "the cache's v"}};
+  if (meet(cache->k, bytes, cache->v, bytes))
+    return fail(SPLAT_ERR_INVALID_ARG, "the cache's k and v must not overlap");
+  if (Q) {
+    CHECK(check_view(q, false));
+    CHECK(check_view(qr, true));
+    if (Q->heads != Qr->heads) return fail(SPLAT_ERR_INVALID_ARG, "Q and Qr differ in heads");
+    if (!qr.same(q)) CHECK(check_apart(qr, q));
+    CHECK(check_apart(qr, k));
+    CHECK(check_apart(qr, v));
+  }
+  const Span ints[] = {{cache->table, (size_t)B * cache->max_pages * 4, "the cache's table"},
+                       {start, (size_t)B * 4, "start"},
+                       {counts, (size_t)B * 4, "counts"}};
+  for (const Span& c : own) {
+    for (const View* x : {&k, &v, &q, &qr})
+      if (x->x && meet(c.p, c.bytes, x->at(), x->extent()))
+        return fail(SPLAT_ERR_INVALID_ARG, "%s must not overlap %s", c.name, x->name);
+    for (const Span& i : ints)
+      if (meet(c.p, c.bytes, i.p, i.bytes))
+        return fail(SPLAT_ERR_INVALID_ARG, "%s must not overlap %s", c.name, i.name);
+  }
+  for (const Span& i : ints)
+    if (Q && meet(qr.at(), qr.extent(), i.p, i.bytes))
+      return fail(SPLAT_ERR_INVALID_ARG, "Qr must not overlap %s", i.name);
+  splat::HeadsArgs a{};
+  a.B = B, a.T = T;
+  a.job[a.n_jobs++] = heads_job(k, nullptr, r != nullptr);
+  a.job[a.n_jobs++] = heads_job(v, nullptr, false);
+  for (int i = 0; i < 2; ++i) a.job[i].y = (char*)own[i].p, a.job[i].paged = true;
+  if (Q) a.job[a.n_jobs++] = heads_job(q, &qr, r != nullptr);
+  if (r) use_rotary(a, r);
+  a.first = start, a.counts = counts, a.pages = cache->table;
+  a.max_pages = cache->max_pages, a.n_pages = cache->n_pages, a.page_shift = log2_of(cache->page);
+  return launched(splat::launch_heads(a, dtype, d, (hipStream_t)stream), "cache_append");
+}
+
+splat_status splat_decode_workspace(splat_acsr_t h, int32_t B, int32_t H, int32_t heads, int32_t d,
+                                    int64_t* bytes) {
+  if (!h || !bytes) return fail(SPLAT_ERR_INVALID_ARG, "handle and bytes must be non-NULL");
+  CHECK(check_batch(B, H));
+  CHECK(check_d(d));
+  if (heads < 1 || H % heads != 0)
+    return fail(SPLAT_ERR_INVALID_ARG, "H must be a multiple of the cache's heads (got %d, %d)", H, heads);
+  *bytes = splat::decode_workspace(h->dev, B, H, heads, d) * 4;
+  return ok();
+}
+
+splat_status splat_sparse_mhsa_decode(splat_acsr_t h, splat_dtype dtype, int32_t B, int32_t H,
+                                      int32_t d, const void* Q, const splat_cache* cache,
+                                      const int32_t* lengths, float scale, void* O, void* workspace,
+                                      void* stream) {
+  CHECK(check_handle(h, B, H));
+  CHECK(check_dtype(dtype, "dtype"));
+  CHECK(check_d(d));
+  CHECK(check_cache(cache, B));
+  int64_t need = 0;
+  CHECK(splat_decode_workspace(h, B, H, cache->heads, d, &need));
+  if (!lengths) return fail(SPLAT_ERR_INVALID_ARG, "lengths is NULL");
+  const size_t e = dtype == SPLAT_BF16 ? 2 : 4, dense = (size_t)B * H * d * e;
+  const size_t bytes = (size_t)cache->n_pages * cache->heads * cache->page * d * e;
+  CHECK(check_ptr(Q, "Q"));
+  CHECK(check_ptr(O, "O"));
+  if (need > 0) CHECK(check_ptr(workspace, "workspace"));
+  const Span in[] = {{Q, dense, "Q"},
+                     {cache->k, bytes, "the cache's k"},
+                     {cache->v, bytes, "the cache's v"},
+                     {cache->table, (size_t)B * cache->max_pages * 4, "the cache's table"},
+                     {lengths, (size_t)B * 4, "lengths"}};
+  const Span out[] = {{O, dense, "O"}, {need > 0 ? workspace : nullptr, (size_t)need, "workspace"}};
+  for (const Span& o : out)
+    for (const Span& i : in)
+      if (meet(o.p, o.bytes, i.p, i.bytes))
+        return fail(SPLAT_ERR_INVALID_ARG, "%s must not overlap %s", o.name, i.name);
+  if (meet(out[0].p, out[0].bytes, out[1].p, out[1].bytes))
+    return fail(SPLAT_ERR_INVALID_ARG, "O must not overlap workspace");
+  const splat::DecodeArgs x{Q, cache->k, cache->v, O, cache->table, lengths, B, H, cache->heads,
+                            cache->max_pages, cache->n_pages, log2_of(cache->page), scale,
+                            (float*)workspace};
+  return launched(splat::launch_decode(h->dev, dtype, d, x, (hipStream_t)stream),
+                  "sparse_mhsa_decode");
+}
+
 splat_status splat_sparse_mhsa_unfused(splat_acsr_t h, splat_dtype dtype, int32_t B, int32_t H,
                                        int32_t d, const void* Q, const void* K, const void* V,
                                        float scale, float* S, float* Pt, void* O,
@@ -797,6 +1124,7 @@ splat_status splat_debug_bounds(uint32_t* flags, int32_t clear) {
   if (e == hipSuccess) e = splat::bounds_collect_tiles(&bits, clear != 0);
   if (e == hipSuccess) e = splat::bounds_collect_slices(&bits, clear != 0);
   if (e == hipSuccess) e = splat::bounds_collect_grad(&bits, clear != 0);
+  if (e == hipSuccess) e = splat::bounds_collect_serve(&bits, clear != 0);
   if (e != hipSuccess) return fail(SPLAT_ERR_HIP, "splat_debug_bounds: %s", hipGetErrorString(e));
   *flags = bits;
   return SPLAT_OK;

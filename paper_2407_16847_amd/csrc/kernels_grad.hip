@@ -30,49 +30,6 @@ constexpr int kMaxGridY = 32768;         // slices per launch dimension; more ar
 constexpr float kLog2e = 1.4426950408889634f;
 
 // ----------------------------------------------------------------- operands
-// Products of 32 staged rows (fetch_k) with this lane's row: the scores' layout
-// of slice_ops, lane i's row against staged rows 8 (r/4) + 4 h + r % 4.
-template <typename T, int D>
-__device__ __forceinline__ f32x16_t dot_staged(const char* stage, const Slice& s,
-                                               const typename Mat<T, D>::Row& x) {
-  constexpr int RB = D * (int)sizeof(T);
-  typedef typename std::remove_reference<decltype(x.v[0])>::type vec_t;
-  const int off = s.qi * RB + 16 * (s.h ^ swz_row<RB / 16>(s.qi));
-  f32x16_t acc;
-#pragma unroll
-  for (int r = 0; r < 16; ++r) acc[r] = 0.f;
-#pragma unroll
-  for (int t = 0; t < RB / 32; ++t) {
-    const vec_t a = *(const vec_t*)(stage + (off ^ (32 * t)));
-    if constexpr (std::is_same<T, float>::value) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        acc = __builtin_amdgcn_mfma_f32_32x32x2f32(a[e], x.v[t][e], acc, 0, 0, 0);
-    } else {
-      acc = mfma32(a, x.v[t], acc);
-    }
-  }
-  return acc;
-}
-
-// The staged rows as the transposed operand: features NB i .. NB i + NB - 1 of
-// rows 16 j + 8 (r/4) + 4 h + r % 4, r < 8.  The swizzle of those rows is the
-// lane's (by h) XOR a constant of r.
-template <typename T, int D>
-__device__ __forceinline__ void load_staged(typename Mat<T, D>::V& x, const char* stage,
-                                            const Slice& s, int j) {
-  using vrow_t = typename Mat<T, D>::vrow_t;
-  constexpr int RB = D * (int)sizeof(T), CPR = RB / 16;
-  const int at = (int)sizeof(vrow_t) * s.qi;
-  const int chunk = (at >> 4) ^ (CPR == 8 ? 2 * s.h : 4 * s.h);
-  const int base = 4 * s.h * RB + 16 * chunk + (at & 15);
-#pragma unroll
-  for (int r = 0; r < 8; ++r) {
-    const int k = 16 * j + 8 * (r >> 2) + (r & 3);
-    x.v[r] = *(const vrow_t*)(stage + ((base ^ (16 * swz_row<CPR>(k))) + k * RB));
-  }
-}
-
 // o[b][.] += sum over the staged rows of feature NB i + b times weight w.  bf16:
 // the weights are rounded to nearest even, half a step (2^-8 of each at most)
 // as the rounding of the outputs.

@@ -103,6 +103,43 @@ struct BwdArgs {
 hipError_t launch_bwd(const DevAcsr& a, int dtype, int BH, int d, const BwdArgs& x, float scale,
                       hipStream_t st);
 
+// ---- serving: the position rotation, the paged cache, single query tokens
+// Heads of one tensor, strides in bytes.  paged: y is the cache's k or v.
+struct HeadsJob {
+  const char* x;
+  char* y;
+  int64_t xb, xh, xt, yb, yh, yt;
+  int32_t heads;
+  bool rotate, paged;
+};
+struct HeadsArgs {
+  HeadsJob job[3];
+  int32_t n_jobs, B, T;
+  const float2* angles;       // [max_len, rot / 2] (cosine, sine)
+  int32_t max_len, rot;       // rot 0: nothing turns
+  bool interleaved, inverse;
+  const int32_t* positions;   // [B, T], or null: first[b] + t (first null: t)
+  const int32_t* first;
+  const int32_t* counts;      // tokens of each sequence that count, or null: all
+  const int32_t* pages;       // [B, max_pages]
+  int32_t max_pages, n_pages, page_shift;
+};
+hipError_t launch_heads(const HeadsArgs& x, int dtype, int d, hipStream_t st);
+
+struct DecodeArgs {
+  const void *Q, *K, *V;
+  void* O;
+  const int32_t *pages, *lengths;
+  int32_t B, H, heads, max_pages, n_pages, page_shift;
+  float scale;
+  float* ws;
+};
+// splits of a sequence's keys, and the floats of workspace that their joining takes
+int decode_splits(const DevAcsr& a, int B, int H, int heads);
+int64_t decode_workspace(const DevAcsr& a, int B, int H, int heads, int d);
+hipError_t launch_decode(const DevAcsr& a, int dtype, int d, const DecodeArgs& x, hipStream_t st);
+hipError_t prepare_decode();
+
 // Allows the fused kernels their dynamic LDS (above the default limit at
 // d = 128) on the current device.  Called once per handle at build time, on
 // the handle's device, so launches never change kernel attributes.
@@ -116,6 +153,7 @@ hipError_t bounds_collect_mfma(uint32_t* bits, bool clear);
 hipError_t bounds_collect_tiles(uint32_t* bits, bool clear);
 hipError_t bounds_collect_slices(uint32_t* bits, bool clear);
 hipError_t bounds_collect_grad(uint32_t* bits, bool clear);
+hipError_t bounds_collect_serve(uint32_t* bits, bool clear);
 // One check of `index` against [0, n) as kind `kind`, run on the device
 // (allocates and frees one int); *result = the checked index.
 hipError_t bounds_probe(int kind, int index, int n, int* result);
