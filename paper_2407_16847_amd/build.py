@@ -27,7 +27,8 @@ BUILD_DIR_CHECKED = os.path.join(HERE, "_build_checked")
 ARCH = "gfx950"
 
 SOURCES = ["acsr_host.cpp", "tiling.cpp", "rotary_host.cpp", "api.hip", "kernels_mfma.hip", "kernels_tiles.hip",
-           "kernels_slices.hip", "kernels_grad.hip", "kernels_serve.hip"]
+           "kernels_slices.hip", "kernels_grad.hip", "kernels_grad_tiles.hip",
+           "kernels_serve.hip"]
 
 COMMON = ["-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function", "-Wno-unknown-pragmas"]
 # Packed fp32 instructions stay off: plain float code must not be turned into

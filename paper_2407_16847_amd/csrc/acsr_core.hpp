@@ -68,8 +68,9 @@ struct Group {
 struct Tile {
   int32_t kb, ks, nk, flags;
   int32_t mask_block;   // -1, or index of the tile's kBM per-row masks in the mask array
-  int32_t pad[3];
+  int32_t pad[3];       // pad[0] = 1: no row of the group has more than kFewKeys keys
 };
+constexpr int kFewKeys = 32;
 
 SPLAT_HD int32_t floor_div(int32_t a, int32_t b) {  // b > 0
   int32_t q = a / b;

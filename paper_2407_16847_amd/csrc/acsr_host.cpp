@@ -345,6 +345,11 @@ void plan_work(HostAcsr& a) {
       for (int32_t m = 0; m < nrows; ++m) a.rows.push_back(rows[off + m]);
       // union of the group's columns; strides present in the group
       U.clear();
+      int32_t few = 1;
+      for (int32_t m = 0; m < nrows; ++m) {
+        const int32_t i = rows[off + m];
+        if (a.row_ptr[i + 1] - a.row_ptr[i] > kFewKeys) few = 0;
+      }
       std::vector<int32_t> strides;
       for (int32_t m = 0; m < nrows; ++m) {
         const RowRuns& rr = a.runs[rows[off + m]];
@@ -377,6 +382,7 @@ void plan_work(HostAcsr& a) {
           pos = cut_tile(U, c, gather_ok, t) + 1;
         }
         t.mask_block = -1;
+        t.pad[0] = few;
         // per-row membership, per-wavefront state
         uint64_t rb[kBM];
         const uint64_t all = t.nk == 64 ? ~0ull : ((1ull << t.nk) - 1);

@@ -24,6 +24,7 @@ struct splat_acsr {
   int device = -1;
   void* dmem = nullptr;
   DevAcsr dev{};
+  std::vector<splat::TileRun> lengths, grad_lengths;
 };
 
 struct splat_rotary {
@@ -76,9 +77,18 @@ void plan_sizes(splat_acsr* h) {
     }
   h->dev.grad_groups = (int32_t)a.grad.groups.size();
   h->dev.grad_tiles = (int32_t)a.grad.tiles.size();
-  h->dev.grad_max_tiles = 0;
-  for (const splat::Group& g : a.grad.groups)
-    h->dev.grad_max_tiles = std::max(h->dev.grad_max_tiles, g.tile_end - g.tile_begin);
+  auto runs = [](const std::vector<splat::Group>& groups, std::vector<splat::TileRun>& out) {
+    for (const splat::Group& g : groups) {
+      const int32_t n = g.tile_end - g.tile_begin;
+      if (out.empty() || out.back().tiles != n) out.push_back({n, 0});
+      ++out.back().groups;
+    }
+  };
+  runs(a.groups, h->lengths);
+  runs(a.grad.groups, h->grad_lengths);
+  h->dev.lengths = h->lengths.data(), h->dev.n_lengths = (int32_t)h->lengths.size();
+  h->dev.grad_lengths = h->grad_lengths.data();
+  h->dev.n_grad_lengths = (int32_t)h->grad_lengths.size();
 }
 
 // One allocation holds every metadata array, each 256-byte aligned.
@@ -166,7 +176,12 @@ splat_status finish_build(splat_acsr* h, splat_status s, const std::string& err,
     delete h;
     return fail(s, "%s", err.c_str());
   }
-  plan_sizes(h);
+  try {
+    plan_sizes(h);
+  } catch (const std::bad_alloc&) {
+    delete h;
+    return fail(SPLAT_ERR_OOM, "host allocation failed during the analysis");
+  }
   s = upload(h);
   if (s != SPLAT_OK) {
     delete h;
@@ -206,13 +221,16 @@ splat_status check_handle(splat_acsr_t h, int32_t B, int32_t H) {
 
 // The bf16 kernels run one 256-thread workgroup per (row group, batch*head)
 // in a one-dimensional grid, whose work-item count must stay below 2^32.
-splat_status check_tile_grid(splat_acsr_t h, int32_t B, int32_t H) {
-  const int64_t wgs = (int64_t)h->dev.n_groups * B * H;
+splat_status check_grid(int32_t groups, const char* what, int32_t B, int32_t H) {
+  const int64_t wgs = (int64_t)groups * B * H;
   if (wgs * 256 > (int64_t)UINT32_MAX)
     return fail(SPLAT_ERR_UNSUPPORTED,
-                "the plan's %d row groups x B*H = %lld workgroups exceed one launch (2^24)",
-                h->dev.n_groups, (long long)wgs);
+                "the plan's %d %s groups x B*H = %lld workgroups exceed one launch (2^24)", groups,
+                what, (long long)wgs);
   return SPLAT_OK;
+}
+splat_status check_tile_grid(splat_acsr_t h, int32_t B, int32_t H) {
+  return check_grid(h->dev.n_groups, "row", B, H);
 }
 
 // The column-major layout needs the column-wise analysis and single-run columns.
@@ -857,7 +875,10 @@ splat_status splat_sparse_mhsa_bwd(splat_acsr_t h, splat_dtype dtype, int32_t B,
   const Span out[] = {{dQ, dense, "dQ"}, {dK, dense, "dK"}, {dV, dense, "dV"},
                       {workspace, rows * 8, "workspace"}};
   CHECK(check_spans(in, 6, out, 4));
-  if (dtype == SPLAT_BF16) CHECK(check_tile_grid(h, B, H));
+  if (dtype == SPLAT_BF16) {   // a group may take four workgroups
+    CHECK(check_grid(4 * h->dev.n_groups, "quarter row", B, H));
+    CHECK(check_grid(4 * h->dev.grad_groups, "quarter key", B, H));
+  }
   const splat::BwdArgs x{Q, K, V, O, dO, lse, workspace, dQ, dK, dV};
   return launched(splat::launch_bwd(h->dev, dtype, B * H, d, x, scale, (hipStream_t)stream),
                   "sparse_mhsa_bwd");
@@ -1124,6 +1145,7 @@ splat_status splat_debug_bounds(uint32_t* flags, int32_t clear) {
   if (e == hipSuccess) e = splat::bounds_collect_tiles(&bits, clear != 0);
   if (e == hipSuccess) e = splat::bounds_collect_slices(&bits, clear != 0);
   if (e == hipSuccess) e = splat::bounds_collect_grad(&bits, clear != 0);
+  if (e == hipSuccess) e = splat::bounds_collect_grad_tiles(&bits, clear != 0);
   if (e == hipSuccess) e = splat::bounds_collect_serve(&bits, clear != 0);
   if (e != hipSuccess) return fail(SPLAT_ERR_HIP, "splat_debug_bounds: %s", hipGetErrorString(e));
   *flags = bits;

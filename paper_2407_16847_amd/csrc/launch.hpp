@@ -8,6 +8,11 @@
 
 namespace splat {
 
+// Consecutive groups of a plan that have as many tiles each.
+struct TileRun {
+  int32_t tiles, groups;
+};
+
 // Device view of an ACSR handle's metadata.
 struct DevAcsr {
   int32_t L;
@@ -31,7 +36,9 @@ struct DevAcsr {
   // the transposed mask's plan (groups of keys, tiles of query rows), or null
   int32_t grad_groups;
   int32_t grad_tiles;
-  int32_t grad_max_tiles;   // tiles of the key group that has the most
+  // the plans' groups by length, longest first (host memory)
+  const TileRun *lengths, *grad_lengths;
+  int32_t n_lengths, n_grad_lengths;
   const int32_t* grad_rows;
   const Group* grad_group;
   const Tile* grad_tile;
@@ -53,6 +60,7 @@ enum Route : int32_t { kRouteRows, kRouteSlices, kRouteTiles, kRouteChain, kRout
 Route rsddmm_route(const DevAcsr& a, int dtype, int BH, int d);
 Route rspmm_route(const DevAcsr& a, int dtype, int BH, int d);   // both layouts
 Route fused_f32_route(const DevAcsr& a, int BH, int d);
+int grad_long_groups(const DevAcsr& a, bool kv, int BH, int d);   // bf16 backward: see there
 int fused_mfma_sets(const DevAcsr& a, int BH, int d);   // sets of wavefronts per tile group
 // values: the caller reads P afterwards
 Route unfused_route(const DevAcsr& a, int dtype, int BH, int d, bool colmajor, bool values);
@@ -100,6 +108,11 @@ struct BwdArgs {
   float* ws;
   void *dQ, *dK, *dV;
 };
+hipError_t launch_grad_q_tiles(const DevAcsr& a, int BH, int d, const BwdArgs& x, float scale,
+                               hipStream_t st);
+hipError_t launch_grad_kv_tiles(const DevAcsr& a, int BH, int d, const BwdArgs& x, float scale,
+                                hipStream_t st);
+hipError_t prepare_bwd_tiles();
 hipError_t launch_bwd(const DevAcsr& a, int dtype, int BH, int d, const BwdArgs& x, float scale,
                       hipStream_t st);
 
@@ -153,6 +166,7 @@ hipError_t bounds_collect_mfma(uint32_t* bits, bool clear);
 hipError_t bounds_collect_tiles(uint32_t* bits, bool clear);
 hipError_t bounds_collect_slices(uint32_t* bits, bool clear);
 hipError_t bounds_collect_grad(uint32_t* bits, bool clear);
+hipError_t bounds_collect_grad_tiles(uint32_t* bits, bool clear);
 hipError_t bounds_collect_serve(uint32_t* bits, bool clear);
 // One check of `index` against [0, n) as kind `kind`, run on the device
 // (allocates and frees one int); *result = the checked index.

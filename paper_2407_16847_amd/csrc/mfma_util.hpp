@@ -121,6 +121,11 @@ __device__ __forceinline__ void dma16(const void* g, char* lds) {
   __builtin_amdgcn_global_load_lds(g, (__attribute__((address_space(3))) void*)lds, kDmaBytes, 0, 0);
 }
 
+// ... 4 bytes a lane
+__device__ __forceinline__ void dma4(const void* g, char* lds) {
+  __builtin_amdgcn_global_load_lds(g, (__attribute__((address_space(3))) void*)lds, 4, 0, 0);
+}
+
 // Wait until at most `pending` vector-memory ops (the global->LDS loads) of
 // this wavefront are outstanding, then barrier.  The LDS/scalar counter is
 // left alone: every LDS read before a ring barrier has its result consumed

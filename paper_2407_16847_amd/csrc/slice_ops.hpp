@@ -205,6 +205,7 @@ struct Slice {
     masks = (const uint32_t*)m + 2 * i;
     return true;
   }
+  __device__ __forceinline__ bool valid() const { return row_valid; }
   // the row's membership bits in a unit
   __device__ __forceinline__ uint32_t bits(const Unit& u) const {
     return u.full ? ~0u : masks[(size_t)u.mask_block * (2 * kBM) + u.half];

@@ -7,7 +7,10 @@ that one accumulator of these sizes adds, so every fp32 quantity below is held t
 C = 32 u times the sum of its terms' magnitudes A(.), two stages deep: a score's
 error scales its p, so A(p_ij) = p_ij (2 + A(s_ij) + |lse_i|).  With bf16 inputs
 p and dS are rounded once for the products that sum them and every output once,
-b of its magnitude each.
+b of its magnitude each.  delta_i = sum_j p_ij dP_ij comes from the O of the
+forward, whose error reaches every dS_ij as p_ij |sum_c dO_ic (O - exact O)_ic|:
+that term is part of the bound, but for bf16 masks of at most 32 keys a row, where
+the call takes it out.
 """
 import math
 
@@ -68,7 +71,7 @@ def forward64(Q, K, V, M, scale):
 
 
 def backward64(Q, K, V, O, lse, dO, M, scale):
-    """((dQ, dK, dV), their bounds) of the call's formulas on the O and lse given."""
+    """((dQ, dK, dV), their bounds) of the gradients with the lse given."""
     q, k, v, o, g = (x.double() for x in (Q, K, V, O, dO))
     half, Mt = HALF[Q.dtype], torch.from_numpy(M)
     s = (q @ k.transpose(-1, -2)) * scale
@@ -76,10 +79,14 @@ def backward64(Q, K, V, O, lse, dO, M, scale):
     p = torch.exp(s - l).masked_fill(~Mt, 0.0)
     ap = p * (2 + (q.abs() @ k.abs().transpose(-1, -2)) * abs(scale) + l.abs())
     dp, adp = g @ v.transpose(-1, -2), g.abs() @ v.abs().transpose(-1, -2)
-    delta, adelta = (g * o).sum(-1, keepdim=True), (g * o).abs().sum(-1, keepdim=True)
+    delta, adelta = (p * dp).sum(-1, keepdim=True), (g * o).abs().sum(-1, keepdim=True)
+    off = (g * (o - p @ v)).sum(-1, keepdim=True).abs()
+    if Q.dtype == torch.bfloat16 and M.sum(-1).max() <= 32:
+        off = torch.zeros_like(off)
     one = Mt.sum(-1, keepdim=True) == 1
     ds = (p * (dp - delta)).masked_fill(one, 0.0)
-    ads = (ap * (adp + adelta)).masked_fill(one, 0.0)     # its error is C of this
+    # its error is C of this
+    ads = (ap * (adp + adelta) + p * off / C).masked_fill(one, 0.0)
     T = lambda x: x.transpose(-1, -2)
     out = (scale * (ds @ k), scale * (T(ds) @ q), T(p) @ g)
     mag = (abs(scale) * (ads @ k.abs()), abs(scale) * (T(ads) @ q.abs()), T(ap) @ g.abs())
