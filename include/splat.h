@@ -508,13 +508,12 @@ splat_status splat_rotary_export(splat_rotary_t r, float* table);
  * others >= 0 and multiples of 16 bytes.  data: 16-byte aligned device memory. */
 typedef struct {
   void* data;
-  int64_t stride_b, stride_h, stride_t;
-  int32_t heads;
+  int64_t stride_b, stride_h, stride_t, heads;
 } splat_heads;
 
 /*
- * splat_rotary_apply -- y = the rotation of x, for one tensor or two (a layer's Q
- * and K; x2 and y2 NULL for one) of `dtype`.  positions: int32 [B, T] on the
+ * splat_rotary_apply -- y = the rotation of x, for n = 1 or 2 tensors (a layer's Q
+ * and K) of `dtype`: xy[2 * n] is x, y for each in turn.  positions: int32 [B, T] on the
  * device, NULL for 0 .. T-1.  inverse: the transposed rotation, which is the
  * gradient (and, at magnitude 1, the inverse).  A token whose position lies
  * outside [0, max_len) gets NaN in its rotated features.  fp32 arithmetic, one
@@ -522,9 +521,8 @@ typedef struct {
  * with either input or the other output (INVALID_ARG).
  */
 splat_status splat_rotary_apply(splat_rotary_t r, splat_dtype dtype, int32_t B, int32_t T, int32_t d,
-                                const int32_t* positions, const splat_heads* x1, const splat_heads* y1,
-                                const splat_heads* x2, const splat_heads* y2, int32_t inverse,
-                                void* stream);
+                                const int32_t* positions, const splat_heads* xy, int32_t n,
+                                int32_t inverse, void* stream);
 
 /*
  * The paged cache: keys and values in pages of `page` tokens, k and v
@@ -536,7 +534,7 @@ splat_status splat_rotary_apply(splat_rotary_t r, splat_dtype dtype, int32_t B, 
 typedef struct {
   void *k, *v;
   const int32_t* table; /* [B, max_pages] */
-  int32_t n_pages, heads, page, max_pages;
+  int64_t n_pages, heads, page, max_pages;
 } splat_cache;
 
 /*
@@ -546,15 +544,15 @@ typedef struct {
  * tokens of sequence b are new, the rest padding: padding is not written, and
  * neither is a token whose position is negative or past the table, or whose page
  * lies outside [0, n_pages); everything else in the cache stays as it was.  Two
- * tokens of one call must not share a place.  Q, Qr (both NULL: none): the step's
- * queries [B, heads, T, d] and their rotation at the same positions, 0 in padding
- * rows; Qr may be Q itself, otherwise it shares no memory with another argument.
+ * tokens of one call must not share a place.  Qr = Q rotated to the same positions,
+ * 0 in padding rows; it may be Q itself, otherwise it shares no memory with another
+ * argument.
  * Positions past r's max_len give NaN, as in splat_rotary_apply.
  */
 splat_status splat_cache_append(splat_rotary_t r, splat_dtype dtype, int32_t B, int32_t T, int32_t d,
                                 const splat_cache* cache, const int32_t* start,
-                                const int32_t* counts, const splat_heads* K, const splat_heads* V,
-                                const splat_heads* Q, const splat_heads* Qr, void* stream);
+                                const int32_t* counts, const splat_heads* kvq, int32_t n,
+                                void* stream);
 
 /*
  * splat_sparse_mhsa_decode -- the attention of one query token a sequence over the

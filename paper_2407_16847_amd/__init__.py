@@ -80,16 +80,9 @@ class RotaryDesc(ctypes.Structure):
                 ("ramp_hi", ctypes.c_double), ("magnitude", ctypes.c_double)]
 
 
-class Heads(ctypes.Structure):
-    _fields_ = [("data", ctypes.c_void_p), ("stride_b", ctypes.c_int64), ("stride_h", ctypes.c_int64),
-                ("stride_t", ctypes.c_int64), ("heads", ctypes.c_int32)]
-
-
-class Cache(ctypes.Structure):
-    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("table", ctypes.c_void_p),
-                ("n_pages", ctypes.c_int32), ("heads", ctypes.c_int32), ("page", ctypes.c_int32),
-                ("max_pages", ctypes.c_int32)]
-
+# splat_heads and splat_cache are 64-bit words throughout: flat arrays of them
+# cost 1 us a call where structures cost 1 us each
+_WORDS = {n: ctypes.c_int64 * n for n in (7, 10, 20)}
 
 TILING_METHODS = {"poset": 0, "grid": 1, "naive": 2}
 
@@ -154,12 +147,10 @@ def _open(path: str) -> ctypes.CDLL:
                                   vp],
         "splat_rotary_build": [P(RotaryDesc), P(vp)],
         "splat_rotary_export": [vp, vp],
-        "splat_rotary_apply": [vp, i32, i32, i32, i32, vp, P(Heads), P(Heads), P(Heads), P(Heads), i32,
-                               vp],
-        "splat_cache_append": [vp, i32, i32, i32, i32, P(Cache), vp, vp, P(Heads), P(Heads), P(Heads),
-                               P(Heads), vp],
+        "splat_rotary_apply": [vp, i32, i32, i32, i32, vp, vp, i32, i32, vp],
+        "splat_cache_append": [vp, i32, i32, i32, i32, vp, vp, vp, vp, i32, vp],
         "splat_decode_workspace": [vp, i32, i32, i32, i32, P(i64)],
-        "splat_sparse_mhsa_decode": [vp, i32, i32, i32, i32, vp, P(Cache), vp, f32, vp, vp, vp],
+        "splat_sparse_mhsa_decode": [vp, i32, i32, i32, i32, vp, vp, vp, f32, vp, vp, vp],
         "splat_sparse_mhsa_unfused_noalloc": [vp, i32, i32, i32, i32, vp, vp, vp, f32, vp, i32, f32,
                                               P(i32), vp],
         "splat_acsr_export_csc": [vp, vp, vp],
@@ -556,17 +547,20 @@ def sparse_mhsa_fwd_lse(acsr: Acsr, Q: torch.Tensor, K: torch.Tensor, V: torch.T
     """The fused forward that keeps the rows' log-sum-exp for sparse_mhsa_bwd:
     (O in the inputs' dtype, lse fp32 [B, H, L])."""
     _dense(Q, "Q", acsr)
-    B, H, L, d = Q.shape
-    _like(K, "K", Q, acsr)
-    _like(V, "V", Q, acsr)
-    O = _result(O, "O", Q, acsr)
+    shape, dt, dev = Q.shape, Q.dtype, _here(Q, "Q")
+    B, H, L, d = shape
+    _alike(acsr, Q, shape, dt, dev, (K, V), ("K", "V"))
+    if O is None:
+        O = _fresh(Q, shape)
+    else:
+        _alike(acsr, Q, shape, dt, dev, (O,), ("O",))
     if lse is None:
         lse = torch.empty((B, H, L), dtype=torch.float32, device=Q.device)
     else:
-        _rows(lse, "lse", Q)
-    _check(load().splat_sparse_mhsa_fwd_lse(acsr.handle, _DT[Q.dtype], B, H, d, Q.data_ptr(),
+        _rows(lse, "lse", (B, H, L), dev)
+    _check(load().splat_sparse_mhsa_fwd_lse(acsr.handle, _DT[dt], B, H, d, Q.data_ptr(),
                                             K.data_ptr(), V.data_ptr(), float(scale), O.data_ptr(),
-                                            lse.data_ptr(), _stream()))
+                                            lse.data_ptr(), _stream_of(dev)))
     return O, lse
 
 
@@ -579,20 +573,75 @@ def sparse_mhsa_bwd(acsr: Acsr, Q: torch.Tensor, K: torch.Tensor, V: torch.Tenso
     handle built with grad=True.  workspace: fp32 [2, B, H, L], made by the call
     unless given."""
     _dense(Q, "Q", acsr)
-    B, H, L, d = Q.shape
-    for x, name in ((K, "K"), (V, "V"), (O, "O"), (dO, "dO")):
-        _like(x, name, Q, acsr)
-    _rows(lse, "lse", Q)
-    dQ, dK, dV = (_result(x, name, Q, acsr) for x, name in ((dQ, "dQ"), (dK, "dK"), (dV, "dV")))
+    shape, dt, dev = Q.shape, Q.dtype, _here(Q, "Q")
+    B, H, L, d = shape
+    _alike(acsr, Q, shape, dt, dev, (K, V, O, dO), ("K", "V", "O", "dO"))
+    _rows(lse, "lse", (B, H, L), dev)
+    if dQ is None:
+        dQ = _fresh(Q, shape)
+    else:
+        _alike(acsr, Q, shape, dt, dev, (dQ,), ("dQ",))
+    if dK is None:
+        dK = _fresh(Q, shape)
+    else:
+        _alike(acsr, Q, shape, dt, dev, (dK,), ("dK",))
+    if dV is None:
+        dV = _fresh(Q, shape)
+    else:
+        _alike(acsr, Q, shape, dt, dev, (dV,), ("dV",))
     if workspace is None:
         workspace = torch.empty((2, B, H, L), dtype=torch.float32, device=Q.device)
     else:
-        _rows(workspace, "workspace", Q, 2)
-    _check(load().splat_sparse_mhsa_bwd(acsr.handle, _DT[Q.dtype], B, H, d, Q.data_ptr(),
-                                        K.data_ptr(), V.data_ptr(), O.data_ptr(), lse.data_ptr(),
-                                        dO.data_ptr(), float(scale), dQ.data_ptr(), dK.data_ptr(),
-                                        dV.data_ptr(), workspace.data_ptr(), _stream()))
+        _rows(workspace, "workspace", (2, B, H, L), dev)
+    _check(load().splat_sparse_mhsa_bwd(acsr.handle, _DT[dt], B, H, d, Q.data_ptr(), K.data_ptr(),
+                                        V.data_ptr(), O.data_ptr(), lse.data_ptr(), dO.data_ptr(),
+                                        float(scale), dQ.data_ptr(), dK.data_ptr(), dV.data_ptr(),
+                                        workspace.data_ptr(), _stream_of(dev)))
     return dQ, dK, dV
+
+
+# The current device's number: without torch.cuda's own checks where this torch
+# has the call (an initialised device is at hand: a tensor lives on it).
+_device_now = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
+def _here(x: torch.Tensor, name: str) -> int:
+    """The number of x's device, which must be the current one."""
+    dev = x.get_device()
+    if dev != _device_now():
+        raise ValueError(f"{name} is on cuda:{dev}, the current device is cuda:{_device_now()}")
+    return dev
+
+
+def _stream_of(dev: int) -> int:
+    return _raw_stream(dev) if _raw_stream is not None else torch.cuda.current_stream().cuda_stream
+
+
+def _alike(acsr: Acsr, Q: torch.Tensor, shape, dt, dev: int, xs, names) -> None:
+    """Every x of xs matches Q, whose shape, dtype and device are given: a few
+    comparisons each (_like's checks find what is wrong)."""
+    for x, name in zip(xs, names):
+        if not (isinstance(x, torch.Tensor) and x.dtype is dt and x.get_device() == dev
+                and x.shape == shape and x.is_contiguous()):
+            _like(x, name, Q, acsr)
+            raise ValueError(f"{name} must match Q")
+
+
+def _fresh(ref: torch.Tensor, shape) -> torch.Tensor:
+    """An uninitialised plain contiguous tensor of `shape`, of ref's dtype and device."""
+    if type(ref) is torch.Tensor:
+        return ref.new_empty(shape)
+    return torch.empty(tuple(shape), dtype=ref.dtype, device=ref.device)
+
+
+def _rows(x: torch.Tensor, name: str, shape, dev: int) -> None:
+    """x is fp32 of `shape`."""
+    if not isinstance(x, torch.Tensor) or not x.is_cuda:
+        raise TypeError(f"{name} must be a CUDA (HIP) tensor")
+    if x.dtype is not torch.float32 or x.shape != shape or not x.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous float32 {list(shape)} tensor")
+    if x.get_device() != dev:
+        raise ValueError(f"{name} is on {x.device}, expected cuda:{dev}")
 
 
 class Rotary:
@@ -639,44 +688,55 @@ class Rotary:
         return t
 
 
-def _heads(x: torch.Tensor, name: str, ref: Optional[torch.Tensor] = None) -> Heads:
-    """x [B, heads, T, d] by its strides; dtype, device, B, T and d of ref."""
+def _heads(x: torch.Tensor, name: str, dt, dev: int, B: int, T: int, d: int):
+    """x [B, heads, T, d] as a splat_heads: (address, strides, heads)."""
+    if not isinstance(x, torch.Tensor) or not x.is_cuda:
+        raise TypeError(f"{name} must be a CUDA (HIP) tensor")
+    shape = x.shape
+    if x.dtype is not dt or len(shape) != 4 or shape[0] != B or shape[2] != T or shape[3] != d:
+        raise ValueError(f"{name} must be {dt} [{B}, heads, {T}, {d}], got {x.dtype} {list(shape)}")
+    sb, sh, st, sd = x.stride()
+    if sd != 1:
+        raise ValueError(f"{name}'s features must be contiguous")
+    if x.get_device() != dev:
+        raise ValueError(f"{name} is on {x.device}, expected cuda:{dev}")
+    return x.data_ptr(), sb, sh, st, shape[1]
+
+
+def _first(x: torch.Tensor, name: str):
+    """(dtype, device number, shape) of a call's first [B, heads, T, d] tensor."""
     if not isinstance(x, torch.Tensor) or not x.is_cuda:
         raise TypeError(f"{name} must be a CUDA (HIP) tensor")
     if x.dtype not in _DT:
         raise TypeError(f"{name} must be float32 or bfloat16, got {x.dtype}")
-    if x.dim() != 4 or 0 in x.shape:
-        raise ValueError(f"{name} must be [B, heads, T, d] with no empty axis, got {tuple(x.shape)}")
-    if x.stride(3) != 1:
-        raise ValueError(f"{name}'s features must be contiguous")
-    if ref is not None and ref is not x:
-        if x.dtype != ref.dtype or (x.shape[0], *x.shape[2:]) != (ref.shape[0], *ref.shape[2:]):
-            raise ValueError(f"{name} must match {tuple(ref.shape)} {ref.dtype} in dtype, B, T and d, "
-                             f"got {tuple(x.shape)} {x.dtype}")
-        _on(x, name, ref)
-    sb, sh, st, _ = x.stride()
-    return Heads(x.data_ptr(), sb, sh, st, x.shape[1])
+    shape = x.shape
+    if len(shape) != 4 or 0 in shape:
+        raise ValueError(f"{name} must be [B, heads, T, d] with no empty axis, got {tuple(shape)}")
+    return x.dtype, _here(x, name), shape
 
 
-def _ints(x: torch.Tensor, name: str, shape, ref: torch.Tensor) -> int:
-    """The address of x, contiguous int32 of `shape` on ref's device."""
-    if not isinstance(x, torch.Tensor) or not x.is_cuda:
-        raise TypeError(f"{name} must be a CUDA (HIP) tensor")
-    if x.dtype != torch.int32 or tuple(x.shape) != tuple(shape) or not x.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous int32 {list(shape)} tensor, "
-                         f"got {x.dtype} {list(x.shape)}")
-    _on(x, name, ref)
-    return x.data_ptr()
-
-
-def _turned(x: torch.Tensor, y: Optional[torch.Tensor], name: str) -> Tuple[torch.Tensor, Heads]:
-    """The output for x: y, or a new contiguous tensor."""
+def _turned(x: torch.Tensor, y: Optional[torch.Tensor], name: str, dt, dev: int):
+    """The output for x and its splat_heads: y, or a new contiguous tensor."""
+    B, H, T, d = x.shape
     if y is None:
-        y = torch.empty(tuple(x.shape), dtype=x.dtype, device=x.device)
-    h = _heads(y, name, x)
-    if y.shape != x.shape:
+        y = _fresh(x, (B, H, T, d))
+        return y, (y.data_ptr(), H * T * d, T * d, d, H)
+    h = _heads(y, name, dt, dev, B, T, d)
+    if h[4] != H:
         raise ValueError(f"{name} must be {tuple(x.shape)}, got {tuple(y.shape)}")
     return y, h
+
+
+def _ints(x: torch.Tensor, name: str, shape, dev: int) -> int:
+    """The address of x, contiguous int32 of `shape`."""
+    if not isinstance(x, torch.Tensor) or not x.is_cuda:
+        raise TypeError(f"{name} must be a CUDA (HIP) tensor")
+    if x.dtype is not torch.int32 or x.shape != shape or not x.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous int32 {list(shape)} tensor, "
+                         f"got {x.dtype} {list(x.shape)}")
+    if x.get_device() != dev:
+        raise ValueError(f"{name} is on {x.device}, expected cuda:{dev}")
+    return x.data_ptr()
 
 
 def rotary(rot: Rotary, X: torch.Tensor, X2: Optional[torch.Tensor] = None, *,
@@ -686,38 +746,46 @@ def rotary(rot: Rotary, X: torch.Tensor, X2: Optional[torch.Tensor] = None, *,
     positions -- int32 [B, T], or 0 .. T-1 -- as a contiguous tensor, or into Y,
     which may be X.  With X2 (its own number of heads; a layer's Q and K in one
     launch) returns both.  inverse=True: the transposed rotation, its gradient."""
-    x, (Y, y) = _heads(X, "X"), _turned(X, Y, "Y")
-    pair = X2 is not None
-    x2, y2 = None, None
-    if pair:
-        x2 = _heads(X2, "X2", X)
-        Y2, y2 = _turned(X2, Y2, "Y2")
-    elif Y2 is not None:
-        raise ValueError("Y2 needs X2")
-    B, _, T, d = X.shape
-    pos = None if positions is None else _ints(positions, "positions", (B, T), X)
-    _check(load().splat_rotary_apply(rot.handle, _DT[X.dtype], B, T, d, pos, ctypes.byref(x),
-                                     ctypes.byref(y), ctypes.byref(x2) if pair else None,
-                                     ctypes.byref(y2) if pair else None, int(bool(inverse)), _stream()))
-    return (Y, Y2) if pair else Y
+    dt, dev, (B, _, T, d) = _first(X, "X")
+    x = _heads(X, "X", dt, dev, B, T, d)
+    Y, y = _turned(X, Y, "Y", dt, dev)
+    if X2 is None:
+        if Y2 is not None:
+            raise ValueError("Y2 needs X2")
+        xy, n = _WORDS[10](*x, *y), 1
+    else:
+        x2 = _heads(X2, "X2", dt, dev, B, T, d)
+        if x2[4] == 0:
+            raise ValueError("X2 has no heads")
+        Y2, y2 = _turned(X2, Y2, "Y2", dt, dev)
+        xy, n = _WORDS[20](*x, *y, *x2, *y2), 2
+    pos = None if positions is None else _ints(positions, "positions", (B, T), dev)
+    _check(load().splat_rotary_apply(rot.handle, _DT[dt], B, T, d, pos, xy, n, 1 if inverse else 0,
+                                     _stream_of(dev)))
+    return Y if X2 is None else (Y, Y2)
 
 
-def _cache(k_cache: torch.Tensor, v_cache: torch.Tensor, table: torch.Tensor, ref: torch.Tensor) -> Cache:
-    """The paged cache, checked against ref [B, heads, T, d]."""
+def _cache(k_cache: torch.Tensor, v_cache: torch.Tensor, table: torch.Tensor, dt, dev: int, B: int,
+           d: int):
+    """The paged cache as a splat_cache, and its heads."""
     for x, name in ((k_cache, "k_cache"), (v_cache, "v_cache")):
         if not isinstance(x, torch.Tensor) or not x.is_cuda:
             raise TypeError(f"{name} must be a CUDA (HIP) tensor")
-        if x.dim() != 4 or x.dtype != ref.dtype or x.shape[3] != ref.shape[3] or not x.is_contiguous():
-            raise ValueError(f"{name} must be a contiguous {ref.dtype} [pages, heads, page, "
-                             f"{ref.shape[3]}] tensor, got {x.dtype} {list(x.shape)}")
-        _on(x, name, ref)
-    if v_cache.shape != k_cache.shape:
-        raise ValueError("k_cache and v_cache must have one shape")
+        if x.dtype is not dt or x.dim() != 4 or not x.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous {dt} [pages, heads, page, {d}] tensor, "
+                             f"got {x.dtype} {list(x.shape)}")
+        if x.get_device() != dev:
+            raise ValueError(f"{name} is on {x.device}, expected cuda:{dev}")
+    shape = k_cache.shape
+    if shape[3] != d or v_cache.shape != shape:
+        raise ValueError(f"k_cache and v_cache must both be [pages, heads, page, {d}], "
+                         f"got {list(shape)} and {list(v_cache.shape)}")
     if not isinstance(table, torch.Tensor) or table.dim() != 2:
         raise ValueError("table must be [B, max_pages]")
-    at = _ints(table, "table", (ref.shape[0], table.shape[1]), ref)
-    n, heads, page, _ = k_cache.shape
-    return Cache(k_cache.data_ptr(), v_cache.data_ptr(), at, n, heads, page, table.shape[1])
+    most = table.shape[1]
+    at = _ints(table, "table", (B, most), dev)
+    return (_WORDS[7](k_cache.data_ptr(), v_cache.data_ptr(), at, shape[0], shape[1], shape[2], most),
+            shape[1])
 
 
 def cache_append(k_cache: torch.Tensor, v_cache: torch.Tensor, table: torch.Tensor,
@@ -730,22 +798,23 @@ def cache_append(k_cache: torch.Tensor, v_cache: torch.Tensor, table: torch.Tens
     position start[b], K rotated on the way; only the first counts[b] tokens, if
     given.  With Q [B, H, T, d] returns its rotation at the same positions (in Qr,
     if given; padding rows 0)."""
-    k = _heads(K, "K")
-    v = _heads(V, "V", K)
-    B, _, T, d = K.shape
-    c = _cache(k_cache, v_cache, table, K)
-    first = _ints(start, "start", (B,), K)
-    n = None if counts is None else _ints(counts, "counts", (B,), K)
-    q, qr = None, None
-    if Q is not None:
-        q = _heads(Q, "Q", K)
-        Qr, qr = _turned(Q, Qr, "Qr")
-    elif Qr is not None:
-        raise ValueError("Qr needs Q")
-    _check(load().splat_cache_append(rot.handle if rot is not None else None, _DT[K.dtype], B, T, d,
-                                     ctypes.byref(c), first, n, ctypes.byref(k), ctypes.byref(v),
-                                     ctypes.byref(q) if q is not None else None,
-                                     ctypes.byref(qr) if q is not None else None, _stream()))
+    dt, dev, (B, _, T, d) = _first(K, "K")
+    k, v = _heads(K, "K", dt, dev, B, T, d), _heads(V, "V", dt, dev, B, T, d)
+    c, _ = _cache(k_cache, v_cache, table, dt, dev, B, d)
+    first = _ints(start, "start", (B,), dev)
+    count = None if counts is None else _ints(counts, "counts", (B,), dev)
+    if Q is None:
+        if Qr is not None:
+            raise ValueError("Qr needs Q")
+        kvq, n = _WORDS[10](*k, *v), 2
+    else:
+        q = _heads(Q, "Q", dt, dev, B, T, d)
+        if q[4] == 0:
+            raise ValueError("Q has no heads")
+        Qr, qr = _turned(Q, Qr, "Qr", dt, dev)
+        kvq, n = _WORDS[20](*k, *v, *q, *qr), 4
+    _check(load().splat_cache_append(None if rot is None else rot.handle, _DT[dt], B, T, d, c, first,
+                                     count, kvq, n, _stream_of(dev)))
     return Qr
 
 
@@ -753,7 +822,7 @@ def decode_workspace(acsr: Acsr, B: int, H: int, heads: int, d: int) -> int:
     """Bytes of workspace that sparse_mhsa_decode takes (0: none)."""
     n = ctypes.c_int64()
     _check(acsr._lib.splat_decode_workspace(acsr.handle, B, H, heads, d, ctypes.byref(n)))
-    return int(n.value)
+    return n.value
 
 
 def sparse_mhsa_decode(acsr: Acsr, Q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor,
@@ -764,54 +833,32 @@ def sparse_mhsa_decode(acsr: Acsr, Q: torch.Tensor, k_cache: torch.Tensor, v_cac
     mask's row lengths[b] - 1, its columns below lengths[b] (int32 [B]).  The
     cache's heads divide H.  workspace: at least decode_workspace() bytes, made by
     the call unless given."""
-    if not isinstance(Q, torch.Tensor) or not Q.is_cuda:
-        raise TypeError("Q must be a CUDA (HIP) tensor")
-    if Q.dtype not in _DT:
-        raise TypeError(f"Q must be float32 or bfloat16, got {Q.dtype}")
-    if Q.dim() != 4 or Q.shape[2] != 1 or not Q.is_contiguous():
-        raise ValueError(f"Q must be a contiguous [B, H, 1, d] tensor, got {tuple(Q.shape)}")
-    B, H, _, d = Q.shape
-    c = _cache(k_cache, v_cache, table, Q)
-    at = _ints(lengths, "lengths", (B,), Q)
+    dt, dev, shape = _first(Q, "Q")
+    B, H, T, d = shape
+    if T != 1 or not Q.is_contiguous():
+        raise ValueError(f"Q must be a contiguous [B, H, 1, d] tensor, got {tuple(shape)}")
+    c, heads = _cache(k_cache, v_cache, table, dt, dev, B, d)
+    at = _ints(lengths, "lengths", (B,), dev)
     if O is None:
-        O = _new(Q, Q.dtype)
+        O = _fresh(Q, shape)
     else:
         if not isinstance(O, torch.Tensor) or not O.is_cuda:
             raise TypeError("O must be a CUDA (HIP) tensor")
-        if O.dtype != Q.dtype or O.shape != Q.shape or not O.is_contiguous():
-            raise ValueError(f"O must be a contiguous {Q.dtype} {list(Q.shape)} tensor")
-        _on(O, "O", Q)
-    need = decode_workspace(acsr, B, H, c.heads, d)
+        if O.dtype is not dt or O.shape != shape or not O.is_contiguous() or O.get_device() != dev:
+            raise ValueError(f"O must be a contiguous {dt} {list(shape)} tensor on cuda:{dev}")
+    need = decode_workspace(acsr, B, H, heads, d)
     if workspace is not None:
         if not isinstance(workspace, torch.Tensor) or not workspace.is_cuda:
             raise TypeError("workspace must be a CUDA (HIP) tensor")
-        if workspace.numel() * workspace.element_size() < need or not workspace.is_contiguous():
-            raise ValueError(f"workspace must be contiguous and hold {need} bytes")
-        _on(workspace, "workspace", Q)
+        if (workspace.numel() * workspace.element_size() < need or not workspace.is_contiguous()
+                or workspace.get_device() != dev):
+            raise ValueError(f"workspace must be contiguous on cuda:{dev} and hold {need} bytes")
     elif need:
         workspace = torch.empty(need // 4, dtype=torch.float32, device=Q.device)
-    _check(load().splat_sparse_mhsa_decode(acsr.handle, _DT[Q.dtype], B, H, d, Q.data_ptr(),
-                                           ctypes.byref(c), at, float(scale), O.data_ptr(),
-                                           workspace.data_ptr() if need else None, _stream()))
+    _check(load().splat_sparse_mhsa_decode(acsr.handle, _DT[dt], B, H, d, Q.data_ptr(), c, at,
+                                           float(scale), O.data_ptr(),
+                                           workspace.data_ptr() if need else None, _stream_of(dev)))
     return O
-
-
-def _result(x: Optional[torch.Tensor], name: str, Q: torch.Tensor, acsr: Acsr) -> torch.Tensor:
-    """x, of Q's shape and dtype, or a new tensor of them."""
-    if x is None:
-        return _new(Q, Q.dtype)
-    _like(x, name, Q, acsr)
-    return x
-
-
-def _rows(x: torch.Tensor, name: str, Q: torch.Tensor, *lead: int) -> None:
-    """x is fp32, a value (or `lead` of them) for every query row."""
-    if not isinstance(x, torch.Tensor) or not x.is_cuda:
-        raise TypeError(f"{name} must be a CUDA (HIP) tensor")
-    shape = (*lead, *Q.shape[:3])
-    if x.dtype != torch.float32 or x.shape != shape or not x.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous float32 {list(shape)} tensor")
-    _on(x, name, Q)
 
 
 def _values(x: torch.Tensor, name: str, acsr: Acsr, B: int, H: int) -> None:

@@ -365,10 +365,13 @@ struct View {
   }
 };
 
+// x as a 32-bit size, 0 (which no check lets pass) if it is none
+int32_t int32_of(int64_t x) { return x > 0 && x <= INT32_MAX ? (int32_t)x : 0; }
+
 splat_status check_view(const View& v, bool output) {
   const splat_heads& x = *v.x;
   CHECK(check_ptr(x.data, v.name));
-  CHECK(check_batch(v.B, x.heads));
+  CHECK(check_batch(v.B, int32_of(x.heads)));
   const int64_t unit = 16 / v.e, most = int64_t(1) << 40;
   struct Dim {
     int64_t n, stride;
@@ -415,7 +418,7 @@ splat::HeadsJob heads_job(const View& x, const View* y, bool rotate) {
   splat::HeadsJob j{};
   j.x = x.at();
   j.xb = x.x->stride_b * x.e, j.xh = x.x->stride_h * x.e, j.xt = x.x->stride_t * x.e;
-  j.heads = x.x->heads;
+  j.heads = (int32_t)x.x->heads;
   j.rotate = rotate;
   if (y) {
     j.y = (char*)y->x->data;
@@ -450,20 +453,21 @@ splat_status check_cache(const splat_cache* c, int32_t B) {
   CHECK(check_ptr(c->k, "the cache's k"));
   CHECK(check_ptr(c->v, "the cache's v"));
   if (!c->table) return fail(SPLAT_ERR_INVALID_ARG, "the cache's table is NULL");
-  CHECK(check_batch(B, c->heads));
-  if (c->n_pages < 1 || c->max_pages < 1)
-    return fail(SPLAT_ERR_INVALID_ARG, "n_pages and max_pages must be >= 1");
+  CHECK(check_batch(B, int32_of(c->heads)));
+  if (!int32_of(c->n_pages) || !int32_of(c->max_pages))
+    return fail(SPLAT_ERR_INVALID_ARG, "n_pages and max_pages must be in [1, 2^31)");
   if (c->page < 1 || c->page > 65536 || (c->page & (c->page - 1)) != 0)
-    return fail(SPLAT_ERR_INVALID_ARG, "page must be a power of two up to 65536, got %d", c->page);
+    return fail(SPLAT_ERR_INVALID_ARG, "page must be a power of two up to 65536, got %lld",
+                (long long)c->page);
   // rows of the cache are counted in 32 bits
-  if ((int64_t)c->n_pages * c->heads > (int64_t)UINT32_MAX / c->page)
+  if (c->n_pages * c->heads > (int64_t)UINT32_MAX / c->page)
     return fail(SPLAT_ERR_UNSUPPORTED, "the cache holds 2^32 rows or more");
   return SPLAT_OK;
 }
 
-int32_t log2_of(int32_t page) {
+int32_t log2_of(int64_t page) {
   int32_t s = 0;
-  while ((1 << s) < page) ++s;
+  while ((int64_t(1) << s) < page) ++s;
   return s;
 }
 
@@ -940,20 +944,17 @@ splat_status splat_rotary_export(splat_rotary_t r, float* table) {
 }
 
 splat_status splat_rotary_apply(splat_rotary_t r, splat_dtype dtype, int32_t B, int32_t T, int32_t d,
-                                const int32_t* positions, const splat_heads* x1, const splat_heads* y1,
-                                const splat_heads* x2, const splat_heads* y2, int32_t inverse,
-                                void* stream) {
+                                const int32_t* positions, const splat_heads* xy, int32_t n,
+                                int32_t inverse, void* stream) {
   CHECK(check_dtype(dtype, "dtype"));
   CHECK(check_d(d));
   CHECK(check_tokens(B, T));
   CHECK(check_rotary(r, d));
-  if (!x1 || !y1) return fail(SPLAT_ERR_INVALID_ARG, "x1 and y1 must be non-NULL");
-  if (!x2 != !y2) return fail(SPLAT_ERR_INVALID_ARG, "x2 and y2 go together");
+  if (!xy || n < 1 || n > 2) return fail(SPLAT_ERR_INVALID_ARG, "xy must hold 1 or 2 pairs");
   if (inverse != 0 && inverse != 1) return fail(SPLAT_ERR_INVALID_ARG, "inverse must be 0 or 1");
   const int32_t e = dtype == SPLAT_BF16 ? 2 : 4;
-  const View x[2] = {{x1, "x1", B, T, d, e}, {x2, "x2", B, T, d, e}};
-  const View y[2] = {{y1, "y1", B, T, d, e}, {y2, "y2", B, T, d, e}};
-  const int n = x2 ? 2 : 1;
+  const View x[2] = {{xy, "x", B, T, d, e}, {xy + 2, "the second x", B, T, d, e}};
+  const View y[2] = {{xy + 1, "y", B, T, d, e}, {xy + 3, "the second y", B, T, d, e}};
   for (int k = 0; k < n; ++k) {
     CHECK(check_view(x[k], false));
     CHECK(check_view(y[k], true));
@@ -979,23 +980,26 @@ splat_status splat_rotary_apply(splat_rotary_t r, splat_dtype dtype, int32_t B, 
 
 splat_status splat_cache_append(splat_rotary_t r, splat_dtype dtype, int32_t B, int32_t T, int32_t d,
                                 const splat_cache* cache, const int32_t* start,
-                                const int32_t* counts, const splat_heads* K, const splat_heads* V,
-                                const splat_heads* Q, const splat_heads* Qr, void* stream) {
+                                const int32_t* counts, const splat_heads* kvq, int32_t n,
+                                void* stream) {
   CHECK(check_dtype(dtype, "dtype"));
   CHECK(check_d(d));
   CHECK(check_tokens(B, T));
   if (r) CHECK(check_rotary(r, d));
   CHECK(check_cache(cache, B));
   if (!start) return fail(SPLAT_ERR_INVALID_ARG, "start is NULL");
-  if (!K || !V) return fail(SPLAT_ERR_INVALID_ARG, "K and V must be non-NULL");
-  if (!Q != !Qr) return fail(SPLAT_ERR_INVALID_ARG, "Q and Qr go together");
+  if (!kvq || (n != 2 && n != 4))
+    return fail(SPLAT_ERR_INVALID_ARG, "kvq must hold K and V, or K, V, Q and Qr");
+  const splat_heads *const K = kvq, *const V = kvq + 1;
+  const splat_heads *const Q = n == 4 ? kvq + 2 : nullptr, *const Qr = n == 4 ? kvq + 3 : nullptr;
   const int32_t e = dtype == SPLAT_BF16 ? 2 : 4;
   const View k{K, "K", B, T, d, e}, v{V, "V", B, T, d, e};
   const View q{Q, "Q", B, T, d, e}, qr{Qr, "Qr", B, T, d, e};
   CHECK(check_view(k, false));
   CHECK(check_view(v, false));
   if (K->heads != cache->heads || V->heads != cache->heads)
-    return fail(SPLAT_ERR_INVALID_ARG, "K and V must have the cache's %d heads", cache->heads);
+    return fail(SPLAT_ERR_INVALID_ARG, "K and V must have the cache's %lld heads",
+                (long long)cache->heads);
   const size_t bytes = (size_t)cache->n_pages * cache->heads * cache->page * d * e;
   const Span own[] = {{cache->k, bytes, "the cache's k"}, {cache->v, bytes, "the cache's v"}};
   if (meet(cache->k, bytes, cache->v, bytes))
@@ -1030,7 +1034,8 @@ splat_status splat_cache_append(splat_rotary_t r, splat_dtype dtype, int32_t B, 
   if (Q) a.job[a.n_jobs++] = heads_job(q, &qr, r != nullptr);
   if (r) use_rotary(a, r);
   a.first = start, a.counts = counts, a.pages = cache->table;
-  a.max_pages = cache->max_pages, a.n_pages = cache->n_pages, a.page_shift = log2_of(cache->page);
+  a.max_pages = (int32_t)cache->max_pages, a.n_pages = (int32_t)cache->n_pages;
+  a.page_shift = log2_of(cache->page);
   return launched(splat::launch_heads(a, dtype, d, (hipStream_t)stream), "cache_append");
 }
 
@@ -1054,7 +1059,8 @@ splat_status splat_sparse_mhsa_decode(splat_acsr_t h, splat_dtype dtype, int32_t
   CHECK(check_d(d));
   CHECK(check_cache(cache, B));
   int64_t need = 0;
-  CHECK(splat_decode_workspace(h, B, H, cache->heads, d, &need));
+  const int32_t heads = (int32_t)cache->heads;
+  CHECK(splat_decode_workspace(h, B, H, heads, d, &need));
   if (!lengths) return fail(SPLAT_ERR_INVALID_ARG, "lengths is NULL");
   const size_t e = dtype == SPLAT_BF16 ? 2 : 4, dense = (size_t)B * H * d * e;
   const size_t bytes = (size_t)cache->n_pages * cache->heads * cache->page * d * e;
@@ -1073,9 +1079,9 @@ splat_status splat_sparse_mhsa_decode(splat_acsr_t h, splat_dtype dtype, int32_t
         return fail(SPLAT_ERR_INVALID_ARG, "%s must not overlap %s", o.name, i.name);
   if (meet(out[0].p, out[0].bytes, out[1].p, out[1].bytes))
     return fail(SPLAT_ERR_INVALID_ARG, "O must not overlap workspace");
-  const splat::DecodeArgs x{Q, cache->k, cache->v, O, cache->table, lengths, B, H, cache->heads,
-                            cache->max_pages, cache->n_pages, log2_of(cache->page), scale,
-                            (float*)workspace};
+  const splat::DecodeArgs x{Q, cache->k, cache->v, O, cache->table, lengths, B, H, heads,
+                            (int32_t)cache->max_pages, (int32_t)cache->n_pages,
+                            log2_of(cache->page), scale, (float*)workspace};
   return launched(splat::launch_decode(h->dev, dtype, d, x, (hipStream_t)stream),
                   "sparse_mhsa_decode");
 }
