@@ -1,9 +1,10 @@
 """Sparse multi-head self-attention over ACSR masks on MI355X (gfx950).
 
 Thin Python binding of ``libsplat.so`` (C ABI in ``include/splat.h``): this
-module only marshals arguments -- PyTorch supplies device memory and the
-stream, every step of the computation runs in the library's HIP kernels.
-There is no fallback: if the library is not built, ``load()`` raises.
+module and its extension ``_native.so`` only marshal arguments -- PyTorch
+supplies device memory and the stream, every step of the computation runs in
+the library's HIP kernels.  There is no fallback: if the library is not built,
+``load()`` raises.
 
     import paper_2407_16847_amd as splat
     pat = splat.Pattern.window_global(4096, w=512, n_global=64)
@@ -79,10 +80,6 @@ class RotaryDesc(ctypes.Structure):
                 ("base", ctypes.c_double), ("factor", ctypes.c_double), ("ramp_lo", ctypes.c_double),
                 ("ramp_hi", ctypes.c_double), ("magnitude", ctypes.c_double)]
 
-
-# splat_heads and splat_cache are 64-bit words throughout: flat arrays of them
-# cost 1 us a call where structures cost 1 us each
-_WORDS = {n: ctypes.c_int64 * n for n in (7, 10, 20)}
 
 TILING_METHODS = {"poset": 0, "grid": 1, "naive": 2}
 
@@ -546,22 +543,7 @@ def sparse_mhsa_fwd_lse(acsr: Acsr, Q: torch.Tensor, K: torch.Tensor, V: torch.T
                         ) -> Tuple[torch.Tensor, torch.Tensor]:
     """The fused forward that keeps the rows' log-sum-exp for sparse_mhsa_bwd:
     (O in the inputs' dtype, lse fp32 [B, H, L])."""
-    _dense(Q, "Q", acsr)
-    shape, dt, dev = Q.shape, Q.dtype, _here(Q, "Q")
-    B, H, L, d = shape
-    _alike(acsr, Q, shape, dt, dev, (K, V), ("K", "V"))
-    if O is None:
-        O = _fresh(Q, shape)
-    else:
-        _alike(acsr, Q, shape, dt, dev, (O,), ("O",))
-    if lse is None:
-        lse = torch.empty((B, H, L), dtype=torch.float32, device=Q.device)
-    else:
-        _rows(lse, "lse", (B, H, L), dev)
-    _check(load().splat_sparse_mhsa_fwd_lse(acsr.handle, _DT[dt], B, H, d, Q.data_ptr(),
-                                            K.data_ptr(), V.data_ptr(), float(scale), O.data_ptr(),
-                                            lse.data_ptr(), _stream_of(dev)))
-    return O, lse
+    return native().fwd_lse(acsr.handle.value, Q, K, V, scale, O, lse, *_where())
 
 
 def sparse_mhsa_bwd(acsr: Acsr, Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, O: torch.Tensor,
@@ -572,76 +554,41 @@ def sparse_mhsa_bwd(acsr: Acsr, Q: torch.Tensor, K: torch.Tensor, V: torch.Tenso
     """(dQ, dK, dV) of sparse_mhsa_fwd_lse from the gradient dO of its O.  Needs a
     handle built with grad=True.  workspace: fp32 [2, B, H, L], made by the call
     unless given."""
-    _dense(Q, "Q", acsr)
-    shape, dt, dev = Q.shape, Q.dtype, _here(Q, "Q")
-    B, H, L, d = shape
-    _alike(acsr, Q, shape, dt, dev, (K, V, O, dO), ("K", "V", "O", "dO"))
-    _rows(lse, "lse", (B, H, L), dev)
-    if dQ is None:
-        dQ = _fresh(Q, shape)
-    else:
-        _alike(acsr, Q, shape, dt, dev, (dQ,), ("dQ",))
-    if dK is None:
-        dK = _fresh(Q, shape)
-    else:
-        _alike(acsr, Q, shape, dt, dev, (dK,), ("dK",))
-    if dV is None:
-        dV = _fresh(Q, shape)
-    else:
-        _alike(acsr, Q, shape, dt, dev, (dV,), ("dV",))
-    if workspace is None:
-        workspace = torch.empty((2, B, H, L), dtype=torch.float32, device=Q.device)
-    else:
-        _rows(workspace, "workspace", (2, B, H, L), dev)
-    _check(load().splat_sparse_mhsa_bwd(acsr.handle, _DT[dt], B, H, d, Q.data_ptr(), K.data_ptr(),
-                                        V.data_ptr(), O.data_ptr(), lse.data_ptr(), dO.data_ptr(),
-                                        float(scale), dQ.data_ptr(), dK.data_ptr(), dV.data_ptr(),
-                                        workspace.data_ptr(), _stream_of(dev)))
-    return dQ, dK, dV
+    return native().bwd(acsr.handle.value, Q, K, V, O, lse, dO, scale, dQ, dK, dV, workspace, *_where())
 
 
-# The current device's number: without torch.cuda's own checks where this torch
-# has the call (an initialised device is at hand: a tensor lives on it).
+_NATIVE = None
+
+
+def native():
+    """The extension with the training and serving calls (csrc/binding.cpp), built
+    beside libsplat.so.  Raises if it is missing."""
+    global _NATIVE
+    if _NATIVE is None:
+        load()
+        path = os.path.join(os.path.dirname(lib_path()), "_native.so")
+        if not os.path.exists(path):
+            raise RuntimeError(f"{path} is not built; run `python -m paper_2407_16847_amd.build` "
+                               "(or __graft_entry__.build()) first")
+        from . import _native
+        _NATIVE = _native
+    return _NATIVE
+
+
+# The current device's number: without torch.cuda's own checks where this torch has
+# the call.
 _device_now = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
-def _here(x: torch.Tensor, name: str) -> int:
-    """The number of x's device, which must be the current one."""
-    dev = x.get_device()
-    if dev != _device_now():
-        raise ValueError(f"{name} is on cuda:{dev}, the current device is cuda:{_device_now()}")
-    return dev
-
-
-def _stream_of(dev: int) -> int:
-    return _raw_stream(dev) if _raw_stream is not None else torch.cuda.current_stream().cuda_stream
-
-
-def _alike(acsr: Acsr, Q: torch.Tensor, shape, dt, dev: int, xs, names) -> None:
-    """Every x of xs matches Q, whose shape, dtype and device are given: a few
-    comparisons each (_like's checks find what is wrong)."""
-    for x, name in zip(xs, names):
-        if not (isinstance(x, torch.Tensor) and x.dtype is dt and x.get_device() == dev
-                and x.shape == shape and x.is_contiguous()):
-            _like(x, name, Q, acsr)
-            raise ValueError(f"{name} must match Q")
-
-
-def _fresh(ref: torch.Tensor, shape) -> torch.Tensor:
-    """An uninitialised plain contiguous tensor of `shape`, of ref's dtype and device."""
-    if type(ref) is torch.Tensor:
-        return ref.new_empty(shape)
-    return torch.empty(tuple(shape), dtype=ref.dtype, device=ref.device)
-
-
-def _rows(x: torch.Tensor, name: str, shape, dev: int) -> None:
-    """x is fp32 of `shape`."""
-    if not isinstance(x, torch.Tensor) or not x.is_cuda:
-        raise TypeError(f"{name} must be a CUDA (HIP) tensor")
-    if x.dtype is not torch.float32 or x.shape != shape or not x.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous float32 {list(shape)} tensor")
-    if x.get_device() != dev:
-        raise ValueError(f"{name} is on {x.device}, expected cuda:{dev}")
+def _where() -> Tuple[int, int]:
+    """The current device's number and its current stream (-1, 0 without a GPU: the
+    calls then refuse their tensors)."""
+    if not torch.cuda.is_initialized():
+        if not torch.cuda.is_available():
+            return -1, 0
+        torch.cuda.init()
+    dev = _device_now()
+    return dev, _raw_stream(dev) if _raw_stream is not None else torch.cuda.current_stream().cuda_stream
 
 
 class Rotary:
@@ -688,57 +635,6 @@ class Rotary:
         return t
 
 
-def _heads(x: torch.Tensor, name: str, dt, dev: int, B: int, T: int, d: int):
-    """x [B, heads, T, d] as a splat_heads: (address, strides, heads)."""
-    if not isinstance(x, torch.Tensor) or not x.is_cuda:
-        raise TypeError(f"{name} must be a CUDA (HIP) tensor")
-    shape = x.shape
-    if x.dtype is not dt or len(shape) != 4 or shape[0] != B or shape[2] != T or shape[3] != d:
-        raise ValueError(f"{name} must be {dt} [{B}, heads, {T}, {d}], got {x.dtype} {list(shape)}")
-    sb, sh, st, sd = x.stride()
-    if sd != 1:
-        raise ValueError(f"{name}'s features must be contiguous")
-    if x.get_device() != dev:
-        raise ValueError(f"{name} is on {x.device}, expected cuda:{dev}")
-    return x.data_ptr(), sb, sh, st, shape[1]
-
-
-def _first(x: torch.Tensor, name: str):
-    """(dtype, device number, shape) of a call's first [B, heads, T, d] tensor."""
-    if not isinstance(x, torch.Tensor) or not x.is_cuda:
-        raise TypeError(f"{name} must be a CUDA (HIP) tensor")
-    if x.dtype not in _DT:
-        raise TypeError(f"{name} must be float32 or bfloat16, got {x.dtype}")
-    shape = x.shape
-    if len(shape) != 4 or 0 in shape:
-        raise ValueError(f"{name} must be [B, heads, T, d] with no empty axis, got {tuple(shape)}")
-    return x.dtype, _here(x, name), shape
-
-
-def _turned(x: torch.Tensor, y: Optional[torch.Tensor], name: str, dt, dev: int):
-    """The output for x and its splat_heads: y, or a new contiguous tensor."""
-    B, H, T, d = x.shape
-    if y is None:
-        y = _fresh(x, (B, H, T, d))
-        return y, (y.data_ptr(), H * T * d, T * d, d, H)
-    h = _heads(y, name, dt, dev, B, T, d)
-    if h[4] != H:
-        raise ValueError(f"{name} must be {tuple(x.shape)}, got {tuple(y.shape)}")
-    return y, h
-
-
-def _ints(x: torch.Tensor, name: str, shape, dev: int) -> int:
-    """The address of x, contiguous int32 of `shape`."""
-    if not isinstance(x, torch.Tensor) or not x.is_cuda:
-        raise TypeError(f"{name} must be a CUDA (HIP) tensor")
-    if x.dtype is not torch.int32 or x.shape != shape or not x.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous int32 {list(shape)} tensor, "
-                         f"got {x.dtype} {list(x.shape)}")
-    if x.get_device() != dev:
-        raise ValueError(f"{name} is on {x.device}, expected cuda:{dev}")
-    return x.data_ptr()
-
-
 def rotary(rot: Rotary, X: torch.Tensor, X2: Optional[torch.Tensor] = None, *,
            positions: Optional[torch.Tensor] = None, inverse: bool = False,
            Y: Optional[torch.Tensor] = None, Y2: Optional[torch.Tensor] = None):
@@ -746,46 +642,7 @@ def rotary(rot: Rotary, X: torch.Tensor, X2: Optional[torch.Tensor] = None, *,
     positions -- int32 [B, T], or 0 .. T-1 -- as a contiguous tensor, or into Y,
     which may be X.  With X2 (its own number of heads; a layer's Q and K in one
     launch) returns both.  inverse=True: the transposed rotation, its gradient."""
-    dt, dev, (B, _, T, d) = _first(X, "X")
-    x = _heads(X, "X", dt, dev, B, T, d)
-    Y, y = _turned(X, Y, "Y", dt, dev)
-    if X2 is None:
-        if Y2 is not None:
-            raise ValueError("Y2 needs X2")
-        xy, n = _WORDS[10](*x, *y), 1
-    else:
-        x2 = _heads(X2, "X2", dt, dev, B, T, d)
-        if x2[4] == 0:
-            raise ValueError("X2 has no heads")
-        Y2, y2 = _turned(X2, Y2, "Y2", dt, dev)
-        xy, n = _WORDS[20](*x, *y, *x2, *y2), 2
-    pos = None if positions is None else _ints(positions, "positions", (B, T), dev)
-    _check(load().splat_rotary_apply(rot.handle, _DT[dt], B, T, d, pos, xy, n, 1 if inverse else 0,
-                                     _stream_of(dev)))
-    return Y if X2 is None else (Y, Y2)
-
-
-def _cache(k_cache: torch.Tensor, v_cache: torch.Tensor, table: torch.Tensor, dt, dev: int, B: int,
-           d: int):
-    """The paged cache as a splat_cache, and its heads."""
-    for x, name in ((k_cache, "k_cache"), (v_cache, "v_cache")):
-        if not isinstance(x, torch.Tensor) or not x.is_cuda:
-            raise TypeError(f"{name} must be a CUDA (HIP) tensor")
-        if x.dtype is not dt or x.dim() != 4 or not x.is_contiguous():
-            raise ValueError(f"{name} must be a contiguous {dt} [pages, heads, page, {d}] tensor, "
-                             f"got {x.dtype} {list(x.shape)}")
-        if x.get_device() != dev:
-            raise ValueError(f"{name} is on {x.device}, expected cuda:{dev}")
-    shape = k_cache.shape
-    if shape[3] != d or v_cache.shape != shape:
-        raise ValueError(f"k_cache and v_cache must both be [pages, heads, page, {d}], "
-                         f"got {list(shape)} and {list(v_cache.shape)}")
-    if not isinstance(table, torch.Tensor) or table.dim() != 2:
-        raise ValueError("table must be [B, max_pages]")
-    most = table.shape[1]
-    at = _ints(table, "table", (B, most), dev)
-    return (_WORDS[7](k_cache.data_ptr(), v_cache.data_ptr(), at, shape[0], shape[1], shape[2], most),
-            shape[1])
+    return native().rotary(rot.handle.value, X, X2, positions, inverse, Y, Y2, *_where())
 
 
 def cache_append(k_cache: torch.Tensor, v_cache: torch.Tensor, table: torch.Tensor,
@@ -798,24 +655,8 @@ def cache_append(k_cache: torch.Tensor, v_cache: torch.Tensor, table: torch.Tens
     position start[b], K rotated on the way; only the first counts[b] tokens, if
     given.  With Q [B, H, T, d] returns its rotation at the same positions (in Qr,
     if given; padding rows 0)."""
-    dt, dev, (B, _, T, d) = _first(K, "K")
-    k, v = _heads(K, "K", dt, dev, B, T, d), _heads(V, "V", dt, dev, B, T, d)
-    c, _ = _cache(k_cache, v_cache, table, dt, dev, B, d)
-    first = _ints(start, "start", (B,), dev)
-    count = None if counts is None else _ints(counts, "counts", (B,), dev)
-    if Q is None:
-        if Qr is not None:
-            raise ValueError("Qr needs Q")
-        kvq, n = _WORDS[10](*k, *v), 2
-    else:
-        q = _heads(Q, "Q", dt, dev, B, T, d)
-        if q[4] == 0:
-            raise ValueError("Q has no heads")
-        Qr, qr = _turned(Q, Qr, "Qr", dt, dev)
-        kvq, n = _WORDS[20](*k, *v, *q, *qr), 4
-    _check(load().splat_cache_append(None if rot is None else rot.handle, _DT[dt], B, T, d, c, first,
-                                     count, kvq, n, _stream_of(dev)))
-    return Qr
+    return native().cache_append(0 if rot is None else rot.handle.value, k_cache, v_cache, table, start,
+                                 K, V, counts, Q, Qr, *_where())
 
 
 def decode_workspace(acsr: Acsr, B: int, H: int, heads: int, d: int) -> int:
@@ -833,32 +674,8 @@ def sparse_mhsa_decode(acsr: Acsr, Q: torch.Tensor, k_cache: torch.Tensor, v_cac
     mask's row lengths[b] - 1, its columns below lengths[b] (int32 [B]).  The
     cache's heads divide H.  workspace: at least decode_workspace() bytes, made by
     the call unless given."""
-    dt, dev, shape = _first(Q, "Q")
-    B, H, T, d = shape
-    if T != 1 or not Q.is_contiguous():
-        raise ValueError(f"Q must be a contiguous [B, H, 1, d] tensor, got {tuple(shape)}")
-    c, heads = _cache(k_cache, v_cache, table, dt, dev, B, d)
-    at = _ints(lengths, "lengths", (B,), dev)
-    if O is None:
-        O = _fresh(Q, shape)
-    else:
-        if not isinstance(O, torch.Tensor) or not O.is_cuda:
-            raise TypeError("O must be a CUDA (HIP) tensor")
-        if O.dtype is not dt or O.shape != shape or not O.is_contiguous() or O.get_device() != dev:
-            raise ValueError(f"O must be a contiguous {dt} {list(shape)} tensor on cuda:{dev}")
-    need = decode_workspace(acsr, B, H, heads, d)
-    if workspace is not None:
-        if not isinstance(workspace, torch.Tensor) or not workspace.is_cuda:
-            raise TypeError("workspace must be a CUDA (HIP) tensor")
-        if (workspace.numel() * workspace.element_size() < need or not workspace.is_contiguous()
-                or workspace.get_device() != dev):
-            raise ValueError(f"workspace must be contiguous on cuda:{dev} and hold {need} bytes")
-    elif need:
-        workspace = torch.empty(need // 4, dtype=torch.float32, device=Q.device)
-    _check(load().splat_sparse_mhsa_decode(acsr.handle, _DT[dt], B, H, d, Q.data_ptr(), c, at,
-                                           float(scale), O.data_ptr(),
-                                           workspace.data_ptr() if need else None, _stream_of(dev)))
-    return O
+    return native().decode(acsr.handle.value, Q, k_cache, v_cache, table, lengths, scale, O, workspace,
+                           *_where())
 
 
 def _values(x: torch.Tensor, name: str, acsr: Acsr, B: int, H: int) -> None:

@@ -22,6 +22,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "libsplat.so")
 BUILD_DIR = os.path.join(HERE, "_build")
+OUT_BINDING = os.path.join(HERE, "_native.so")
 OUT_CHECKED = os.path.join(HERE, "libsplat_checked.so")
 BUILD_DIR_CHECKED = os.path.join(HERE, "_build_checked")
 ARCH = "gfx950"
@@ -89,9 +90,36 @@ def build(verbose: bool = False, checked: bool = False) -> str:
     return target
 
 
+def build_binding(verbose: bool = False) -> str:
+    """The Python extension of the training and serving calls (csrc/binding.cpp),
+    against the installed torch and the libsplat.so beside it."""
+    import sysconfig
+
+    import torch
+    from torch.utils.cpp_extension import include_paths
+    t0 = time.time()
+    inc = [f"-isystem{p}" for p in (*include_paths(), sysconfig.get_paths()["include"])]
+    lib = os.path.join(torch.__path__[0], "lib")
+    tmp = OUT_BINDING + ".tmp"
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", *inc,
+           os.path.join(CSRC, "binding.cpp"), "-o", tmp, f"-L{HERE}", "-l:libsplat.so",
+           "-Wl,-rpath,$ORIGIN", f"-L{lib}", "-ltorch", "-ltorch_cpu", "-lc10", "-ltorch_python"]
+    if verbose:
+        print(" ".join(cmd), flush=True)
+    r = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT)
+    if r.returncode != 0:
+        raise RuntimeError("binding build failed:\n" + r.stdout.decode(errors="replace"))
+    os.replace(tmp, OUT_BINDING)
+    if verbose:
+        print(f"built {OUT_BINDING} in {time.time() - t0:.1f} s", flush=True)
+    return OUT_BINDING
+
+
 def build_all(verbose: bool = False) -> None:
-    """Both libraries: the regular one and the checked one."""
+    """Both libraries, the regular one and the checked one, and the extension."""
     build(verbose=verbose)
+    build_binding(verbose=verbose)
     build(verbose=verbose, checked=True)
 
 
