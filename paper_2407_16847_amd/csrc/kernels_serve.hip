@@ -3,6 +3,8 @@
 #include <hip/hip_runtime.h>
 #include <math.h>
 
+#include <algorithm>
+
 #include "serve_core.hpp"
 #include "slice_ops.hpp"
 
@@ -66,41 +68,37 @@ __global__ __launch_bounds__(kThreads) void k_heads(const HeadsArgs x, int per_b
   const int page =
       x.pages && counts ? page_of(x.pages, b, x.max_pages, x.n_pages, x.page_shift, pos) : -1;
 
-  const int first = blockIdx.y * per_block;
-  int all = 0;
-  for (int k = 0; k < x.n_jobs; ++k) all += x.job[k].heads;
-  const int last = min(first + per_block, all);
+  // blockIdx.y: a run of one tensor's heads
+  int j = 0, run = blockIdx.y;
+  while (run >= (x.job[j].heads + per_block - 1) / per_block)
+    run -= (x.job[j].heads + per_block - 1) / per_block, ++j;
+  const HeadsJob& job = x.job[j];
+  const int first = run * per_block, last = min(first + per_block, job.heads);
+  const bool rot = job.rotate && turns && counts;
+  char* to = job.y + c0;
+  int64_t next = job.yh;                // to the next head
+  if (job.paged) {
+    if (page < 0) return;
+    to += (size_t)cache_row(page, job.heads, first, x.page_shift, pos) * (D * sizeof(T));
+    next = ((int64_t)D * (int)sizeof(T)) << x.page_shift;
+  } else {
+    to += b * job.yb + t * job.yt + first * job.yh;
+  }
+  const char* from = job.x + c0 + b * job.xb + t * job.xt + first * job.xh;
   for (int h0 = first; h0 < last; h0 += kInFlight) {
     vec_t v[kInFlight][2];
-    char* to[kInFlight];
-    bool rot[kInFlight];
 #pragma unroll
     for (int k = 0; k < kInFlight; ++k) {
-      to[k] = nullptr;
-      if (h0 + k >= last) continue;
-      int h = h0 + k, j = 0;
-      while (h >= x.job[j].heads) h -= x.job[j].heads, ++j;
-      const HeadsJob& job = x.job[j];
-      rot[k] = job.rotate && turns;
-      if (job.paged) {
-        if (page < 0) continue;
-        to[k] = job.y +
-                (size_t)cache_row(page, job.heads, h, x.page_shift, pos) * (D * sizeof(T)) + c0;
-      } else {
-        to[k] = job.y + b * job.yb + h * job.yh + t * job.yt + c0;
+      v[k][0] = vec_t{}, v[k][1] = vec_t{};
+      if (h0 + k < last && counts) {
+        v[k][0] = *(const vec_t*)(from + k * job.xh);
+        v[k][1] = *(const vec_t*)(from + k * job.xh + step);
       }
-      if (!counts) {
-        v[k][0] = vec_t{}, v[k][1] = vec_t{};
-        rot[k] = false;
-        continue;
-      }
-      const char* from = job.x + b * job.xb + h * job.xh + t * job.xt + c0;
-      v[k][0] = *(const vec_t*)from, v[k][1] = *(const vec_t*)(from + step);
     }
 #pragma unroll
     for (int k = 0; k < kInFlight; ++k) {
-      if (!to[k]) continue;
-      if (rot[k]) {
+      if (h0 + k >= last) continue;
+      if (rot) {
         vec_t r[2];
 #pragma unroll
         for (int e = 0; e < E; ++e) {
@@ -116,8 +114,9 @@ __global__ __launch_bounds__(kThreads) void k_heads(const HeadsArgs x, int per_b
         }
         v[k][0] = r[0], v[k][1] = r[1];
       }
-      *(vec_t*)to[k] = v[k][0], *(vec_t*)(to[k] + step) = v[k][1];
+      *(vec_t*)(to + k * next) = v[k][0], *(vec_t*)(to + k * next + step) = v[k][1];
     }
+    from += kInFlight * job.xh, to += kInFlight * next;
   }
 }
 
@@ -130,7 +129,9 @@ hipError_t heads_launch(const HeadsArgs& x, hipStream_t st) {
   // as many heads a thread as leave the chip eight workgroups a CU
   int64_t per = blocks * heads / 2048;
   per = per < 1 ? 1 : per > 8 ? 8 : per;
-  const dim3 grid((unsigned)blocks, (unsigned)((heads + per - 1) / per));
+  int64_t runs = 0;
+  for (int k = 0; k < x.n_jobs; ++k) runs += (x.job[k].heads + per - 1) / per;
+  const dim3 grid((unsigned)blocks, (unsigned)runs);
   if (x.interleaved)
     hipLaunchKernelGGL((k_heads<T, D, true>), grid, dim3(kThreads), 0, st, x, (int)per);
   else
@@ -307,32 +308,48 @@ __global__ __launch_bounds__(kThreads) void k_decode(
       *(f32x2_t*)(part + 4 + c) = f32x2_t{v[2], v[3]};
     }
   }
-  if (splits > 1 && (threadIdx.x & 7) == 0) *(f32x2_t*)part = f32x2_t{mt, lt};
+  if (splits > 1 && (threadIdx.x & 7) == 0)
+    *(f32x2_t*)part = n == 0 ? f32x2_t{0.f, 1.f} : f32x2_t{mt, lt};
 }
 
-// One wavefront per (sequence, head): the splits' parts to O.
+// One wavefront per (sequence, head): the splits' parts (m, l, O) to O, eight
+// parts' loads in flight at a time (one after the other they took 10 us of a
+// decode of one sequence).  A row without keys has parts (0, 1, 0).
 template <typename T, int D>
-__global__ __launch_bounds__(64) void k_decode_join(
-    const RowRuns* __restrict__ runs, int L, int H, const int32_t* __restrict__ lengths,
-    int max_pages, int page_shift, int splits, const float* __restrict__ ws, T* __restrict__ O) {
+__global__ __launch_bounds__(64) void k_decode_join(int splits, const float* __restrict__ ws,
+                                                    T* __restrict__ O) {
+  constexpr int STEP = 8;
   const int lane = threadIdx.x, row = blockIdx.x;
   const float* const part = ws + (size_t)row * splits * (D + 2);
-  RowRuns rr;
-  const int n = row_keys(runs, L, lengths[row / H], (int64_t)max_pages << page_shift, rr);
   float m = -INFINITY, l = 0.f;
-  if (lane < splits) m = part[lane * (D + 2)], l = part[lane * (D + 2) + 1];
-  const float mt = wave_max(m), f = m == -INFINITY ? 0.f : exp2_hw(m - mt);
-  const float lt = wave_sum(m == -INFINITY ? l : l * f);
-  const float inv = n == 0 ? 0.f : 1.f / (lt == 0.f ? NAN : lt);
-  float acc[D / 64];
+  if (lane < splits) {
+    const f32x2_t ml = *(const f32x2_t*)(part + lane * (D + 2));
+    m = ml[0], l = ml[1];
+  }
+  float acc[D / 64], x[STEP][D / 64];
 #pragma unroll
   for (int b = 0; b < D / 64; ++b) acc[b] = 0.f;
-  for (int s = 0; s < splits; ++s) {
-    const float fs = __builtin_bit_cast(
-        float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, f), s));
+  auto load = [&](int s0) {
 #pragma unroll
-    for (int b = 0; b < D / 64; ++b)
-      acc[b] = fmaf(part[s * (D + 2) + 2 + 64 * b + lane], fs, acc[b]);
+    for (int k = 0; k < STEP; ++k)
+#pragma unroll
+      for (int b = 0; b < D / 64; ++b)
+        x[k][b] = part[min(s0 + k, splits - 1) * (D + 2) + 2 + 64 * b + lane];
+  };
+  load(0);
+  const float mt = wave_max(m), f = m == -INFINITY ? 0.f : exp2_hw(m - mt);
+  const float lt = wave_sum(m == -INFINITY ? l : l * f);
+  const float inv = 1.f / (lt == 0.f ? NAN : lt);   // keys that all score -inf: NaN
+  for (int s0 = 0; s0 < splits; s0 += STEP) {
+    if (s0) load(s0);
+#pragma unroll
+    for (int k = 0; k < STEP; ++k) {
+      if (s0 + k >= splits) continue;
+      const float fk = __builtin_bit_cast(
+          float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, f), s0 + k));
+#pragma unroll
+      for (int b = 0; b < D / 64; ++b) acc[b] = fmaf(x[k][b], fk, acc[b]);
+    }
   }
 #pragma unroll
   for (int b = 0; b < D / 64; ++b) store1(O + (size_t)row * D + 64 * b + lane, acc[b] * inv);
@@ -350,8 +367,7 @@ hipError_t decode_launch(const DevAcsr& a, const DecodeArgs& x, hipStream_t st) 
                      x.page_shift, sl2, (T*)x.O, x.ws);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || splits == 1) return e;
-  hipLaunchKernelGGL((k_decode_join<T, D>), dim3(x.B * x.H), dim3(64), 0, st, a.runs, a.L, x.H,
-                     x.lengths, x.max_pages, x.page_shift, splits, x.ws, (T*)x.O);
+  hipLaunchKernelGGL((k_decode_join<T, D>), dim3(x.B * x.H), dim3(64), 0, st, splits, x.ws, (T*)x.O);
   return hipGetLastError();
 }
 
@@ -378,14 +394,16 @@ hipError_t prepare_decode() {
   return e;
 }
 
-// As many splits as fill the chip with two workgroups a CU, while each wavefront
-// keeps a unit.
+// As many splits as fill the chip with two workgroups a CU while each wavefront
+// keeps two units.  One / two / four units a wavefront: window 512 + 64 global at
+// L = 4000, 16 heads, one sequence 10.4 / 8.5 / 7.8 us; every key of 8192, d = 128, 32
+// heads over 8, one sequence 21 / 15 / 17 us.  Twice and four times the workgroups
+// for 32 sequences of 1000 .. 8192 keys: 130 -> 138, 150 us.
 int decode_splits(const DevAcsr& a, int B, int H, int heads) {
   const int64_t groups = (int64_t)B * heads * head_chunks(H, heads);
   const int64_t units = (a.max_row_nnz + kUnit - 1) / kUnit;
-  int64_t s = (512 + groups - 1) / groups;
-  if (s > (units + 3) / 4) s = (units + 3) / 4;
-  return (int)(s < 1 ? 1 : s > kMaxSplits ? kMaxSplits : s);
+  const int64_t s = std::min((512 + groups - 1) / groups, (units + 7) / 8);
+  return (int)std::min<int64_t>(std::max<int64_t>(s, 1), kMaxSplits);
 }
 
 int64_t decode_workspace(const DevAcsr& a, int B, int H, int heads, int d) {
