@@ -444,7 +444,8 @@ splat_status splat_sparse_mhsa_fwd(splat_acsr_t h, splat_dtype dtype, int32_t B,
  * rounds scale * Q to bf16 first), so O may differ from that call's by roundings
  * of that size.  Only a row's own keys count, whatever the others hold: a row
  * whose products over its tiles are not finite is formed again from its keys
- * alone.  O and lse share no memory with Q, K, V or each other (INVALID_ARG).
+ * alone; a row whose scores are all -inf gets NaN (and lse -inf).  O and lse share no
+ * memory with Q, K, V or each other (INVALID_ARG).
  *
  * splat_sparse_mhsa_bwd -- dQ, dK, dV [B,H,L,d] of `dtype` from Q, K, V, the O and
  * lse of splat_sparse_mhsa_fwd_lse and the gradient dO of O, all [B,H,L,d] of
@@ -457,7 +458,8 @@ splat_status splat_sparse_mhsa_fwd(splat_acsr_t h, splat_dtype dtype, int32_t B,
  * workspace: 2*B*H*L floats of device memory that the call writes and reads (calls
  * that may run at the same time need one each).  The gradients and the workspace
  * share no memory with the inputs or each other (INVALID_ARG).  The handle must
- * have been built with SPLAT_PLAN_GRAD (INVALID_ARG).
+ * have been built with SPLAT_PLAN_GRAD (INVALID_ARG).  bf16: UNSUPPORTED where the
+ * row or key groups times B*H exceed 2^22.
  */
 splat_status splat_sparse_mhsa_fwd_lse(splat_acsr_t h, splat_dtype dtype, int32_t B, int32_t H,
                                        int32_t d, const void* Q, const void* K, const void* V,
@@ -516,8 +518,8 @@ typedef struct {
  * and K) of `dtype`: xy[2 * n] is x, y for each in turn.  positions: int32 [B, T] on the
  * device, NULL for 0 .. T-1.  inverse: the transposed rotation, which is the
  * gradient (and, at magnitude 1, the inverse).  A token whose position lies
- * outside [0, max_len) gets NaN in its rotated features.  fp32 arithmetic, one
- * rounding.  y may be x itself (same strides) and otherwise shares no memory
+ * outside [0, max_len) gets NaN in its rotated features.  B*T <= 2^27.  fp32
+ * arithmetic, one rounding.  y may be x itself (same strides) and otherwise shares no memory
  * with either input or the other output (INVALID_ARG).
  */
 splat_status splat_rotary_apply(splat_rotary_t r, splat_dtype dtype, int32_t B, int32_t T, int32_t d,
@@ -614,6 +616,15 @@ splat_status splat_debug_bounds_probe(int32_t kind, int32_t index, int32_t n, in
  */
 splat_status splat_debug_route(splat_acsr_t h, int32_t call, splat_dtype dtype, int32_t B,
                                int32_t H, int32_t d, int32_t* route, int32_t* sets);
+
+/*
+ * splat_debug_bwd_shared -- how many of the plan's groups the backward pass gives
+ * four workgroups each (bf16; the longest ones), in the kernel of dQ (shared[0])
+ * and of dK and dV (shared[1]); 0 and 0 with fp32 inputs.  Host only, for tests of
+ * the choice, which may change between versions.  The handle needs SPLAT_PLAN_GRAD.
+ */
+splat_status splat_debug_bwd_shared(splat_acsr_t h, splat_dtype dtype, int32_t B, int32_t H, int32_t d,
+                                    int32_t shared[2]);
 
 /* Message of the calling thread's last non-OK status ("" if none). */
 const char* splat_last_error(void);

@@ -157,6 +157,7 @@ def _open(path: str) -> ctypes.CDLL:
         "splat_sparse_mhsa_unfused": [vp, i32, i32, i32, i32, vp, vp, vp, f32, vp, vp, vp, i32, f32,
                                       P(i32), vp],
         "splat_debug_route": [vp, i32, i32, i32, i32, i32, P(i32), P(i32)],
+        "splat_debug_bwd_shared": [vp, i32, i32, i32, i32, P(i32)],
         "splat_debug_bounds": [P(ctypes.c_uint32), i32],
         "splat_debug_bounds_probe": [i32, i32, i32, P(i32)],
     }
@@ -403,6 +404,14 @@ def route(acsr: Acsr, call: str, dtype: torch.dtype, B: int, H: int, d: int) -> 
     _check(acsr._lib.splat_debug_route(acsr.handle, _CALLS.index(call), _DT[dtype], B, H, d,
                                        ctypes.byref(r), ctypes.byref(n)))
     return _ROUTES[r.value], n.value
+
+
+def bwd_shared(acsr: Acsr, dtype: torch.dtype, B: int, H: int, d: int) -> Tuple[int, int]:
+    """How many of the plan's groups sparse_mhsa_bwd gives four workgroups each, for
+    dQ and for dK and dV (splat_debug_bwd_shared): for tests; needs no GPU."""
+    n = (ctypes.c_int32 * 2)()
+    _check(acsr._lib.splat_debug_bwd_shared(acsr.handle, _DT[dtype], B, H, d, n))
+    return n[0], n[1]
 
 
 

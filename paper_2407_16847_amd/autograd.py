@@ -1,0 +1,68 @@
+"""The training calls as differentiable functions.
+
+    from paper_2407_16847_amd import autograd as sag
+    Q, K = sag.rotary(rot, Q), sag.rotary(rot, K)
+    O = sag.sparse_mhsa(acsr, Q, K, V, scale)      # acsr built with grad=True
+    O.backward(dO)
+
+The gradients are the library's backward calls and can be taken once (not
+differentiated again).  To capture a training step into a graph, capture
+sparse_mhsa_fwd_lse, sparse_mhsa_bwd and rotary themselves: they allocate
+nothing when given their outputs.
+"""
+from __future__ import annotations
+
+from typing import Optional
+
+import torch
+from torch.autograd.function import once_differentiable
+
+from . import Acsr, Rotary
+from . import rotary as _rotary
+from . import sparse_mhsa_bwd, sparse_mhsa_fwd, sparse_mhsa_fwd_lse
+
+__all__ = ["sparse_mhsa", "rotary"]
+
+
+class _SparseMHSA(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, acsr, Q, K, V, scale):
+        O, lse = sparse_mhsa_fwd_lse(acsr, Q, K, V, scale)
+        ctx.save_for_backward(Q, K, V, O, lse)
+        ctx.acsr, ctx.scale = acsr, scale
+        return O
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dO):
+        Q, K, V, O, lse = ctx.saved_tensors
+        dQ, dK, dV = sparse_mhsa_bwd(ctx.acsr, Q, K, V, O, lse, dO.contiguous(), ctx.scale)
+        return None, dQ, dK, dV, None
+
+
+class _Rotary(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, rot, X, positions):
+        ctx.rot, ctx.positions = rot, positions
+        return _rotary(rot, X, positions=positions)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dY):
+        return None, _rotary(ctx.rot, dY.contiguous(), positions=ctx.positions, inverse=True), None
+
+
+def sparse_mhsa(acsr: Acsr, Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor,
+                scale: float) -> torch.Tensor:
+    """O = softmax_nz(scale * M (x) Q K^T) V with gradients for Q, K and V.  Without
+    any to take this is sparse_mhsa_fwd."""
+    if not (torch.is_grad_enabled() and (Q.requires_grad or K.requires_grad or V.requires_grad)):
+        return sparse_mhsa_fwd(acsr, Q, K, V, scale)
+    if not acsr._info["grad"]:
+        raise ValueError("gradients need a handle built with grad=True")
+    return _SparseMHSA.apply(acsr, Q, K, V, float(scale))
+
+
+def rotary(rot: Rotary, X: torch.Tensor, positions: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """X [B, H, T, d] rotated to its tokens' positions, with its gradient."""
+    return _Rotary.apply(rot, X, positions)

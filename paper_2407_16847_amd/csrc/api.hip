@@ -428,8 +428,8 @@ splat::HeadsJob heads_job(const View& x, const View* y, bool rotate) {
 }
 
 splat_status check_tokens(int32_t B, int32_t T) {
-  if (B < 1 || T < 1 || (int64_t)B * T > INT32_MAX)
-    return fail(SPLAT_ERR_INVALID_ARG, "B and T must be >= 1 with B*T < 2^31 (got B=%d, T=%d)", B, T);
+  if (B < 1 || T < 1 || (int64_t)B * T > (1 << 27))   // 16 tokens a workgroup at least
+    return fail(SPLAT_ERR_INVALID_ARG, "B and T must be >= 1 with B*T <= 2^27 (got B=%d, T=%d)", B, T);
   return SPLAT_OK;
 }
 
@@ -1136,6 +1136,19 @@ splat_status splat_debug_route(splat_acsr_t h, int32_t call, splat_dtype dtype, 
   }
   if (call >= 3) *route = splat::unfused_route(a, dtype, BH, d, call == 4, call != 5);
   if (sets) *sets = n;
+  return ok();
+}
+
+splat_status splat_debug_bwd_shared(splat_acsr_t h, splat_dtype dtype, int32_t B, int32_t H, int32_t d,
+                                    int32_t shared[2]) {
+  if (!h || !shared) return fail(SPLAT_ERR_INVALID_ARG, "handle and shared must be non-NULL");
+  CHECK(check_batch(B, H));
+  CHECK(check_dtype(dtype, "dtype"));
+  CHECK(check_d(d));
+  if (!h->host.has_grad)
+    return fail(SPLAT_ERR_INVALID_ARG, "the handle was built without SPLAT_PLAN_GRAD");
+  for (int k = 0; k < 2; ++k)
+    shared[k] = dtype == SPLAT_BF16 ? splat::grad_long_groups(h->dev, k == 1, B * H, d) : 0;
   return ok();
 }
 

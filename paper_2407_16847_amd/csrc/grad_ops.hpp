@@ -56,16 +56,28 @@ struct RowSum {
 #pragma unroll
     for (int b = 0; b < D / 64; ++b) acc[b] = 0.f;
   }
-  // adds w of lane t times row j of lane t, for the lanes t in `which`
+  // adds w of lane t times row j of lane t, for the lanes t in `which`: eight rows'
+  // loads in flight at a time (lanes without a row hold row 0)
   __device__ __forceinline__ void add(uint64_t which, int j, float w, const T* X, int lane) {
+    if (!which) return;
+    const int end = 64 - __builtin_clzll(which);
 #pragma unroll 1
-    for (; which; which &= which - 1) {
-      const int t = __builtin_ctzll(which);
-      const float wt = __builtin_bit_cast(
-          float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, w), t));
-      const T* const x = X + (size_t)__builtin_amdgcn_readlane(j, t) * D;
+    for (int t0 = __builtin_ctzll(which); t0 < end; t0 += 8) {
+      float x[8][D / 64];
 #pragma unroll
-      for (int b = 0; b < D / 64; ++b) acc[b] = fmaf(wt, (float)x[64 * b + lane], acc[b]);
+      for (int e = 0; e < 8; ++e) {
+        const T* const r = X + (size_t)__builtin_amdgcn_readlane(j, min(t0 + e, 63)) * D;
+#pragma unroll
+        for (int b = 0; b < D / 64; ++b) x[e][b] = (float)r[64 * b + lane];
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        if (t0 + e >= 64 || !((which >> (t0 + e)) & 1)) continue;
+        const float wt = __builtin_bit_cast(
+            float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, w), t0 + e));
+#pragma unroll
+        for (int b = 0; b < D / 64; ++b) acc[b] = fmaf(wt, x[e][b], acc[b]);
+      }
     }
   }
   __device__ __forceinline__ void store(T* out, float f, int lane) {

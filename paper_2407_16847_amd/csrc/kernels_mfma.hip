@@ -430,10 +430,12 @@ __device__ __forceinline__ void fused_tiles(
   }
 
   const float l_tot = l_run + lane_xor32(l_run);
-  const float inv = l_tot > 0.f ? 1.f / l_tot : 0.f;
+  float inv = l_tot > 0.f ? 1.f / l_tot : 0.f;
   uint64_t bad = 0;                    // LSE: rows to form again, by their lanes
   if constexpr (LSE) {
     const float lx = lx_run + lane_xor32(lx_run);
+    // keys that all score -inf: NaN
+    if (l_tot == 0.f && x.row_ptr[row + 1] > x.row_ptr[row]) inv = NAN;
     if (h == 0 && row_valid)
       x.lse[(size_t)bh * L + row] =
           lx == 0.f ? -INFINITY : (m_run + log2f(lx)) * 0.6931471805599453f;

@@ -39,6 +39,13 @@ CASES = [
     ("window_rows", {"w": 9, "lo": 40, "hi": 170}, 300, 2),
     ("none", {}, 50, 2),
 ]
+# launches whose groups stay with one workgroup each, and mixed ones: rows of few
+# keys, rows and keys of global tokens beside short ones, halves of 32 and less
+LARGE = [
+    ("window", {"w": 9}, 700, 130), ("window_global", {"w": 70, "n_global": 40}, 900, 60),
+    ("strided_local", {"local": 20, "stride": 50}, 1000, 90), ("full", {}, 290, 150),
+    ("dilated", {"w": 40, "dilation": 2}, 600, 120), ("window_rows", {"w": 25, "lo": 70, "hi": 400}, 560, 110),
+]
 TYPES = [torch.float32, torch.bfloat16]
 
 
@@ -148,6 +155,55 @@ def test_backward(gpu_lib, kind, params, L, heads, d, dtype):
         assert all(torch.equal(x, y) for x, y in zip(got, again))
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("kind,params,L,heads", LARGE)
+def test_backward_of_large_launches(gpu_lib, kind, params, L, heads, d):
+    """bf16: the first and the last heads of launches that fill the chip."""
+    splat = gpu_lib
+    print(f"[gpu] bwd large {kind} {params} L={L} heads={heads} d={d}", flush=True)
+    x = inputs(L, d, heads, torch.bfloat16, L + heads)
+    a, M = make(splat, kind, params, L)
+    dev, scale = [t.cuda() for t in x], 1.0 / math.sqrt(d)
+    O, lse = splat.sparse_mhsa_fwd_lse(a, *dev[:3], scale)
+    got = splat.sparse_mhsa_bwd(a, *dev[:3], O, lse, dev[3], scale)
+    torch.cuda.synchronize()
+    for h in (0, heads - 1):
+        one = [t[:, h:h + 1].cpu() for t in (*x[:3], O, lse, x[3])]
+        want, bound = backward64(*one, M, scale)
+        for name, g, w, b in zip(("dQ", "dK", "dV"), got, want, bound):
+            check(f"{name} head {h}", g[:, h:h + 1], w, b)
+
+
+@pytest.mark.parametrize("where", ["K", "V", "Q", "dO"])
+@pytest.mark.parametrize("kind,params,L,heads", [LARGE[0], LARGE[1], LARGE[5]])
+def test_large_launches_and_values_that_are_not_finite(gpu_lib, kind, params, L, heads, where):
+    """As above, where one workgroup has a group: a row or key with NaN."""
+    splat = gpu_lib
+    d, scale, x = 64, 0.125, L // 2
+    a, M = make(splat, kind, params, L)
+    T = dict(zip(("Q", "K", "V", "dO"), (t.cuda() for t in inputs(L, d, heads, torch.bfloat16, 9))))
+    T[where][:, :, x, 3] = 0.0
+
+    def run():
+        O, lse = splat.sparse_mhsa_fwd_lse(a, T["Q"], T["K"], T["V"], scale)
+        grads = splat.sparse_mhsa_bwd(a, T["Q"], T["K"], T["V"], O, lse, T["dO"], scale)
+        torch.cuda.synchronize()
+        return [y.cpu() for y in (O, *grads)]
+
+    clean = run()
+    T[where][:, :, x, 3] = math.nan
+    got = run()
+    rows = M[:, x].copy() if where in ("K", "V") else np.arange(L) == x
+    keys = M[rows].any(0)
+    rows, keys = torch.from_numpy(~rows), torch.from_numpy(~keys)
+    for g, r, ok in zip(got, clean, (rows, rows, keys, keys)):
+        g, r = g[:, :, ok].double(), r[:, :, ok].double()
+        assert torch.isfinite(g).all()
+        if g.numel():
+            top = r.abs().amax(-1, keepdim=True)
+            assert ((g - r).abs() <= 8 * HALF[torch.bfloat16] * top + 1e-6).all()
+
+
 @pytest.mark.parametrize("kind,params,L", [("window", {"w": 6}, 40), ("strided_local", {"local": 5, "stride": 7}, 45)])
 def test_gradients_are_the_differences(gpu_lib, kind, params, L):
     """fp32: each gradient along a direction against the change of sum(O dO),
@@ -248,6 +304,21 @@ def test_large_scores(gpu_lib):
             check(name, g, w, b)
 
 
+def test_scores_of_minus_infinity(gpu_lib):
+    """A row whose keys all score -inf gets NaN (both types); the others are as if
+    they were not there."""
+    splat = gpu_lib
+    for dtype in TYPES:
+        Q, K, V = inputs(200, 64, 2, dtype, 3, 3)
+        a, M = make(splat, "window", {"w": 10}, 200, grad=False)
+        Q[..., 0], K[..., 0] = 1.0, 0.0
+        K[:, :, :60, 0] = -math.inf
+        O, lse = splat.sparse_mhsa_fwd_lse(a, Q.cuda(), K.cuda(), V.cuda(), 0.125)
+        torch.cuda.synchronize()
+        assert torch.isnan(O[:, :, :50]).all() and (lse[:, :, :50] == -math.inf).all()
+        assert torch.isfinite(O[:, :, 50:]).all() and torch.isfinite(lse[:, :, 50:]).all()
+
+
 def test_batches_match_single_heads(gpu_lib):
     """A (batch, head) on its own gives what it gives among others."""
     splat = gpu_lib
@@ -298,3 +369,73 @@ def test_graph_replays_match_eager(gpu_lib):
             eager = (eO, el, *splat.sparse_mhsa_bwd(a, *sets[r][:3], eO, el, sets[r][3], 0.125))
             torch.cuda.synchronize()
             assert all(torch.equal(x, y) for x, y in zip((O, lse, dQ, dK, dV), eager)), r
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_autograd(gpu_lib, dtype):
+    """A layer's attention from its projections' layout: rotation, attention, and
+    the gradients of everything, against 64-bit autograd."""
+    from paper_2407_16847_amd import autograd as sag
+    from test_host_serve import frequencies
+    splat = gpu_lib
+    B, H, L, d, R, scale = 2, 3, 150, 64, 32, 0.125
+    a, M = make(splat, "window_global", {"w": 40, "n_global": 5}, L)
+    rot = splat.Rotary(L, R)
+    g = torch.Generator().manual_seed(3)
+    x = [torch.randn((B, L, H, d), generator=g).to(dtype) for _ in range(3)]
+    dO = torch.randn((B, H, L, d), generator=g).to(dtype)
+    leaf = [t.cuda().requires_grad_() for t in x]
+    q, k, v = (t.transpose(1, 2) for t in leaf)
+    O = sag.sparse_mhsa(a, sag.rotary(rot, q), sag.rotary(rot, k), v.contiguous(), scale)
+    O.backward(dO.cuda())
+    torch.cuda.synchronize()
+
+    ref = [t.double().requires_grad_() for t in x]
+    ang = torch.arange(L).double()[:, None] * torch.from_numpy(frequencies(R))
+
+    def turn(t):
+        u, w = t[..., :R // 2], t[..., R // 2:R]
+        c, s = ang.cos(), ang.sin()
+        return torch.cat((u * c - w * s, w * c + u * s, t[..., R:]), -1)
+
+    rq, rk, rv = (t.transpose(1, 2) for t in ref)
+    s = (turn(rq) @ turn(rk).transpose(-1, -2) * scale).masked_fill(~torch.from_numpy(M), -math.inf)
+    out = torch.softmax(s, -1) @ rv
+    out.backward(dO.double())
+    # roundings of the rotated inputs, O, p, dS and the results, each 2^-8 of values
+    # up to the largest; fp32: C of them, n <= 150 terms deep
+    for name, got, want in [("O", O, out)] + list(zip(("dQ", "dK", "dV"), [t.grad for t in leaf],
+                                                     [t.grad for t in ref])):
+        assert got.dtype == dtype
+        tol = (6 * HALF[dtype] + 8 * C) * want.abs().max().item()
+        assert (got.detach().double().cpu() - want.detach()).abs().max().item() <= tol, name
+
+    with torch.no_grad():
+        assert torch.equal(sag.sparse_mhsa(a, q.contiguous(), k.contiguous(), v.contiguous(), scale),
+                           splat.sparse_mhsa_fwd(a, q.contiguous(), k.contiguous(), v.contiguous(), scale))
+    b, _ = make(splat, "window", {"w": 4}, L, grad=False)
+    with pytest.raises(ValueError, match="grad=True"):
+        sag.sparse_mhsa(b, q.contiguous(), k.contiguous(), v.contiguous(), scale)
+
+
+def test_another_stream(gpu_lib):
+    """Everything runs on the current stream: work queued behind a long kernel on
+    a side stream, and read there."""
+    splat = gpu_lib
+    a, M = make(splat, "window", {"w": 30}, 400)
+    Q, K, V, dO = inputs(400, 64, 4, torch.bfloat16, 3)
+    side = torch.cuda.Stream()
+    dev = [torch.zeros(x.shape, dtype=x.dtype, device="cuda") for x in (Q, K, V, dO)]
+    host = [x.cuda() for x in (Q, K, V, dO)]
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(20_000_000)
+        for x, y in zip(dev, host):
+            x.copy_(y)
+        O, lse = splat.sparse_mhsa_fwd_lse(a, *dev[:3], 0.125)
+        got = splat.sparse_mhsa_bwd(a, *dev[:3], O, lse, dev[3], 0.125)
+    side.synchronize()
+    eO, el = splat.sparse_mhsa_fwd_lse(a, *host[:3], 0.125)
+    eager = splat.sparse_mhsa_bwd(a, *host[:3], eO, el, host[3], 0.125)
+    torch.cuda.synchronize()
+    assert torch.equal(O, eO) and all(torch.equal(x, y) for x, y in zip(got, eager))

@@ -113,3 +113,31 @@ def test_refusals():
     assert lib.splat_acsr_from_mask_ex(8, at, 8, None) == 1
     with pytest.raises(ValueError):
         splat.Acsr(mask=m, columns=True, grad=True)
+
+
+def test_with_other_flags():
+    """The transposed plan does not depend on the plan's other options."""
+    pat = splat.Pattern.window(300, 20)
+    ref = splat.Acsr(pat, grad=True).export_grad_plan()
+    for kw in (dict(columns=True), dict(span=False), dict(columns=True, span=False)):
+        got = splat.Acsr(pat, grad=True, **kw).export_grad_plan()
+        assert all(np.array_equal(x, y) for x, y in zip(ref, got))
+
+
+def test_sanitized(tmp_path):
+    """The planner built with the address and undefined-behaviour sanitizers, with
+    the transposed plan asked for, over the cases above and random masks."""
+    import test_host_sanitized as sanitized
+    import os
+    import shutil
+    import subprocess
+    cxx = shutil.which(os.environ.get("CXX", "g++"))
+    exe = str(tmp_path / "host_check")
+    r = subprocess.run([cxx, "-std=c++17", "-O1", "-g", "-fno-omit-frame-pointer",
+                        "-fsanitize=address,undefined", "-fno-sanitize-recover=all",
+                        "-I" + os.path.join(sanitized.ROOT, "include"), *sanitized.SRC, "-o", exe],
+                       capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr
+    pats = [splat.Pattern.named(k, p, L) for k, p, L in CASES] + [splat.Pattern.from_terms(100, [])]
+    out = sanitized.run(exe, [sanitized.desc_line(p, splat.PLAN_GRAD) for p in pats])
+    assert all(x["status"] == 0 for x in out)
