@@ -563,8 +563,10 @@ splat_status splat_cache_append(splat_rotary_t r, splat_dtype dtype, int32_t B, 
  * Q, O: [B, H, 1, d] contiguous, of `dtype`.  H is a multiple of the cache's heads:
  * query head h reads head h / (H / heads).  Length 0, or a row without columns:
  * O = 0.  A length outside [0, L] or past the table, or a page outside
- * [0, n_pages) among the row's keys: NaN in that sequence's O.  fp32 arithmetic,
- * one rounding, a fixed order of sums.  O shares no memory with the inputs.
+ * [0, n_pages) among the row's keys: NaN in that sequence's O.  An infinity in V of
+ * one of the row's keys gives an infinity or a NaN; what other keys hold does not
+ * matter.  fp32 arithmetic, one rounding, a fixed order of sums.  O shares no memory
+ * with the inputs.
  * workspace: splat_decode_workspace() bytes, 16-byte aligned, that the call writes
  * and reads (calls that may run at the same time need one each); NULL if 0.
  */

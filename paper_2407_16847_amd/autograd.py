@@ -8,7 +8,9 @@
 The gradients are the library's backward calls and can be taken once (not
 differentiated again).  To capture a training step into a graph, capture
 sparse_mhsa_fwd_lse, sparse_mhsa_bwd and rotary themselves: they allocate
-nothing when given their outputs.
+nothing when given their outputs.  A backward pass of these functions refuses
+to be captured: torch would run the leaves' accumulation on the stream of any
+eager graph of the same leaves that still lives, outside the capture.
 """
 from __future__ import annotations
 
@@ -24,6 +26,12 @@ from . import sparse_mhsa_bwd, sparse_mhsa_fwd, sparse_mhsa_fwd_lse
 __all__ = ["sparse_mhsa", "rotary"]
 
 
+def _not_captured() -> None:
+    if torch.cuda.is_available() and torch.cuda.is_current_stream_capturing():
+        raise RuntimeError("the backward pass of autograd functions is not captured into a graph; "
+                           "capture sparse_mhsa_bwd and rotary(inverse=True) instead")
+
+
 class _SparseMHSA(torch.autograd.Function):
     @staticmethod
     def forward(ctx, acsr, Q, K, V, scale):
@@ -35,6 +43,7 @@ class _SparseMHSA(torch.autograd.Function):
     @staticmethod
     @once_differentiable
     def backward(ctx, dO):
+        _not_captured()
         Q, K, V, O, lse = ctx.saved_tensors
         dQ, dK, dV = sparse_mhsa_bwd(ctx.acsr, Q, K, V, O, lse, dO.contiguous(), ctx.scale)
         return None, dQ, dK, dV, None
@@ -43,13 +52,16 @@ class _SparseMHSA(torch.autograd.Function):
 class _Rotary(torch.autograd.Function):
     @staticmethod
     def forward(ctx, rot, X, positions):
-        ctx.rot, ctx.positions = rot, positions
+        ctx.rot = rot
+        ctx.save_for_backward(positions)
         return _rotary(rot, X, positions=positions)
 
     @staticmethod
     @once_differentiable
     def backward(ctx, dY):
-        return None, _rotary(ctx.rot, dY.contiguous(), positions=ctx.positions, inverse=True), None
+        _not_captured()
+        positions, = ctx.saved_tensors
+        return None, _rotary(ctx.rot, dY.contiguous(), positions=positions, inverse=True), None
 
 
 def sparse_mhsa(acsr: Acsr, Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor,

@@ -356,9 +356,10 @@ struct View {
   const char* name;
   int32_t B, T, d, e;
   const char* at() const { return (const char*)x->data; }
-  // bytes from the first place of a token (of the tensor) to past its last
+  // bytes from the first place of a token (a sequence, the tensor) to past its last
   int64_t token() const { return ((x->heads - 1) * x->stride_h + d) * e; }
-  int64_t extent() const { return token() + ((B - 1) * x->stride_b + (T - 1) * x->stride_t) * e; }
+  int64_t sequence() const { return token() + (T - 1) * x->stride_t * e; }
+  int64_t extent() const { return sequence() + (B - 1) * x->stride_b * e; }
   bool same(const View& o) const {
     return x->data == o.x->data && x->heads == o.x->heads && x->stride_b == o.x->stride_b &&
            x->stride_h == o.x->stride_h && x->stride_t == o.x->stride_t;
@@ -395,17 +396,24 @@ splat_status check_view(const View& v, bool output) {
   return SPLAT_OK;
 }
 
-// Whether two views share no memory; views of one buffer that take turns, as Q, K
-// and V of a joint projection, are told apart by their tokens' places.
+// Whether two views of equal B and T share no memory; views of one buffer that take
+// turns, as Q, K and V of a joint projection, are told apart by the places of their
+// sequences, or of their tokens.
 bool apart(const View& a, const View& b) {
   if (!meet(a.at(), a.extent(), b.at(), b.extent())) return true;
-  const int64_t st = a.x->stride_t * a.e;
-  if (a.T == 1 || b.T == 1 || b.x->stride_t * b.e != st || a.token() > st || b.token() > st)
-    return false;
+  // blocks of na and nb bytes every st bytes
+  auto turns = [&](int64_t st, int64_t na, int64_t nb) {
+    if (st < 1 || na > st || nb > st) return false;
+    const int64_t off = ((b.at() - a.at()) % st + st) % st;
+    return off >= na && off + nb <= st;
+  };
+  const int64_t sb = a.x->stride_b * a.e, st = a.x->stride_t * a.e;
+  const bool even = a.B == 1 || b.x->stride_b * b.e == sb;
+  if (a.B > 1 && even && turns(sb, a.sequence(), b.sequence())) return true;
+  if (a.T == 1 || b.x->stride_t * b.e != st) return false;
   for (const View* v : {&a, &b})
-    if (v->B > 1 && (v->x->stride_b * v->e) % st != 0) return false;
-  const int64_t off = ((b.at() - a.at()) % st + st) % st;
-  return off >= a.token() && off + b.token() <= st;
+    if (v->B > 1 && (st < 1 || (v->x->stride_b * v->e) % st != 0)) return false;
+  return turns(st, a.token(), b.token());
 }
 
 splat_status check_apart(const View& out, const View& in) {

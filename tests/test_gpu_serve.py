@@ -430,3 +430,41 @@ def test_refusals(gpu_lib):
         if isinstance(e.value, splat.SplatError):
             assert e.value.name in ("INVALID_ARG", "UNSUPPORTED"), (i, e.value)
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("B,T", [(3, 1), (3, 5), (1, 5)])
+@pytest.mark.parametrize("order", ["b t h", "b h t"])
+def test_joint_projection_in_place(gpu_lib, B, T, order):
+    """Q, K and V as views of one buffer, Q and K turned where they are: views that
+    take turns share no memory, whatever the batch and the order of axes."""
+    splat = gpu_lib
+    H, H2, d, page = 4, 2, 64, 16
+    rot = splat.Rotary(64, d)
+    n = H + 2 * H2
+
+    def views(x):
+        x = x if order == "b h t" else x.transpose(1, 2)
+        return x[:, :H], x[:, H:H + H2], x[:, H + H2:]
+
+    x = torch.randn((B, n, T, d) if order == "b h t" else (B, T, n, d), device="cuda")
+    q, k, v = views(x)
+    kc, vc = (torch.zeros((B, H2, page, d), device="cuda") for _ in range(2))
+    table = torch.arange(B, dtype=torch.int32, device="cuda")[:, None].contiguous()
+    start = torch.arange(B, dtype=torch.int32, device="cuda")
+    wq = splat.cache_append(kc, vc, table, start, k, v, rot=rot, Q=q)
+    wk, wv = kc.clone(), vc.clone()
+    y = x.clone()
+    q, k, v = views(y)
+    kc.zero_(), vc.zero_()
+    splat.cache_append(kc, vc, table, start, k, v, rot=rot, Q=q, Qr=q)
+    assert torch.equal(q, wq) and torch.equal(kc, wk) and torch.equal(vc, wv)
+    assert torch.equal(k, views(x)[1]) and torch.equal(v, views(x)[2])
+    # both turned in place, in one launch
+    want = splat.rotary(rot, *views(x)[:2])
+    y = x.clone()
+    splat.rotary(rot, *views(y)[:2], Y=views(y)[0], Y2=views(y)[1])
+    assert torch.equal(views(y)[0], want[0]) and torch.equal(views(y)[1], want[1])
+    # shifted by a head they do share memory
+    with pytest.raises(splat.SplatError):
+        splat.rotary(rot, y[:, :H] if order == "b h t" else y.transpose(1, 2)[:, :H],
+                     Y=y[:, 1:H + 1] if order == "b h t" else y.transpose(1, 2)[:, 1:H + 1])

@@ -90,3 +90,23 @@ def test_cache_addresses(tmp_path):
     env.pop("LD_PRELOAD", None)
     r = subprocess.run([exe], capture_output=True, text=True, env=env, timeout=120)
     assert r.returncode == 0 and r.stdout.strip() == "ok", (r.returncode, r.stderr[-2000:])
+
+
+def test_backward_passes_are_not_captured(monkeypatch):
+    """A backward pass under capture is refused before anything is launched, and
+    positions that change between the passes are noticed."""
+    from paper_2407_16847_amd import autograd as sag
+    x = torch.zeros(1, 1, 1, 64, requires_grad=True)
+    monkeypatch.setattr(sag, "_rotary", lambda rot, X, positions=None, inverse=False: X * 1.0)
+    y = sag.rotary(None, x, torch.zeros(1, 1, dtype=torch.int32))
+    monkeypatch.setattr(torch.cuda, "is_available", lambda: True)
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: True)
+    with pytest.raises(RuntimeError, match="not captured"):
+        y.sum().backward()
+    monkeypatch.undo()
+    monkeypatch.setattr(sag, "_rotary", lambda rot, X, positions=None, inverse=False: X * 1.0)
+    at = torch.zeros(1, 1, dtype=torch.int32)
+    y = sag.rotary(None, x, at)
+    at += 1
+    with pytest.raises(RuntimeError, match="modified"):
+        y.sum().backward()
