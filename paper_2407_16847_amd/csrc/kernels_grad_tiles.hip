@@ -17,7 +17,15 @@
 // through a two-slot LDS ring, the next tile's loads issued while this one is
 // computed.  A launch's longest groups (global rows and columns) may instead go to
 // four workgroups each, of 32 rows, whose wavefronts share out the tiles' halves:
-// about twice the time a tile, but the chain of a group's tiles is a fifth as long.
+// 1.2 to 1.6 times the work a tile, but the chain of a group's tiles takes less than
+// half as long (grad_long_groups, below).
+//
+// Measured, dQ and dK, dV, us: window 512 + 64 global, L = 4096, d = 64, 64 heads
+// 132, 183 (817 and 786 TFLOP/s of their 6 d and 8 d flops a non-zero; a product of
+// 8192^3 reaches 1187); dilated 2, L = 4096, d = 128, 16 heads 41, 48 (590, 672);
+// strided+local 128, L = 2048, 24 heads 16, 25, the longest group's chain.  Bound by
+// the matrix cores and the vector ALUs in turn: an exponential, a product and two
+// conversions an element beside 12 to 16 matrix instructions for 32 x 32 of them.
 #include <hip/hip_runtime.h>
 #include <math.h>
 
@@ -199,7 +207,8 @@ __device__ __forceinline__ void q_rows(const Reads<D>& l, unsigned k_at, unsigne
 }
 
 // 32 staged query rows for a key: dK and dV.  stat: LDS address of the rows' lse2;
-// `apart` bytes on, their -delta.  v: the key's V, from registers or Parked.  lone: the rows that have a single key.
+// `apart` bytes on, their -delta.  v: the key's V, from registers or Parked.  lone:
+// the rows that have a single key.
 template <int D, typename X>
 __device__ __forceinline__ void kv_rows(const Reads<D>& l, unsigned q_at, unsigned g_at,
                                         unsigned stat, int apart, int h, const bf16x8_t (&k)[D / 16],
@@ -610,7 +619,8 @@ __global__ __launch_bounds__(kThreads, 2) void k_grad_kv_tiles(
         const unsigned stat = lds_addr(slot) + 2 * G::TB + kBM * 8;
 #pragma unroll
         for (int e = 0; e < 2; ++e)
-          kv_rows<D>(at, e * G::UB, G::TB + e * G::UB, stat + e * 128, kBN * 4, x.h, k, v_of(), sl2, state == kWavePartial, (unsigned)(bits >> (32 * e)),
+          kv_rows<D>(at, e * G::UB, G::TB + e * G::UB, stat + e * 128, kBN * 4, x.h, k, v_of(),
+                     sl2, state == kWavePartial, (unsigned)(bits >> (32 * e)),
                      (unsigned)tl.pad[e], ak, av);
       });
     }
