@@ -23,9 +23,13 @@
 // Measured, dQ and dK, dV, us: window 512 + 64 global, L = 4096, d = 64, 64 heads
 // 132, 183 (817 and 786 TFLOP/s of their 6 d and 8 d flops a non-zero; a product of
 // 8192^3 reaches 1187); dilated 2, L = 4096, d = 128, 16 heads 41, 48 (590, 672);
-// strided+local 128, L = 2048, 24 heads 16, 25, the longest group's chain.  Bound by
-// the matrix cores and the vector ALUs in turn: an exponential, a product and two
-// conversions an element beside 12 to 16 matrix instructions for 32 x 32 of them.
+// strided+local 128, L = 2048, 24 heads 16, 25, the longest group's chain.  For 32 x
+// 32 elements a SIMD has 12 (16) matrix instructions, 384 (512) cycles; 16
+// exponentials, multiply-adds and products and 8 (16) conversions, 416 (448) cycles;
+// and a quarter of the CU's LDS reads, 12 (16) KB a wavefront, 384 (512) cycles.
+// Matrix cores and vector ALUs take turns rather than run side by side.  (A third
+// wavefront a SIMD for dK, dV: 28 registers spilled, or 16 and more LDS reads with V
+// in LDS.)
 #include <hip/hip_runtime.h>
 #include <math.h>
 
