@@ -26,10 +26,12 @@
 // strided+local 128, L = 2048, 24 heads 16, 25, the longest group's chain.  For 32 x
 // 32 elements a SIMD has 12 (16) matrix instructions, 384 (512) cycles; 16
 // exponentials, multiply-adds and products and 8 (16) conversions, 416 (448) cycles;
-// and a quarter of the CU's LDS reads, 12 (16) KB a wavefront, 384 (512) cycles.
-// Matrix cores and vector ALUs take turns rather than run side by side.  (A third
-// wavefront a SIMD for dK, dV: 28 registers spilled, or 16 and more LDS reads with V
-// in LDS.)
+// and a quarter of the CU's LDS reads, 12 (24) KB a wavefront, 384 (768) cycles.
+// These take turns rather than run side by side, and what was tried to change that
+// did not: both halves of a tile interleaved (dK, dV 193 to 223), a third wavefront a
+// SIMD for dK, dV (28 registers spilled, or 16 with V in LDS), the statistics
+// spread by the matrix cores instead of read from LDS (202 for 210, 189 for 186 of
+// window 512 alone), transposed reads that do not wait for the next tile (210 for 199).
 #include <hip/hip_runtime.h>
 #include <math.h>
 
