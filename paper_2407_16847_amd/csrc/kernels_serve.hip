@@ -181,7 +181,7 @@ __device__ __forceinline__ int row_keys(const RowRuns* runs, int L, int len, int
 
 template <typename T, int D>
 __global__ __launch_bounds__(kThreads) void k_decode(
-    const RowRuns* __restrict__ runs, int L, int B, int H, int heads, int chunks,
+    const RowRuns* __restrict__ runs, int L, int H, int heads, int chunks,
     const T* __restrict__ Q, const T* __restrict__ K, const T* __restrict__ V,
     const int32_t* __restrict__ pages, const int32_t* __restrict__ lengths, int max_pages,
     int n_pages, int page_shift, float sl2, T* __restrict__ O, float* __restrict__ ws) {
@@ -371,7 +371,7 @@ hipError_t decode_launch(const DevAcsr& a, const DecodeArgs& x, hipStream_t st) 
   const int splits = decode_splits(a, x.B, x.H, x.heads), chunks = head_chunks(x.H, x.heads);
   const float sl2 = (float)((double)x.scale * 1.4426950408889634074);
   hipLaunchKernelGGL((k_decode<T, D>), dim3(splits, x.B * x.heads * chunks), dim3(kThreads),
-                     (kDecodeLds<T, D>), st, a.runs, a.L, x.B, x.H, x.heads, chunks, (const T*)x.Q,
+                     (kDecodeLds<T, D>), st, a.runs, a.L, x.H, x.heads, chunks, (const T*)x.Q,
                      (const T*)x.K, (const T*)x.V, x.pages, x.lengths, x.max_pages, x.n_pages,
                      x.page_shift, sl2, (T*)x.O, x.ws);
   hipError_t e = hipGetLastError();
