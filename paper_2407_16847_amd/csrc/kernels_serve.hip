@@ -22,8 +22,8 @@ constexpr int kThreads = 256;
 // (nothing is read back here).  Rotation of Q and K, 4096 tokens, 16 + 16 heads of d =
 // 64 in bf16, 4 sequences: 26.8 us, 5.05 TB/s, what a copy of 1 GiB reaches;
 // ordinary stores 29.9, with nontemporal loads besides 33.1.  1000 tokens into the
-// cache, d = 128, 8 sequences: 34.0 us, 4.6 TB/s; ordinary stores 39.6; four heads
-// in flight and at most 8 a thread 34.7 .. 36.6.
+// cache, d = 128, 8 sequences: 34.0 .. 35.7 us, 4.4 .. 4.6 TB/s; ordinary stores
+// 39.6; four heads in flight and at most 8 a thread 34.7 .. 36.6.
 constexpr int kInFlight = 2;
 constexpr int kMaxHeads = 16;
 

@@ -439,3 +439,28 @@ def test_another_stream(gpu_lib):
     eager = splat.sparse_mhsa_bwd(a, *host[:3], eO, el, host[3], 0.125)
     torch.cuda.synchronize()
     assert torch.equal(O, eO) and all(torch.equal(x, y) for x, y in zip(got, eager))
+
+
+def test_two_streams_at_once(gpu_lib):
+    """One handle's calls on two streams, neither waiting for the other: the
+    workspaces are the calls' own."""
+    splat = gpu_lib
+    a, M = make(splat, "window_global", {"w": 60, "n_global": 20}, 1500)
+    sides = [torch.cuda.Stream() for _ in range(2)]
+    x = [[t.cuda() for t in inputs(1500, 64, 6, torch.bfloat16, 7 + k)] for k in range(2)]
+
+    def step(q, k, v, do):
+        O, lse = splat.sparse_mhsa_fwd_lse(a, q, k, v, 0.125)
+        return (O, *splat.sparse_mhsa_bwd(a, q, k, v, O, lse, do, 0.125))
+
+    want = [step(*t) for t in x]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(10):
+        for k, side in enumerate(sides):
+            with torch.cuda.stream(side):
+                got[k].append(step(*x[k]))
+    torch.cuda.synchronize()
+    for k in range(2):
+        for r in got[k]:
+            assert all(torch.equal(u, v) for u, v in zip(r, want[k]))

@@ -468,3 +468,22 @@ def test_joint_projection_in_place(gpu_lib, B, T, order):
     with pytest.raises(splat.SplatError):
         splat.rotary(rot, y[:, :H] if order == "b h t" else y.transpose(1, 2)[:, :H],
                      Y=y[:, 1:H + 1] if order == "b h t" else y.transpose(1, 2)[:, 1:H + 1])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_decode_of_shared_pages(gpu_lib, dtype):
+    """Sequences that share pages (a common beginning), and a page that a table
+    names twice."""
+    splat = gpu_lib
+    a, M = make(splat, "full", {}, 200, grad=False)
+    kc, vc, _ = paged([200], 16, 13, 2, 64, dtype, 3, spare=13)
+    assert kc.shape[0] == 26
+    table = torch.randperm(26, generator=torch.Generator().manual_seed(4)).to(torch.int32).view(2, 13)
+    table[1, :7] = table[0, :7]
+    table[0, 9] = table[0, 2]
+    Q = torch.randn((2, 6, 1, 64), generator=torch.Generator().manual_seed(5)).to(dtype)
+    O = splat.sparse_mhsa_decode(a, Q.cuda(), kc.cuda(), vc.cuda(), table.cuda(),
+                                 torch.tensor([200, 119], dtype=torch.int32).cuda(), 0.125)
+    torch.cuda.synchronize()
+    want, bound = decode64(Q, kc, vc, table, [200, 119], M, 0.125)
+    assert ((O.double().cpu() - want).abs() <= bound).all()
