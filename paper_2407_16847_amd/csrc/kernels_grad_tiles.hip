@@ -63,6 +63,9 @@ struct Geo {
   static constexpr int KV_RING = kHalves ? 2 * UNIT : LDS;
   static constexpr int KV_LDS = KV_RING + 4 * VB;
   static constexpr int KV_LONG = KV_LDS > LONG + VB ? KV_LDS : LONG + VB;
+  // four wavefronts' staged rows of a result (store_rows)
+  static constexpr int STAGE = 4 * 32 * (RB + 16);
+  static_assert(STAGE <= LDS && STAGE <= KV_LDS, "the staged results fit");
 };
 
 // Place of chunk c of row r: c ^ swz(r).  Row reads take one chunk of 16 rows at a
@@ -586,7 +589,10 @@ __global__ __launch_bounds__(kThreads, 2) void k_grad_kv_tiles(
   // the parked V lies behind the ring, or behind the units of all wavefronts
   const unsigned parked =
       lds_addr(lds) + (shared ? G::LONG : G::KV_RING + wave * G::VB) + 16 * x.lane;
-  if (G::kHalves && (!shared || wave == 0))
+  // (Not for a group without tiles: store_rows stages all wavefronts' rows from the
+  // start of LDS, past the ring, and only a ring's end has a barrier before that.)
+  const int nt = grp.tile_end - grp.tile_begin;
+  if (G::kHalves && nt > 0 && (!shared || wave == 0))
 #pragma unroll
     for (int ks = 0; ks < D / 16; ++ks)
       *(__attribute__((address_space(3))) bf16x8_t*)(uintptr_t)(parked + 1024 * ks) = v[ks];
@@ -598,7 +604,6 @@ __global__ __launch_bounds__(kThreads, 2) void k_grad_kv_tiles(
   f32x16_t ak[D / 32], av[D / 32];
   zero(ak), zero(av);
   const Tile* const mine = tiles + grp.tile_begin;
-  const int nt = grp.tile_end - grp.tile_begin;
 
   auto again_v = [&](int j, int r) {
     grad_kv_row<__bf16, D, false>(j, w * 32 + r, x.lane, mine, nt, masks, L, Qh, K + head, V + head,

@@ -1,0 +1,40 @@
+"""The backward pass of rows and keys at the mask's edge: keys that no row has,
+rows of few keys beside longer ones, values that are not finite at d = 128.
+
+Bounds as in test_gpu_grad.py.
+"""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from test_gpu_grad import TYPES, backward64, check, inputs, make
+
+pytestmark = pytest.mark.gpu
+
+# masks with whole groups of 128 keys that no row has
+NO_ROWS = [("none", {}, 300, 2), ("window_rows", {"w": 40, "lo": 200, "hi": 400}, 1024, 3),
+           ("window_rows", {"w": 3, "lo": 900, "hi": 1000}, 1024, 40)]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("kind,params,L,heads", NO_ROWS)
+def test_groups_of_keys_without_rows(gpu_lib, kind, params, L, heads, d, dtype):
+    """dK and dV of keys that no row has are 0, in groups of such keys alone too:
+    nothing that a workgroup keeps in LDS reaches them."""
+    splat = gpu_lib
+    print(f"[gpu] no rows {kind} {params} L={L} heads={heads} d={d} {dtype}", flush=True)
+    a, M = make(splat, kind, params, L)
+    Q, K, V, dO = inputs(L, d, heads, dtype, L + d)
+    dev, scale = [x.cuda() for x in (Q, K, V, dO)], 1.0 / math.sqrt(d)
+    O, lse = splat.sparse_mhsa_fwd_lse(a, *dev[:3], scale)
+    got = splat.sparse_mhsa_bwd(a, *dev[:3], O, lse, dev[3], scale)
+    torch.cuda.synchronize()
+    want, bound = backward64(Q, K, V, O.cpu(), lse.cpu(), dO, M, scale)
+    for name, g, w, b in zip(("dQ", "dK", "dV"), got, want, bound):
+        check(name, g, w, b)
+    rows, keys = torch.from_numpy(~M.any(1)), torch.from_numpy(~M.any(0))
+    assert (got[0].cpu()[:, :, rows] == 0).all()
+    assert (got[1].cpu()[:, :, keys] == 0).all() and (got[2].cpu()[:, :, keys] == 0).all()
