@@ -158,8 +158,9 @@ splat_status splat_acsr_build(const splat_pattern_desc* desc, splat_acsr_t* out)
  *   still builds (columns = 0).  O(nnz) host time; UNSUPPORTED above 2^28
  *   non-zeros per head.
  * SPLAT_PLAN_GRAD -- also plans the transposed mask (groups of keys, tiles of
- *   query rows), which splat_sparse_mhsa_bwd works from.  Any mask; about as
- *   much host time and device memory again as the plan itself.
+ *   query rows), which splat_sparse_mhsa_bwd works from.  Any mask; mostly about
+ *   as much host time and device memory again as the plan itself: both grow with
+ *   the groups of up to 128 keys that the rows reach.
  *
  * Returns INVALID_ARG for unknown flag bits; otherwise as splat_acsr_build.
  */
@@ -459,7 +460,7 @@ splat_status splat_sparse_mhsa_fwd(splat_acsr_t h, splat_dtype dtype, int32_t B,
  * that may run at the same time need one each).  The gradients and the workspace
  * share no memory with the inputs or each other (INVALID_ARG).  The handle must
  * have been built with SPLAT_PLAN_GRAD (INVALID_ARG).  bf16: UNSUPPORTED where the
- * row or key groups times B*H exceed 2^22.
+ * row or key groups times B*H reach 2^24, as for the forward.
  */
 splat_status splat_sparse_mhsa_fwd_lse(splat_acsr_t h, splat_dtype dtype, int32_t B, int32_t H,
                                        int32_t d, const void* Q, const void* K, const void* V,

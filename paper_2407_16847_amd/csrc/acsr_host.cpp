@@ -445,6 +445,8 @@ void transpose64(uint64_t (&x)[64]) {
     }
 }
 
+constexpr int64_t kGroupTiles = 1;
+
 // A group's keys as arithmetic progressions, none of them across the group's
 // key 64: a row's membership in each is O(1) per run.
 struct KeyPiece {
@@ -463,6 +465,27 @@ std::vector<KeyPiece> key_pieces(const int32_t* keys, int32_t n) {
   return out;
 }
 
+// Every row of several keys is one run of stride `step`: whether groups of keys
+// of one residue take less than groups of kBM keys in a row.  Either way a group
+// has about as many tiles as it has query rows / kBN, at least one; a group itself
+// (its operands and results) counts as kGroupTiles.  Window of 1 at steps of 8000,
+// L = 65536, 8 heads, bf16, forward and backward: 8000 groups of 8 keys 1471 us, 512
+// of 128 keys 995 us.
+bool residues_pay(const HostAcsr& a, int32_t step) {
+  int64_t runs = 0, rows = 0;            // (row, group) pairs: keys in a row, by residue
+  for (int32_t i = 0; i < a.L; ++i) {
+    const int32_t n = a.row_ptr[i + 1] - a.row_ptr[i];
+    if (n == 0) continue;
+    runs += std::min<int64_t>(n, int64_t(step) * (n - 1) / kBM + 1);
+    rows += (n - 1) / kBM + 1;
+  }
+  int64_t groups = 0;                    // of keys j, j + step, ..
+  for (int32_t j = 0; j < std::min(step, a.L); ++j) groups += (a.L - 1 - j) / step / kBM + 1;
+  const int64_t all = (a.L + kBM - 1) / kBM;
+  return std::max(groups, rows / kBN) + kGroupTiles * groups <=
+         std::max(all, runs / kBN) + kGroupTiles * all;
+}
+
 }  // namespace
 
 void plan_grad(HostAcsr& a) {
@@ -470,9 +493,10 @@ void plan_grad(HostAcsr& a) {
   GradPlan& g = a.grad;
   g = GradPlan();
   // 1. Group the keys.  Where every row of several keys is one run of the same
-  //    stride s > 1, keys of one residue mod s share their rows.  Otherwise the
-  //    keys that many more rows have than the others (global columns) form
-  //    groups of their own, so that their rows cost the others nothing.
+  //    stride s > 1, keys of one residue mod s share their rows: they are grouped
+  //    by residue where that takes less.  Otherwise the keys that many more rows
+  //    have than the others (global columns) form groups of their own, so that
+  //    their rows cost the others nothing.
   int32_t step = 0;   // 0: no row of several keys yet, 1: no common stride
   std::vector<int32_t> diff(L + 1, 0), count(L, 0);
   for (int32_t i = 0; i < L; ++i) {
@@ -491,16 +515,64 @@ void plan_grad(HostAcsr& a) {
     }
   }
   for (int32_t j = 0, n = 0; j < L; ++j) n += diff[j], count[j] += n;
-  std::map<int32_t, std::vector<int32_t>> classes;
-  if (step > 1) {
+  const bool residues = step > 1 && residues_pay(a, step);
+  std::vector<std::vector<int32_t>> classes(residues ? std::min(step, L) : 2);
+  std::vector<int32_t> below(L + 1, 0);   // keys below j that are in class 0 of two
+  if (residues) {
     for (int32_t j = 0; j < L; ++j) classes[j % step].push_back(j);
   } else {
     std::vector<int32_t> sorted(count);
     std::nth_element(sorted.begin(), sorted.begin() + L / 2, sorted.end());
     const int32_t many = 2 * sorted[L / 2] + kBM;
-    for (int32_t j = 0; j < L; ++j) classes[count[j] > many ? 0 : 1].push_back(j);
+    for (int32_t j = 0; j < L; ++j) {
+      const bool global = count[j] > many;
+      classes[global ? 0 : 1].push_back(j);
+      below[j + 1] = below[j] + global;
+    }
   }
-  // 2. Cut each group's query rows into tiles.
+  // 2. The rows of each group's keys, so that a group costs what it has and not a
+  //    pass over all rows.
+  std::vector<int32_t> base(classes.size()), group_of(L);   // base: a class's first group
+  int32_t n_groups = 0;
+  for (size_t c = 0; c < classes.size(); ++c) {
+    base[c] = n_groups;
+    for (size_t k = 0; k < classes[c].size(); ++k) group_of[classes[c][k]] = n_groups + (int32_t)(k / kBM);
+    n_groups += (int32_t)((classes[c].size() + kBM - 1) / kBM);
+  }
+  std::vector<int32_t> seen(n_groups);
+  auto visit = [&](auto&& f) {             // f(row, group), a row's groups once each
+    std::fill(seen.begin(), seen.end(), -1);
+    for (int32_t i = 0; i < L; ++i) {
+      auto one = [&](int32_t x) {
+        if (seen[x] != i) seen[x] = i, f(i, x);
+      };
+      auto span = [&](int32_t c, int32_t lo, int32_t hi) {   // the class's keys lo .. hi - 1
+        for (int32_t x = lo / kBM; lo < hi && x <= (hi - 1) / kBM; ++x) one(base[c] + x);
+      };
+      for (int r = 0; r < SPLAT_MAX_RUNS; ++r) {
+        const Run& q = a.runs[i].r[r];
+        if (q.count <= 0) continue;
+        if (residues) {
+          span(q.start % step, q.start / step, q.start / step + q.count);
+        } else if (q.stride == 1) {
+          const int32_t end = q.start + q.count;
+          span(0, below[q.start], below[end]);
+          span(1, q.start - below[q.start], end - below[end]);
+        } else {
+          for (int32_t k = 0; k < q.count; ++k) one(group_of[q.start + q.stride * k]);
+        }
+      }
+    }
+  };
+  std::vector<int64_t> at(n_groups + 1, 0);
+  visit([&](int32_t, int32_t x) { ++at[x + 1]; });
+  for (int32_t x = 0; x < n_groups; ++x) at[x + 1] += at[x];
+  std::vector<int32_t> group_rows(at[n_groups]);
+  {
+    std::vector<int64_t> next(at.begin(), at.end() - 1);
+    visit([&](int32_t i, int32_t x) { group_rows[next[x]++] = i; });
+  }
+  // 3. Cut each group's query rows into tiles.
   struct Pending {
     Group g;
     std::vector<Tile> t;
@@ -511,24 +583,25 @@ void plan_grad(HostAcsr& a) {
     if (a.row_ptr[i + 1] - a.row_ptr[i] == 1) one.set(i);
   std::vector<uint64_t> in(2 * (size_t)L, 0ull);   // each row's keys of the group
   auto any_step = [](int32_t) { return true; };    // masks are not evaluated on the device
-  for (auto& kv : classes) {
-    const std::vector<int32_t>& keys = kv.second;
+  for (size_t c = 0; c < classes.size(); ++c) {
+    const std::vector<int32_t>& keys = classes[c];
     for (size_t off = 0; off < keys.size(); off += kBM) {
       const int32_t nk = (int32_t)std::min<size_t>(kBM, keys.size() - off);
+      const int32_t x = base[c] + (int32_t)(off / kBM);
       Pending p;
       p.g = Group{(int32_t)g.rows.size(), nk, 0, 0};
       g.rows.insert(g.rows.end(), keys.begin() + off, keys.begin() + off + nk);
       const std::vector<KeyPiece> pieces = key_pieces(keys.data() + off, nk);
-      U.clear();
-      for (int32_t i = 0; i < L; ++i) {
+      for (int64_t k = at[x]; k < at[x + 1]; ++k) {
+        const int32_t i = group_rows[k];
         uint64_t w[2] = {0, 0};
         for (int r = 0; r < SPLAT_MAX_RUNS; ++r) {
           const Run& q = a.runs[i].r[r];
           if (q.count <= 0 || q.start > keys[off + nk - 1] ||
               q.start + q.stride * (q.count - 1) < keys[off])
             continue;
-          for (const KeyPiece& k : pieces)
-            w[k.at >> 6] |= run_tile_bits(q, k.kb, k.ks, k.n) << (k.at & 63);
+          for (const KeyPiece& y : pieces)
+            w[y.at >> 6] |= run_tile_bits(q, y.kb, y.ks, y.n) << (y.at & 63);
         }
         in[2 * (size_t)i] = w[0], in[2 * (size_t)i + 1] = w[1];
         if (w[0] | w[1]) U.set(i);
@@ -569,9 +642,13 @@ void plan_grad(HostAcsr& a) {
         p.t.push_back(t);
       }
       pend.push_back(std::move(p));
+      for (int64_t k = at[x]; k < at[x + 1]; ++k) {   // empty for the next group
+        const int32_t i = group_rows[k];
+        in[2 * (size_t)i] = in[2 * (size_t)i + 1] = 0, U.w[i >> 6] = 0;
+      }
     }
   }
-  // 3. heaviest groups first
+  // 4. heaviest groups first
   std::stable_sort(pend.begin(), pend.end(),
                    [](const Pending& x, const Pending& y) { return x.t.size() > y.t.size(); });
   for (Pending& p : pend) {

@@ -887,9 +887,9 @@ splat_status splat_sparse_mhsa_bwd(splat_acsr_t h, splat_dtype dtype, int32_t B,
   const Span out[] = {{dQ, dense, "dQ"}, {dK, dense, "dK"}, {dV, dense, "dV"},
                       {workspace, rows * 8, "workspace"}};
   CHECK(check_spans(in, 6, out, 4));
-  if (dtype == SPLAT_BF16) {   // a group may take four workgroups
-    CHECK(check_grid(4 * h->dev.n_groups, "quarter row", B, H));
-    CHECK(check_grid(4 * h->dev.grad_groups, "quarter key", B, H));
+  if (dtype == SPLAT_BF16) {
+    CHECK(check_tile_grid(h, B, H));
+    CHECK(check_grid(h->dev.grad_groups, "key", B, H));
   }
   const splat::BwdArgs x{Q, K, V, O, dO, lse, workspace, dQ, dK, dV};
   return launched(splat::launch_bwd(h->dev, dtype, B * H, d, x, scale, (hipStream_t)stream),

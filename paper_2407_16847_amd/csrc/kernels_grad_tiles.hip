@@ -729,7 +729,9 @@ int grad_long_groups(const DevAcsr& a, bool kv, int BH, int d) {
     const double tiles = (double)runs[k].tiles * runs[k].groups;
     rest -= tiles, longs += tiles, groups += runs[k].groups;
   }
-  return take;
+  // the work-items of a launch stay below 2^32
+  const int64_t all = kv ? a.grad_groups : a.n_groups;
+  return (all + (kWavesPerGroup - 1) * (int64_t)take) * BH < (1 << 24) ? take : 0;
 }
 
 hipError_t bounds_collect_grad_tiles(uint32_t* bits, bool clear) { return dbg::collect(bits, clear); }

@@ -38,3 +38,24 @@ def test_groups_of_keys_without_rows(gpu_lib, kind, params, L, heads, d, dtype):
     rows, keys = torch.from_numpy(~M.any(1)), torch.from_numpy(~M.any(0))
     assert (got[0].cpu()[:, :, rows] == 0).all()
     assert (got[1].cpu()[:, :, keys] == 0).all() and (got[2].cpu()[:, :, keys] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("kind,params,L,heads", [
+    ("dilated", {"w": 3, "dilation": 100}, 300, 2), ("dilated", {"w": 2, "dilation": 130}, 700, 60),
+    ("dilated", {"w": 40, "dilation": 16}, 640, 2), ("strided_local", {"local": 7, "stride": 200}, 900, 2)])
+def test_large_strides(gpu_lib, kind, params, L, heads, d, dtype):
+    splat = gpu_lib
+    print(f"[gpu] strides {kind} {params} L={L} heads={heads} d={d} {dtype}", flush=True)
+    a, M = make(splat, kind, params, L)
+    x, scale = inputs(L, d, heads, dtype, L + d), 1.0 / math.sqrt(d)
+    dev = [t.cuda() for t in x]
+    O, lse = splat.sparse_mhsa_fwd_lse(a, *dev[:3], scale)
+    got = splat.sparse_mhsa_bwd(a, *dev[:3], O, lse, dev[3], scale)
+    torch.cuda.synchronize()
+    for h in (0, heads - 1):
+        one = [t[:, h:h + 1].cpu() for t in (*x[:3], O, lse, x[3])]
+        want, bound = backward64(*one, M, scale)
+        for name, g, w, b in zip(("dQ", "dK", "dV"), got, want, bound):
+            check(f"{name} head {h}", g[:, h:h + 1], w, b)
