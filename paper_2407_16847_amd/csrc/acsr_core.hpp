@@ -68,7 +68,9 @@ struct Group {
 struct Tile {
   int32_t kb, ks, nk, flags;
   int32_t mask_block;   // -1, or index of the tile's kBM per-row masks in the mask array
-  int32_t pad[3];       // pad[0] = 1: no row of the group has more than kFewKeys keys
+  // of a group's first tile: the range of its tiles, pad[0] the first and pad[1] how
+  // many, that rows of 2 .. kFewKeys keys have keys in
+  int32_t pad[3];
 };
 constexpr int kFewKeys = 32;
 

@@ -345,11 +345,12 @@ void plan_work(HostAcsr& a) {
       for (int32_t m = 0; m < nrows; ++m) a.rows.push_back(rows[off + m]);
       // union of the group's columns; strides present in the group
       U.clear();
-      int32_t few = 1;
+      bool few[kBM] = {};                  // rows of few keys
       for (int32_t m = 0; m < nrows; ++m) {
-        const int32_t i = rows[off + m];
-        if (a.row_ptr[i + 1] - a.row_ptr[i] > kFewKeys) few = 0;
+        const int32_t i = rows[off + m], n = a.row_ptr[i + 1] - a.row_ptr[i];
+        few[m] = n > 1 && n <= kFewKeys;
       }
+      int32_t few_first = -1, few_last = -1;   // tiles that they have keys in
       std::vector<int32_t> strides;
       for (int32_t m = 0; m < nrows; ++m) {
         const RowRuns& rr = a.runs[rows[off + m]];
@@ -382,7 +383,6 @@ void plan_work(HostAcsr& a) {
           pos = cut_tile(U, c, gather_ok, t) + 1;
         }
         t.mask_block = -1;
-        t.pad[0] = few;
         // per-row membership, per-wavefront state
         uint64_t rb[kBM];
         const uint64_t all = t.nk == 64 ? ~0ull : ((1ull << t.nk) - 1);
@@ -390,6 +390,11 @@ void plan_work(HostAcsr& a) {
         bool any_partial = false;
         for (int32_t m = 0; m < kBM; ++m)
           rb[m] = m < nrows ? tile_row_bits(a.runs[rows[off + m]], t.kb, t.ks, t.nk) : 0ull;
+        for (int32_t m = 0; m < kBM; ++m)
+          if (few[m] && rb[m]) {
+            few_last = (int32_t)p.t.size();
+            if (few_first < 0) few_first = few_last;
+          }
         for (int32_t w = 0; w < kWavesPerGroup; ++w) {
           bool full = t.nk == kBN, empty = true;
           for (int32_t m = w * kWaveRows; m < (w + 1) * kWaveRows && m < nrows; ++m) {
@@ -413,6 +418,7 @@ void plan_work(HostAcsr& a) {
         p.t.push_back(t);
         if (pos >= L) break;
       }
+      if (few_first >= 0) p.t[0].pad[0] = few_first, p.t[0].pad[1] = few_last - few_first + 1;
       pend.push_back(std::move(p));
     }
   }

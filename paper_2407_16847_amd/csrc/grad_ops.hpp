@@ -43,9 +43,10 @@ struct RowStat {
 
 // -delta from a bf16 O carries O's rounding, an error e that is the same for all
 // of a row's dS_ij = p_ij (dP_ij - delta): next to dS it is about 2^-9.3 / sqrt(n)
-// for weight spread over n keys.  Rows of few keys (kFewKeys; Tile::pad[0] marks
-// the tiles of a group that has no other rows) therefore sum their dS first, which
-// with the exact delta is 0, take that from delta and start again.
+// for weight spread over n keys (and more where few of them have the weight).  Rows
+// of 2 .. kFewKeys keys therefore sum their dS first, over the tiles of their group
+// that such rows have keys in (Tile::pad), which with the exact delta is 0, and take
+// that from delta.
 // ---------------------------------------------------------- one row, VALU
 // Sums over the keys (or query rows) of one row by a wavefront, 64 of them at a
 // time, a lane each: weight(j) for lanes that have one, then features by lanes.

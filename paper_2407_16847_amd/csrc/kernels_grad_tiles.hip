@@ -499,7 +499,9 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void k_grad_q_tiles(
   zero(acc);
   const Tile* const mine = tiles + grp.tile_begin;
   const int nt = grp.tile_end - grp.tile_begin;
-  const bool few = nt > 0 && mine[0].pad[0];             // see grad_ops.hpp
+  // see grad_ops.hpp: the tiles of rows of few keys, and whether this lane's is one
+  const int few_first = nt > 0 ? mine[0].pad[0] : 0, few_tiles = nt > 0 ? mine[0].pad[1] : 0;
+  const bool few = keys > 1 && keys <= kFewKeys, any_few = __any(few && x.ok);
   const bool writes = x.h == 0 && x.ok && (!shared || wave == 0);
 
   auto again = [&](int i, int r) {
@@ -508,10 +510,11 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void k_grad_q_tiles(
                           dQ + head);
   };
   if (!shared) {
-    auto sweep = [&](auto add) {
+    auto sweep = [&](auto add, const Tile* from, int n) {
       float sum = 0.f;
-      for_tiles<D, false>(lds, mine, nt, Kh, Vh, masks, nullptr, nullptr, L, wave, x.lane,
+      for_tiles<D, false>(lds, from, n, Kh, Vh, masks, nullptr, nullptr, L, wave, x.lane,
                           [&](const char* slot, const Tile&, int state) {
+        if (!decltype(add)::value && !any_few) return;
         uint64_t bits = ~0ull;
         if (state == kWavePartial) bits = *(const uint64_t*)(slot + 2 * G::TB + x.place * 8);
         const Reads<D> at(lds_addr(slot), x);
@@ -523,9 +526,12 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void k_grad_q_tiles(
       });
       return sum + lane_xor32(sum);
     };
-    if (few) st.nd -= sweep(std::false_type());
+    if (few_tiles > 0) {
+      const float sum = sweep(std::false_type(), mine + few_first, few_tiles);
+      if (few) st.nd -= sum;
+    }
     if (writes) lse2[head_rows + x.row] = st.lse2, nd[head_rows + x.row] = st.nd;
-    if (nt > 0) sweep(std::true_type());
+    if (nt > 0) sweep(std::true_type(), mine, nt);
     uint64_t bad = store_rows<D>(lds + wave * 32 * (2 * D + 16), acc, scale, keys <= 1, x, grp.nrows,
                                  dQ + head);
     for (; bad; bad &= bad - 1) {
@@ -535,25 +541,26 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void k_grad_q_tiles(
     return;
   }
   Slice s;
-  s.lane = x.lane, s.wave = wave, s.qi = x.qi, s.h = x.h, s.w = w, s.nt = nt;
+  s.lane = x.lane, s.wave = wave, s.qi = x.qi, s.h = x.h, s.w = w;
   s.masks = (const uint32_t*)masks + 2 * x.place;
-  auto sweep = [&](auto add) {
+  auto sweep = [&](auto add, const Tile* from, int n) {
     float sum = 0.f;
-    for_units<D>(lds, mine, s, Kh, Vh, nullptr, L,
+    s.nt = n;
+    for_units<D>(lds, from, s, Kh, Vh, nullptr, L,
                  [&](unsigned at, const Unit& u, uint32_t bits, uint32_t) {
       q_rows<D, decltype(add)::value>(Reads<D>(at, x), 0, G::UB, x.h, q, go, st, sl2, !u.full, bits, acc, sum);
     });
     return sum + lane_xor32(sum);
   };
-  if (few) {
+  if (any_few) {   // the same in all four wavefronts: they have the same rows
     float* const part = (float*)(lds + G::LONG);
-    const float sum = sweep(std::false_type());
+    const float sum = sweep(std::false_type(), mine + few_first, few_tiles);
     if (x.h == 0) part[wave * 32 + x.qi] = sum;
     __syncthreads();
-    st.nd -= (part[x.qi] + part[32 + x.qi]) + (part[64 + x.qi] + part[96 + x.qi]);
+    if (few) st.nd -= (part[x.qi] + part[32 + x.qi]) + (part[64 + x.qi] + part[96 + x.qi]);
   }
   if (writes) lse2[head_rows + x.row] = st.lse2, nd[head_rows + x.row] = st.nd;
-  sweep(std::true_type());
+  sweep(std::true_type(), mine, nt);
   combine_rows<D, false>(lds, acc, x, scale, dQ + head,
                          [&](int i) { return row_ptr[i + 1] - row_ptr[i] > 1; }, again);
 }

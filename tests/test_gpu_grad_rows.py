@@ -59,3 +59,51 @@ def test_large_strides(gpu_lib, kind, params, L, heads, d, dtype):
         want, bound = backward64(*one, M, scale)
         for name, g, w, b in zip(("dQ", "dK", "dV"), got, want, bound):
             check(f"{name} head {h}", g[:, h:h + 1], w, b)
+
+
+def few(M):
+    """Rows whose delta is the sum of p dP itself, not dO.O with the rounded O."""
+    n = M.sum(-1)
+    return torch.from_numpy((n > 1) & (n <= 32))
+
+
+# rows of few keys beside longer ones: the first rows of causal masks, rows beside
+# global ones, one row alone, groups of one workgroup and of four
+BESIDE = [
+    ("strided_local", {"local": 128, "stride": 128}, 700, 2), ("strided_local", {"local": 128, "stride": 128}, 700, 130),
+    ("strided_local", {"local": 4, "stride": 16}, 900, 3), ("window_global", {"w": 8, "n_global": 8}, 900, 2),
+    ("window_global", {"w": 3, "n_global": 2}, 1300, 60), ("window", {"w": 20}, 400, 2),
+    ("window_rows", {"w": 40, "lo": 30, "hi": 31}, 300, 2), ("dilated", {"w": 20, "dilation": 3}, 500, 2),
+]
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("kind,params,L,heads", BESIDE)
+def test_rows_of_few_keys_beside_longer_ones(gpu_lib, kind, params, L, heads, d):
+    """bf16: the gradients of a row of 2 .. 32 keys do not depend on the rows that
+    share its group: dQ of every such row, and dK of the keys that only such rows
+    have, without the rounding of O in the bound."""
+    splat = gpu_lib
+    print(f"[gpu] few keys {kind} {params} L={L} heads={heads} d={d}", flush=True)
+    a, M = make(splat, kind, params, L)
+    x, scale = inputs(L, d, heads, torch.bfloat16, L + d), 1.0 / math.sqrt(d)
+    dev = [t.cuda() for t in x]
+    O, lse = splat.sparse_mhsa_fwd_lse(a, *dev[:3], scale)
+    got = splat.sparse_mhsa_bwd(a, *dev[:3], O, lse, dev[3], scale)
+    torch.cuda.synchronize()
+    rows = few(M)
+    for h in {0, heads - 1}:
+        one = [t[:, h:h + 1].cpu() for t in (*x[:3], O, lse, x[3])]
+        want, bound = backward64(*one, M, scale)
+        for name, g, w, b in zip(("dQ", "dK", "dV"), got, want, bound):
+            check(f"{name} head {h}", g[:, h:h + 1], w, b)
+        # the rows without the term: their part of the mask alone, whose rows all have
+        # at most 32 keys
+        Mf = M & rows.numpy()[:, None]
+        want, bound = backward64(*one, Mf, scale)
+        keys = torch.from_numpy(Mf.any(0) & ~(M & ~rows.numpy()[:, None]).any(0))
+        for k, name, part in ((0, "dQ of rows of few keys", rows), (1, "dK of their keys", keys)):
+            if part.any():
+                check(f"{name}, head {h}", got[k][:, h:h + 1].cpu()[:, :, part], want[k][:, :, part],
+                      bound[k][:, :, part])
+    assert rows.any() or kind == "window_rows"
