@@ -6,7 +6,7 @@
     O.backward(dO)
 
 The gradients are the library's backward calls and can be taken once (not
-differentiated again).  To capture a training step into a graph, capture
+differentiated again); forward-mode tangents are refused.  To capture a training step into a graph, capture
 sparse_mhsa_fwd_lse, sparse_mhsa_bwd and rotary themselves: they allocate
 nothing when given their outputs.  A backward pass of these functions refuses
 to be captured: torch would run the leaves' accumulation on the stream of any
@@ -17,6 +17,7 @@ from __future__ import annotations
 from typing import Optional
 
 import torch
+from torch.autograd import forward_ad
 from torch.autograd.function import once_differentiable
 
 from . import Acsr, Rotary
@@ -68,6 +69,8 @@ def sparse_mhsa(acsr: Acsr, Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor,
                 scale: float) -> torch.Tensor:
     """O = softmax_nz(scale * M (x) Q K^T) V with gradients for Q, K and V.  Without
     any to take this is sparse_mhsa_fwd."""
+    if any(forward_ad.unpack_dual(x).tangent is not None for x in (Q, K, V)):
+        raise NotImplementedError("sparse_mhsa has no forward-mode derivative")
     if not (torch.is_grad_enabled() and (Q.requires_grad or K.requires_grad or V.requires_grad)):
         return sparse_mhsa_fwd(acsr, Q, K, V, scale)
     if not acsr._info["grad"]:
