@@ -66,12 +66,17 @@ class _Rotary(torch.autograd.Function):
 
 
 def sparse_mhsa(acsr: Acsr, Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor,
-                scale: float) -> torch.Tensor:
+                scale: float, training: bool = False) -> torch.Tensor:
     """O = softmax_nz(scale * M (x) Q K^T) V with gradients for Q, K and V.  Without
-    any to take this is sparse_mhsa_fwd."""
+    any to take this is sparse_mhsa_fwd, whose O in bf16 differs by roundings from
+    that of the training forward; training=True takes the training forward there too.
+    Set it where a pass is run without gradients first and again with them, as some
+    activation checkpointing does: the layers behind then see the same O both times."""
     if any(forward_ad.unpack_dual(x).tangent is not None for x in (Q, K, V)):
         raise NotImplementedError("sparse_mhsa has no forward-mode derivative")
     if not (torch.is_grad_enabled() and (Q.requires_grad or K.requires_grad or V.requires_grad)):
+        if training:
+            return sparse_mhsa_fwd_lse(acsr, Q, K, V, scale)[0]
         return sparse_mhsa_fwd(acsr, Q, K, V, scale)
     if not acsr._info["grad"]:
         raise ValueError("gradients need a handle built with grad=True")

@@ -67,3 +67,16 @@ def test_functional_tangents_are_refused(calls):
     with pytest.raises((NotImplementedError, RuntimeError)):
         torch.func.jvp(lambda t: sag.sparse_mhsa(Handle, t, k, v, 1.0), (q,), (q,))
     assert calls == []
+
+
+def test_training_forward_without_gradients(calls):
+    """training=True takes one forward in both modes."""
+    x = three()
+    sag.sparse_mhsa(Handle, *x, 1.0)
+    sag.sparse_mhsa(Handle, *x, 1.0, training=True)
+    leaf = three(requires_grad=True)
+    with torch.no_grad():
+        sag.sparse_mhsa(Handle, *leaf, 1.0, training=True)
+    sag.sparse_mhsa(Handle, *leaf, 1.0, training=True)
+    sag.sparse_mhsa(Handle, *leaf, 1.0)
+    assert calls == ["fwd", "fwd_lse", "fwd_lse", "fwd_lse", "fwd_lse"]
