@@ -511,7 +511,10 @@ void splat_rotary_destroy(splat_rotary_t r); /* NULL is a no-op */
 splat_status splat_rotary_export(splat_rotary_t r, float* table);
 
 /* A [B, heads, T, d] tensor by its strides in elements: feature stride 1, the
- * others >= 0 and multiples of 16 bytes.  data: 16-byte aligned device memory. */
+ * others >= 0 and multiples of 16 bytes.  data: 16-byte aligned device memory.
+ * heads: 1 .. SPLAT_SERVE_MAX_HEADS, whatever B (tokens of a packed batch may be
+ * seen as [tokens, heads, 1, d]). */
+#define SPLAT_SERVE_MAX_HEADS 1048576
 typedef struct {
   void* data;
   int64_t stride_b, stride_h, stride_t, heads;

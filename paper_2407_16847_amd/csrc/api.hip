@@ -369,10 +369,17 @@ struct View {
 // x as a 32-bit size, 0 (which no check lets pass) if it is none
 int32_t int32_of(int64_t x) { return x > 0 && x <= INT32_MAX ? (int32_t)x : 0; }
 
+splat_status check_heads(int64_t heads, const char* what) {
+  if (heads < 1 || heads > SPLAT_SERVE_MAX_HEADS)
+    return fail(SPLAT_ERR_INVALID_ARG, "%s must have 1 .. %d heads, got %lld", what,
+                SPLAT_SERVE_MAX_HEADS, (long long)heads);
+  return SPLAT_OK;
+}
+
 splat_status check_view(const View& v, bool output) {
   const splat_heads& x = *v.x;
   CHECK(check_ptr(x.data, v.name));
-  CHECK(check_batch(v.B, int32_of(x.heads)));
+  CHECK(check_heads(x.heads, v.name));
   const int64_t unit = 16 / v.e, most = int64_t(1) << 40;
   struct Dim {
     int64_t n, stride;
@@ -456,12 +463,12 @@ void use_rotary(splat::HeadsArgs& a, splat_rotary_t r) {
   a.max_len = d.max_len, a.rot = d.rot_dim, a.interleaved = d.interleaved != 0;
 }
 
-splat_status check_cache(const splat_cache* c, int32_t B) {
+splat_status check_cache(const splat_cache* c) {
   if (!c) return fail(SPLAT_ERR_INVALID_ARG, "cache is NULL");
   CHECK(check_ptr(c->k, "the cache's k"));
   CHECK(check_ptr(c->v, "the cache's v"));
   if (!c->table) return fail(SPLAT_ERR_INVALID_ARG, "the cache's table is NULL");
-  CHECK(check_batch(B, int32_of(c->heads)));
+  CHECK(check_heads(c->heads, "the cache"));
   if (!int32_of(c->n_pages) || !int32_of(c->max_pages))
     return fail(SPLAT_ERR_INVALID_ARG, "n_pages and max_pages must be in [1, 2^31)");
   if (c->page < 1 || c->page > 65536 || (c->page & (c->page - 1)) != 0)
@@ -994,7 +1001,7 @@ splat_status splat_cache_append(splat_rotary_t r, splat_dtype dtype, int32_t B, 
   CHECK(check_d(d));
   CHECK(check_tokens(B, T));
   if (r) CHECK(check_rotary(r, d));
-  CHECK(check_cache(cache, B));
+  CHECK(check_cache(cache));
   if (!start) return fail(SPLAT_ERR_INVALID_ARG, "start is NULL");
   if (!kvq || (n != 2 && n != 4))
     return fail(SPLAT_ERR_INVALID_ARG, "kvq must hold K and V, or K, V, Q and Qr");
@@ -1065,7 +1072,7 @@ splat_status splat_sparse_mhsa_decode(splat_acsr_t h, splat_dtype dtype, int32_t
   CHECK(check_handle(h, B, H));
   CHECK(check_dtype(dtype, "dtype"));
   CHECK(check_d(d));
-  CHECK(check_cache(cache, B));
+  CHECK(check_cache(cache));
   int64_t need = 0;
   const int32_t heads = (int32_t)cache->heads;
   CHECK(splat_decode_workspace(h, B, H, heads, d, &need));

@@ -26,6 +26,7 @@ constexpr int kThreads = 256;
 // 39.6; four heads in flight and at most 8 a thread 34.7 .. 36.6.
 constexpr int kInFlight = 2;
 constexpr int kMaxHeads = 16;
+constexpr int64_t kMaxRuns = 65000;
 
 template <typename T>
 struct Chunk;
@@ -131,11 +132,13 @@ template <typename T, int D>
 hipError_t heads_launch(const HeadsArgs& x, hipStream_t st) {
   constexpr int TB = kThreads / (D / (2 * Chunk<T>::E));
   const int64_t blocks = ((int64_t)x.B * x.T + TB - 1) / TB;
-  int heads = 0;
+  int64_t heads = 0;
   for (int k = 0; k < x.n_jobs; ++k) heads += x.job[k].heads;
-  // as many heads a thread as leave the chip eight workgroups a CU
+  // as many heads a thread as leave the chip eight workgroups a CU, and more where
+  // their runs would pass a grid's second dimension
   int64_t per = blocks * heads / 2048;
   per = per < 1 ? 1 : per > kMaxHeads ? kMaxHeads : per;
+  per = std::max(per, heads / kMaxRuns + 1);
   int64_t runs = 0;
   for (int k = 0; k < x.n_jobs; ++k) runs += (x.job[k].heads + per - 1) / per;
   const dim3 grid((unsigned)blocks, (unsigned)runs);
