@@ -17,6 +17,7 @@ the library's HIP kernels.  There is no fallback: if the library is not built,
 from __future__ import annotations
 
 import ctypes
+import operator
 import os
 from typing import Optional, Tuple
 
@@ -410,7 +411,8 @@ def bwd_shared(acsr: Acsr, dtype: torch.dtype, B: int, H: int, d: int) -> Tuple[
     """How many of the plan's groups sparse_mhsa_bwd gives four workgroups each, for
     dQ and for dK and dV (splat_debug_bwd_shared): for tests; needs no GPU."""
     n = (ctypes.c_int32 * 2)()
-    _check(acsr._lib.splat_debug_bwd_shared(acsr.handle, _DT[dtype], B, H, d, n))
+    _check(acsr._lib.splat_debug_bwd_shared(acsr.handle, _DT[dtype], _int32(B, "B"), _int32(H, "H"),
+                                            _int32(d, "d"), n))
     return n[0], n[1]
 
 
@@ -600,6 +602,14 @@ def _where() -> Tuple[int, int]:
     return dev, _raw_stream(dev) if _raw_stream is not None else torch.cuda.current_stream().cuda_stream
 
 
+def _int32(x: int, name: str) -> int:
+    """x, if it fits 32 bits: ctypes would take its low half silently."""
+    x = operator.index(x)
+    if not -2 ** 31 <= x < 2 ** 31:
+        raise ValueError(f"{name} must fit 32 bits, got {x}")
+    return x
+
+
 class Rotary:
     """Rotary positions (see splat_rotary_build): the cosines and sines of
     positions 0 .. max_len - 1 on the current device."""
@@ -612,7 +622,8 @@ class Rotary:
         hi) only those of pairs that turn fewer than lo times in original_len
         positions, fading out until hi.  magnitude multiplies the result."""
         lo, hi = (0.0, 0.0) if ramp is None else ramp
-        self.desc = RotaryDesc(int(max_len), int(rot_dim), int(bool(interleaved)), int(original_len),
+        self.desc = RotaryDesc(_int32(int(max_len), "max_len"), _int32(int(rot_dim), "rot_dim"),
+                               int(bool(interleaved)), _int32(int(original_len), "original_len"),
                                float(base), float(factor), float(lo), float(hi), float(magnitude))
         self._h = ctypes.c_void_p()
         self._lib = load()
@@ -671,7 +682,8 @@ def cache_append(k_cache: torch.Tensor, v_cache: torch.Tensor, table: torch.Tens
 def decode_workspace(acsr: Acsr, B: int, H: int, heads: int, d: int) -> int:
     """Bytes of workspace that sparse_mhsa_decode takes (0: none)."""
     n = ctypes.c_int64()
-    _check(acsr._lib.splat_decode_workspace(acsr.handle, B, H, heads, d, ctypes.byref(n)))
+    _check(acsr._lib.splat_decode_workspace(acsr.handle, _int32(B, "B"), _int32(H, "H"),
+                                            _int32(heads, "heads"), _int32(d, "d"), ctypes.byref(n)))
     return n.value
 
 
