@@ -122,6 +122,14 @@ struct Call {
   }
 };
 
+// The caller's tensors that a call has written: autograd then notices a backward
+// pass that would read what they held before.
+void written(std::initializer_list<const Tensor*> xs) {
+  for (const Tensor* x : xs)
+    if (x && x->defined() && !x->is_inference()) x->unsafeGetTensorImpl()->bump_version();
+}
+const Tensor* given(const Opt& x) { return x ? &*x : nullptr; }
+
 splat_acsr_t acsr_of(int64_t handle) { return (splat_acsr_t)(uintptr_t)handle; }
 splat_rotary_t rotary_of(int64_t handle) { return (splat_rotary_t)(uintptr_t)handle; }
 
@@ -145,6 +153,7 @@ py::tuple fwd_lse(int64_t handle, const Tensor& Q, const Tensor& K, const Tensor
   const Tensor lse = c.out(lse_, "lse", at::kFloat, s.slice(0, 3), Q);
   check(splat_sparse_mhsa_fwd_lse(h, c.dtype(), s[0], s[1], s[3], Q.data_ptr(), k, v, (float)scale,
                                   O.data_ptr(), (float*)lse.data_ptr(), c.stream));
+  written({given(O_), given(lse_)});
   return py::make_tuple(O, lse);
 }
 
@@ -164,6 +173,7 @@ py::tuple bwd(int64_t handle, const Tensor& Q, const Tensor& K, const Tensor& V,
   check(splat_sparse_mhsa_bwd(h, c.dtype(), s[0], s[1], s[3], Q.data_ptr(), k, v, o, l, g, (float)scale,
                               dQ.data_ptr(), dK.data_ptr(), dV.data_ptr(), (float*)ws.data_ptr(),
                               c.stream));
+  written({given(dQ_), given(dK_), given(dV_), given(workspace)});
   return py::make_tuple(dQ, dK, dV);
 }
 
@@ -183,6 +193,7 @@ py::object rotary(int64_t handle, const Tensor& X, const Opt& X2, const Opt& pos
   const int32_t* const pos = positions ? c.ints(*positions, "positions", {s[0], s[2]}) : nullptr;
   check(splat_rotary_apply(rotary_of(handle), c.dtype(), s[0], s[2], s[3], pos, xy, X2 ? 2 : 1,
                            inverse, c.stream));
+  written({given(Y), given(Y2)});
   if (X2) return py::make_tuple(y[0], y[1]);
   return py::cast(y[0]);
 }
@@ -206,6 +217,7 @@ py::object cache_append(int64_t rot, const Tensor& k_cache, const Tensor& v_cach
   }
   check(splat_cache_append(rotary_of(rot), c.dtype(), s[0], s[2], s[3], &cache, at, n, kvq, Q ? 4 : 2,
                            c.stream));
+  written({&k_cache, &v_cache, given(Qr)});
   if (!Q) return py::none();
   return py::cast(q);
 }
@@ -236,6 +248,7 @@ Tensor decode(int64_t handle, const Tensor& Q, const Tensor& k_cache, const Tens
   }
   check(splat_sparse_mhsa_decode(h, c.dtype(), s[0], s[1], s[3], Q.data_ptr(), &cache, n, (float)scale,
                                  O.data_ptr(), need ? ws.data_ptr() : nullptr, c.stream));
+  written({given(O_), need ? given(workspace) : nullptr});
   return O;
 }
 
