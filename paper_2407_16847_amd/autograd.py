@@ -33,6 +33,13 @@ def _not_captured() -> None:
                            "capture sparse_mhsa_bwd and rotary(inverse=True) instead")
 
 
+def _gradient(x: torch.Tensor) -> torch.Tensor:
+    """x as the calls take it: contiguous and at 16 bytes, which a gradient behind a
+    concatenation need not be."""
+    x = x.contiguous()
+    return x if x.data_ptr() % 16 == 0 else x.clone()
+
+
 class _SparseMHSA(torch.autograd.Function):
     @staticmethod
     def forward(ctx, acsr, Q, K, V, scale):
@@ -46,7 +53,7 @@ class _SparseMHSA(torch.autograd.Function):
     def backward(ctx, dO):
         _not_captured()
         Q, K, V, O, lse = ctx.saved_tensors
-        dQ, dK, dV = sparse_mhsa_bwd(ctx.acsr, Q, K, V, O, lse, dO.contiguous(), ctx.scale)
+        dQ, dK, dV = sparse_mhsa_bwd(ctx.acsr, Q, K, V, O, lse, _gradient(dO), ctx.scale)
         return None, dQ, dK, dV, None
 
 
@@ -62,7 +69,7 @@ class _Rotary(torch.autograd.Function):
     def backward(ctx, dY):
         _not_captured()
         positions, = ctx.saved_tensors
-        return None, _rotary(ctx.rot, dY.contiguous(), positions=positions, inverse=True), None
+        return None, _rotary(ctx.rot, _gradient(dY), positions=positions, inverse=True), None
 
 
 def sparse_mhsa(acsr: Acsr, Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor,

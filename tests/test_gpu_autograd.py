@@ -74,3 +74,27 @@ def test_a_call_into_a_saved_tensor_is_noticed(gpu_lib, which):
     out.backward(dO)                      # and new outputs of the calls are no such writes
     torch.cuda.synchronize()
     assert torch.isfinite(q.grad).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_gradients_off_their_alignment(gpu_lib, dtype):
+    """The gradients behind a concatenation are those of the pass without it."""
+    from paper_2407_16847_amd import autograd as sag
+    splat = gpu_lib
+    a, _ = make(splat, "window", {"w": 20}, 100)
+    rot = splat.Rotary(100, 64)
+    x = [t.cuda() for t in inputs(100, 64, 2, dtype, 3)]
+    dO, x = x[3], x[:3]
+    grads = []
+    for cat in (False, True):
+        leaf = [t.clone().requires_grad_() for t in x]
+        for k, call in ((3, lambda: sag.sparse_mhsa(a, *leaf, 0.125)), (1, lambda: sag.rotary(rot, leaf[0]))):
+            out = call().flatten()
+            want = dO.flatten()
+            if cat:
+                one = torch.zeros(1, dtype=dtype, device="cuda", requires_grad=True)
+                out, want = torch.cat((one, out)), torch.cat((one.detach(), want))
+            grads.append(torch.autograd.grad(out, leaf[:k], want))
+    torch.cuda.synchronize()
+    for got, ref in zip(grads[2:], grads[:2]):
+        assert all(torch.equal(u, v) for u, v in zip(got, ref))

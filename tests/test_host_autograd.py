@@ -80,3 +80,32 @@ def test_training_forward_without_gradients(calls):
     sag.sparse_mhsa(Handle, *leaf, 1.0, training=True)
     sag.sparse_mhsa(Handle, *leaf, 1.0)
     assert calls == ["fwd", "fwd_lse", "fwd_lse", "fwd_lse", "fwd_lse"]
+
+
+def test_gradients_off_their_alignment(calls, monkeypatch):
+    """A gradient arrives as its graph leaves it: contiguous but not at 16 bytes
+    behind a concatenation, without strides behind a sum."""
+    seen = []
+    for name in ("sparse_mhsa_bwd", "_rotary"):
+        f = getattr(sag, name)
+
+        def check(*args, f=f, **kw):
+            x = args[1] if kw.get("inverse") else args[6] if len(args) > 6 else None
+            if x is not None:
+                seen.append(x.clone())
+                assert x.is_contiguous() and x.data_ptr() % 16 == 0
+            return f(*args, **kw)
+
+        monkeypatch.setattr(sag, name, check)
+    for dtype in (torch.float32, torch.bfloat16):
+        for call in (lambda q, k, v: sag.sparse_mhsa(Handle, q, k, v, 1.0), lambda q, k, v: sag.rotary(None, q)):
+            x = three(requires_grad=True, dtype=dtype)
+            one = torch.zeros(1, dtype=dtype, requires_grad=True)
+            want = torch.randn(513, dtype=dtype)
+            torch.cat((one, call(*x).flatten())).backward(want)
+            assert torch.equal(seen.pop().flatten(), want[1:])
+            call(*x).sum().backward()
+            assert (seen.pop() == 1).all()
+            call(*x).transpose(1, 2).backward(want[1:].view(1, 4, 2, 64))
+            assert torch.equal(seen.pop(), want[1:].view(1, 4, 2, 64).transpose(1, 2))
+    assert not seen
