@@ -9,7 +9,7 @@ import numpy as np
 import pytest
 import torch
 
-from test_gpu_grad import TYPES, backward64, check, inputs, make
+from test_gpu_grad import C, HALF, LARGE, TYPES, backward64, check, inputs, make
 
 pytestmark = pytest.mark.gpu
 
@@ -107,3 +107,56 @@ def test_rows_of_few_keys_beside_longer_ones(gpu_lib, kind, params, L, heads, d)
                 check(f"{name}, head {h}", got[k][:, h:h + 1].cpu()[:, :, part], want[k][:, :, part],
                       bound[k][:, :, part])
     assert rows.any() or kind == "window_rows"
+
+
+def _not_finite(splat, a, M, T, where, value, x, scale, dtype):
+    """Rows and keys that a value in row or key x does not reach are as without it."""
+    T[where][:, :, x, 3] = 0.0
+
+    def run():
+        O, lse = splat.sparse_mhsa_fwd_lse(a, T["Q"], T["K"], T["V"], scale)
+        grads = splat.sparse_mhsa_bwd(a, T["Q"], T["K"], T["V"], O, lse, T["dO"], scale)
+        torch.cuda.synchronize()
+        return [y.cpu() for y in (O, *grads)]
+
+    clean = run()
+    T[where][:, :, x, 3] = value
+    got = run()
+    rows = M[:, x].copy() if where in ("K", "V") else np.arange(M.shape[0]) == x
+    keys = M[rows].any(0)
+    rows, keys = torch.from_numpy(~rows), torch.from_numpy(~keys)
+    # a row or key that is formed again has its sums in another order: roundings of p,
+    # dS, delta and the result, and of fp32's sums
+    half = 8 * HALF[dtype] + 256 * C
+    for name, g, r, ok in zip(("O", "dQ", "dK", "dV"), got, clean, (rows, rows, keys, keys)):
+        g, r = g[:, :, ok].double(), r[:, :, ok].double()
+        assert torch.isfinite(g).all(), name
+        if g.numel():
+            top = r.abs().amax(-1, keepdim=True)
+            assert ((g - r).abs() <= half * top + 1e-6).all(), name
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("value", [math.inf, -math.inf, math.nan])
+@pytest.mark.parametrize("where", ["K", "V", "Q", "dO"])
+@pytest.mark.parametrize("kind,params,L", [
+    ("window", {"w": 16}, 300), ("blocked", {"block": 33}, 200), ("dilated", {"w": 9, "dilation": 3}, 250),
+    ("strided_local", {"local": 40, "stride": 33}, 200)])
+def test_values_that_are_not_finite_in_wide_heads(gpu_lib, kind, params, L, where, value, dtype):
+    """d = 128: half tiles and V in LDS, and the rows that are formed again behind them."""
+    splat = gpu_lib
+    print(f"[gpu] not finite, d=128, {kind} {where} {value} {dtype}", flush=True)
+    a, M = make(splat, kind, params, L)
+    T = dict(zip(("Q", "K", "V", "dO"), (t.cuda() for t in inputs(L, 128, 2, dtype, 9))))
+    _not_finite(splat, a, M, T, where, value, L // 2, 1 / math.sqrt(128), dtype)
+
+
+@pytest.mark.parametrize("value", [math.inf, math.nan])
+@pytest.mark.parametrize("where", ["K", "V", "Q", "dO"])
+@pytest.mark.parametrize("kind,params,L,heads", [LARGE[0], LARGE[1], LARGE[5]])
+def test_large_launches_of_wide_heads_and_values_that_are_not_finite(gpu_lib, kind, params, L, heads,
+                                                                    where, value):
+    splat = gpu_lib
+    a, M = make(splat, kind, params, L)
+    T = dict(zip(("Q", "K", "V", "dO"), (t.cuda() for t in inputs(L, 128, heads, torch.bfloat16, 9))))
+    _not_finite(splat, a, M, T, where, value, L // 2, 1 / math.sqrt(128), torch.bfloat16)
