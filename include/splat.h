@@ -450,15 +450,15 @@ splat_status splat_sparse_mhsa_fwd(splat_acsr_t h, splat_dtype dtype, int32_t B,
  *
  * splat_sparse_mhsa_bwd -- dQ, dK, dV [B,H,L,d] of `dtype` from Q, K, V, the O and
  * lse of splat_sparse_mhsa_fwd_lse and the gradient dO of O, all [B,H,L,d] of
- * `dtype`.  The probabilities are recomputed, in fp32; with bf16 inputs p and dS
- * are rounded to nearest even bf16 for the products that sum them, which run in
- * fp32, and dO_i.O_i is taken from the rounded O given, except for rows of 2 to 32
- * keys, for which it is formed as sum_j p_ij dP_ij: in a row of more keys the
- * rounding of O, 2^-8 at most of |dO_i| |O_i|, reaches each dS_ij times p_ij,
- * which is much next to dS_ij where one key has nearly all the weight.  Sums have a fixed order: equal calls give equal bits.  A row with one
- * key has p = 1 whatever its score: its dS is 0, and so its dQ.  Rows without keys
- * have dQ = 0, keys without rows dK = dV = 0.  An infinity or a NaN reaches only
- * the gradients that the mask connects it with.
+ * `dtype`.  The probabilities are recomputed, in fp32; with bf16 inputs p and dS are
+ * rounded to nearest even bf16 for the products that sum them, which run in fp32, and
+ * dO_i.O_i is taken from the rounded O given, except for rows of 2 to 32 keys, for
+ * which it is formed as sum_j p_ij dP_ij: in a row of more keys the rounding of O,
+ * 2^-8 at most of |dO_i| |O_i|, reaches each dS_ij times p_ij, which is much next to
+ * dS_ij where one key has nearly all the weight.  Sums have a fixed order: equal
+ * calls give equal bits.  A row with one key has p = 1 whatever its score: its dS is
+ * 0, and so its dQ.  Rows without keys have dQ = 0, keys without rows dK = dV = 0.
+ * An infinity or a NaN reaches only the gradients that the mask connects it with.
  * workspace: 2*B*H*L floats of device memory that the call writes and reads (calls
  * that may run at the same time need one each).  The gradients and the workspace
  * share no memory with the inputs or each other (INVALID_ARG).  The handle must

@@ -23,9 +23,10 @@
 // has bf16.  Bound by the matrix cores where the chip is full: they are 75 and 79%
 // busy in dQ and dK, dV (full mask, L = 2048, d = 64, 16 heads: 250 and 310 us, 103
 // and 111 TFLOP/s; a product of 8192^3 reaches 153), and by the longest slice where
-// it is not (window 256 + 32 global, L = 2048, 12 heads: 82 and 106 us).  Two sets of
-// staged rows a wavefront, one loading while the other is used, gained nothing (86,
-// 108 us), eight wavefronts a slice lost (95, 112 us).
+// it is not (window 256 + 32 global, L = 2048, 12 heads: 77 and 94 us, 82 and 106 in
+// the run of the next pairs).  Two sets of staged rows a wavefront, one loading while
+// the other is used, gained nothing (86, 108 us), eight wavefronts a slice lost (95,
+// 112 us).
 #include <hip/hip_runtime.h>
 #include <math.h>
 

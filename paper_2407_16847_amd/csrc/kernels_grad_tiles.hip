@@ -20,10 +20,11 @@
 // 1.2 to 1.6 times the work a tile, but the chain of a group's tiles takes less than
 // half as long (grad_long_groups, below).
 //
-// Measured, dQ and dK, dV, us: window 512 + 64 global, L = 4096, d = 64, 64 heads
-// 132, 183 (817 and 786 TFLOP/s of their 6 d and 8 d flops a non-zero; a product of
-// 8192^3 reaches 1187); dilated 2, L = 4096, d = 128, 16 heads 41, 48 (590, 672);
-// strided+local 128, L = 2048, 24 heads 16, 25, the longest group's chain.  For 32 x
+// Measured, dQ and dK, dV, us, in a trace of passes one after the other: window 512 +
+// 64 global, L = 4096, d = 64, 64 heads 122, 166 (880 and 870 TFLOP/s of their 6 d and
+// 8 d flops a non-zero; a product of 8192^3 reaches 1187); dilated 2, L = 4096, d = 128,
+// 16 heads 39, 45 (620, 710); strided+local 128, L = 2048, 24 heads 15, 24, the longest
+// group's chain.  Pairs below are of one run each, on a colder chip.  For 32 x
 // 32 elements a SIMD has 12 (16) matrix instructions, 384 (512) cycles; 16
 // exponentials, multiply-adds and products and 8 (16) conversions, 416 (448) cycles;
 // and a quarter of the CU's LDS reads, 12 (24) KB a wavefront, 384 (768) cycles.

@@ -179,8 +179,8 @@ __device__ __forceinline__ void mask_scores(f32x16_t* s, uint64_t mk, int h) {
 // not scaled and rounded beforehand, the scores are scaled in fp32 (so that
 // both passes see the same scores), the rows' log-sum-exp adds the p before
 // their rounding, and rows that are not finite are formed again from their own
-// keys alone.  99 us where the other takes 87 (window 512 + 64 global, L = 4096, 64
-// heads): 32 products and 30 sums a lane and tile more.
+// keys alone.  102 us where the other takes 91 to 96 (window 512 + 64 global, L = 4096,
+// 64 heads, changing inputs): 32 products and 30 sums a lane and tile more.
 struct LseArgs {
   float* lse;
   const int32_t* row_ptr;

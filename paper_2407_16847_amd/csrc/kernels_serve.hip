@@ -158,9 +158,10 @@ hipError_t heads_launch(const HeadsArgs& x, hipStream_t st) {
 // has a contiguous range of a sequence's units, its wavefronts every fourth of
 // them; ranges of one sequence are joined by a second kernel.  Bound by memory:
 // K and V of the row's keys are read once, staged in LDS by loads that take whole
-// rows.  32 sequences of 1000 .. 8192 keys, 32 heads over 8, d = 128: 120 us, 5.0
-// TB/s, what a copy of 1 GiB reaches; one sequence of a window's 577 keys 5.3 us and
-// 3.9 to join, a chain of loads (row, pages, keys) with nothing to hide it.
+// rows.  32 sequences of 1000 .. 8192 keys, 32 heads over 8, d = 128, bf16: 117 us and
+// 4.7 to join, 5.0 TB/s, what a copy of 1 GiB reaches (fp32: 274 in all, 4.4 TB/s; fp32,
+// d = 64: 165, 3.7 TB/s); one sequence of a window's 577 keys 5.4 us and 4.0 to join, a
+// chain of loads (row, pages, keys) with nothing to hide it.
 constexpr int kHeadRows = 32;
 constexpr int kMaxSplits = 64;
 
@@ -407,7 +408,7 @@ hipError_t prepare_decode() {
 }
 
 // As many splits as fill the chip with two workgroups a CU while each wavefront
-// keeps two units.  One / two / four units a wavefront: window 512 + 64 global at
+// keeps two units, between what a short row and a long one like best.  One / two / four units a wavefront: window 512 + 64 global at
 // L = 4000, 16 heads, one sequence 10.4 / 8.5 / 7.8 us; every key of 8192, d = 128, 32
 // heads over 8, one sequence 21 / 15 / 17 us.  Twice and four times the workgroups
 // for 32 sequences of 1000 .. 8192 keys: 130 -> 138, 150 us.
