@@ -6,11 +6,12 @@
     O.backward(dO)
 
 The gradients are the library's backward calls and can be taken once (not
-differentiated again); forward-mode tangents are refused.  To capture a training step into a graph, capture
-sparse_mhsa_fwd_lse, sparse_mhsa_bwd and rotary themselves: they allocate
-nothing when given their outputs.  A backward pass of these functions refuses
-to be captured: torch would run the leaves' accumulation on the stream of any
-eager graph of the same leaves that still lives, outside the capture.
+differentiated again); forward-mode tangents are refused. To capture a training
+step into a graph, capture sparse_mhsa_fwd_lse, sparse_mhsa_bwd and rotary
+themselves: they allocate nothing when given their outputs. A backward pass of
+these functions refuses to be captured: torch would run the leaves' accumulation
+on the stream of any eager graph of the same leaves that still lives, outside
+the capture.
 """
 from __future__ import annotations
 

@@ -408,10 +408,11 @@ hipError_t prepare_decode() {
 }
 
 // As many splits as fill the chip with two workgroups a CU while each wavefront
-// keeps two units, between what a short row and a long one like best.  One / two / four units a wavefront: window 512 + 64 global at
-// L = 4000, 16 heads, one sequence 10.4 / 8.5 / 7.8 us; every key of 8192, d = 128, 32
-// heads over 8, one sequence 21 / 15 / 17 us.  Twice and four times the workgroups
-// for 32 sequences of 1000 .. 8192 keys: 130 -> 138, 150 us.
+// keeps two units, between what a short row and a long one like best.  One / two /
+// four units a wavefront: window 512 + 64 global at L = 4000, 16 heads, one
+// sequence 10.4 / 8.5 / 7.8 us; every key of 8192, d = 128, 32 heads over 8, one
+// sequence 21 / 15 / 17 us.  Twice and four times the workgroups for 32 sequences
+// of 1000 .. 8192 keys: 130 -> 138, 150 us.
 int decode_splits(const DevAcsr& a, int B, int H, int heads) {
   const int64_t groups = (int64_t)B * heads * head_chunks(H, heads);
   const int64_t units = (a.max_row_nnz + kUnit - 1) / kUnit;
