@@ -507,6 +507,27 @@ typedef struct {
 
 typedef struct splat_rotary* splat_rotary_t;
 splat_status splat_rotary_build(const splat_rotary_desc* desc, splat_rotary_t* out);
+
+/*
+ * Rotary positions with several axes, for tokens that have a place in time, a row
+ * and a column: pair t turns by its own axis's position.  The axes' pairs lie one
+ * axis after the other, or (cyclic) the axes take turns, one pair each, while they
+ * have pairs left.  The frequency of pair t is base^(-2t/rot_dim) as with one axis,
+ * or (restart) that of its number k among its axis's `pairs`, base^(-k/pairs); it is
+ * scaled as with one axis.  Calls with such a handle take positions [axes, B, T],
+ * one axis after the other, and need them (INVALID_ARG); a position outside the
+ * table gives NaN in that axis's pairs alone.
+ *
+ * splat_rotary_build_axes -- axes NULL: one axis, as splat_rotary_build.
+ */
+#define SPLAT_ROTARY_MAX_AXES 4
+typedef struct {
+  int32_t n;       /* axes, 1 .. SPLAT_ROTARY_MAX_AXES */
+  int32_t pairs[SPLAT_ROTARY_MAX_AXES]; /* of each axis: >= 1, rot_dim/2 in all; 0 past n */
+  int32_t cyclic, restart;              /* 0 or 1 */
+} splat_rotary_axes;
+splat_status splat_rotary_build_axes(const splat_rotary_desc* desc, const splat_rotary_axes* axes,
+                                     splat_rotary_t* out);
 void splat_rotary_destroy(splat_rotary_t r); /* NULL is a no-op */
 splat_status splat_rotary_export(splat_rotary_t r, float* table);
 
@@ -523,7 +544,7 @@ typedef struct {
 /*
  * splat_rotary_apply -- y = the rotation of x, for n = 1 or 2 tensors (a layer's Q
  * and K) of `dtype`: xy[2 * n] is x, y for each in turn.  positions: int32 [B, T] on the
- * device, NULL for 0 .. T-1.  inverse: the transposed rotation, which is the
+ * device ([axes, B, T] for a handle with axes), NULL for 0 .. T-1.  inverse: the transposed rotation, which is the
  * gradient (and, at magnitude 1, the inverse).  A token whose position lies
  * outside [0, max_len) gets NaN in its rotated features.  B*T <= 2^27.  fp32
  * arithmetic, one rounding.  y may be x itself (same strides) and otherwise shares no memory
@@ -557,11 +578,21 @@ typedef struct {
  * 0 in padding rows; it may be Q itself, otherwise it shares no memory with another
  * argument.
  * Positions past r's max_len give NaN, as in splat_rotary_apply.
+ *
+ * splat_cache_append_at -- the same with the tokens' positions apart from their
+ * places in the cache: positions int32 [B, T] ([axes, B, T] for a handle with axes)
+ * say how far K and Q turn, start where the tokens lie.  So a cache that holds fewer
+ * tokens than its sequence has had (splat_cache_evict) goes on.  positions NULL: the
+ * places; otherwise r must be given, and Qr and the cache share no memory with them.
  */
 splat_status splat_cache_append(splat_rotary_t r, splat_dtype dtype, int32_t B, int32_t T, int32_t d,
                                 const splat_cache* cache, const int32_t* start,
                                 const int32_t* counts, const splat_heads* kvq, int32_t n,
                                 void* stream);
+splat_status splat_cache_append_at(splat_rotary_t r, splat_dtype dtype, int32_t B, int32_t T, int32_t d,
+                                   const splat_cache* cache, const int32_t* start,
+                                   const int32_t* counts, const int32_t* positions,
+                                   const splat_heads* kvq, int32_t n, void* stream);
 
 /*
  * splat_sparse_mhsa_decode -- the attention of one query token a sequence over the

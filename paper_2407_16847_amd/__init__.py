@@ -19,7 +19,7 @@ from __future__ import annotations
 import ctypes
 import operator
 import os
-from typing import Optional, Tuple
+from typing import Optional, Sequence, Tuple
 
 import numpy as np
 import torch  # loaded first: libsplat then binds to the HIP runtime torch uses
@@ -80,6 +80,11 @@ class RotaryDesc(ctypes.Structure):
                 ("interleaved", ctypes.c_int32), ("original_len", ctypes.c_int32),
                 ("base", ctypes.c_double), ("factor", ctypes.c_double), ("ramp_lo", ctypes.c_double),
                 ("ramp_hi", ctypes.c_double), ("magnitude", ctypes.c_double)]
+
+
+class RotaryAxes(ctypes.Structure):
+    _fields_ = [("n", ctypes.c_int32), ("pairs", ctypes.c_int32 * 4), ("cyclic", ctypes.c_int32),
+                ("restart", ctypes.c_int32)]
 
 
 TILING_METHODS = {"poset": 0, "grid": 1, "naive": 2}
@@ -144,9 +149,11 @@ def _open(path: str) -> ctypes.CDLL:
         "splat_sparse_mhsa_bwd": [vp, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, f32, vp, vp, vp, vp,
                                   vp],
         "splat_rotary_build": [P(RotaryDesc), P(vp)],
+        "splat_rotary_build_axes": [P(RotaryDesc), P(RotaryAxes), P(vp)],
         "splat_rotary_export": [vp, vp],
         "splat_rotary_apply": [vp, i32, i32, i32, i32, vp, vp, i32, i32, vp],
         "splat_cache_append": [vp, i32, i32, i32, i32, vp, vp, vp, vp, i32, vp],
+        "splat_cache_append_at": [vp, i32, i32, i32, i32, vp, vp, vp, vp, vp, i32, vp],
         "splat_decode_workspace": [vp, i32, i32, i32, i32, P(i64)],
         "splat_sparse_mhsa_decode": [vp, i32, i32, i32, i32, vp, vp, vp, f32, vp, vp, vp],
         "splat_sparse_mhsa_unfused_noalloc": [vp, i32, i32, i32, i32, vp, vp, vp, f32, vp, i32, f32,
@@ -616,11 +623,16 @@ class Rotary:
 
     def __init__(self, max_len: int, rot_dim: int, *, base: float = 10000.0, interleaved: bool = False,
                  factor: float = 1.0, ramp: Optional[Tuple[float, float]] = None,
-                 original_len: int = 0, magnitude: float = 1.0):
+                 original_len: int = 0, magnitude: float = 1.0, axes: Optional[Sequence[int]] = None,
+                 cyclic: bool = False, restart: bool = False):
         """The first rot_dim features turn: pairs (t, t + rot_dim/2), or (2t,
         2t + 1) if interleaved.  factor divides the frequencies; with ramp = (lo,
         hi) only those of pairs that turn fewer than lo times in original_len
-        positions, fading out until hi.  magnitude multiplies the result."""
+        positions, fading out until hi.  magnitude multiplies the result.
+        axes: how many of the rot_dim/2 pairs turn by each of 1 to 4 axes of
+        positions (time, row, column), one axis's pairs after the other's or
+        (cyclic) the axes in turn; restart gives each axis frequencies from base^0
+        on.  Positions are then [axes, B, T]."""
         lo, hi = (0.0, 0.0) if ramp is None else ramp
         self.desc = RotaryDesc(_int32(int(max_len), "max_len"), _int32(int(rot_dim), "rot_dim"),
                                int(bool(interleaved)), _int32(int(original_len), "original_len"),
@@ -629,7 +641,16 @@ class Rotary:
         self._lib = load()
         if ramp is not None and not hi > lo:
             raise ValueError("ramp must be (lo, hi) with lo < hi")
-        _check(self._lib.splat_rotary_build(ctypes.byref(self.desc), ctypes.byref(self._h)))
+        if axes is None and (cyclic or restart):
+            raise ValueError("cyclic and restart need axes")
+        pairs = [_int32(n, "axes") for n in axes] if axes is not None else [int(rot_dim) // 2]
+        if not 1 <= len(pairs) <= 4:
+            raise ValueError(f"1 to 4 axes, got {len(pairs)}")
+        self.axes = len(pairs)
+        ax = RotaryAxes(len(pairs), (ctypes.c_int32 * 4)(*pairs), int(bool(cyclic)), int(bool(restart)))
+        _check(self._lib.splat_rotary_build_axes(ctypes.byref(self.desc),
+                                                 None if axes is None else ctypes.byref(ax),
+                                                 ctypes.byref(self._h)))
 
     def close(self) -> None:
         if getattr(self, "_h", None) is not None and self._h.value:
@@ -659,24 +680,26 @@ def rotary(rot: Rotary, X: torch.Tensor, X2: Optional[torch.Tensor] = None, *,
            positions: Optional[torch.Tensor] = None, inverse: bool = False,
            Y: Optional[torch.Tensor] = None, Y2: Optional[torch.Tensor] = None):
     """X [B, H, T, d] (any strides, contiguous features) rotated to its tokens'
-    positions -- int32 [B, T], or 0 .. T-1 -- as a contiguous tensor, or into Y,
-    which may be X.  With X2 (its own number of heads; a layer's Q and K in one
+    positions -- int32 [B, T], or 0 .. T-1; [axes, B, T] where rot has several axes --
+    as a contiguous tensor, or into Y, which may be X.  With X2 (its own number of heads; a layer's Q and K in one
     launch) returns both.  inverse=True: the transposed rotation, its gradient."""
-    return native().rotary(rot.handle.value, X, X2, positions, inverse, Y, Y2, *_where())
+    return native().rotary(rot.handle.value, X, X2, positions, inverse, Y, Y2, rot.axes, *_where())
 
 
 def cache_append(k_cache: torch.Tensor, v_cache: torch.Tensor, table: torch.Tensor,
                  start: torch.Tensor, K: torch.Tensor, V: torch.Tensor, *,
                  counts: Optional[torch.Tensor] = None, rot: Optional[Rotary] = None,
-                 Q: Optional[torch.Tensor] = None, Qr: Optional[torch.Tensor] = None
-                 ) -> Optional[torch.Tensor]:
+                 Q: Optional[torch.Tensor] = None, Qr: Optional[torch.Tensor] = None,
+                 positions: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
     """Writes K and V [B, heads, T, d] into the paged cache ([pages, heads, page,
     d] each; table int32 [B, max_pages]), the first token of sequence b at
     position start[b], K rotated on the way; only the first counts[b] tokens, if
     given.  With Q [B, H, T, d] returns its rotation at the same positions (in Qr,
-    if given; padding rows 0)."""
+    if given; padding rows 0).  positions, int32 [B, T] ([axes, B, T] where rot has
+    several axes): how far the tokens turn, where that is not their place in the
+    cache, as behind a cache_evict; start then says the place alone."""
     return native().cache_append(0 if rot is None else rot.handle.value, k_cache, v_cache, table, start,
-                                 K, V, counts, Q, Qr, *_where())
+                                 K, V, counts, Q, Qr, positions, 1 if rot is None else rot.axes, *_where())
 
 
 def decode_workspace(acsr: Acsr, B: int, H: int, heads: int, d: int) -> int:

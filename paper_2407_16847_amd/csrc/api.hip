@@ -461,6 +461,8 @@ void use_rotary(splat::HeadsArgs& a, splat_rotary_t r) {
   const splat_rotary_desc& d = r->host.desc;
   a.angles = (const float2*)r->dmem;
   a.max_len = d.max_len, a.rot = d.rot_dim, a.interleaved = d.interleaved != 0;
+  a.axes = r->host.axes;
+  if (a.axes > 1) a.axis = (const uint8_t*)(a.angles + (size_t)d.max_len * (d.rot_dim / 2));
 }
 
 splat_status check_cache(const splat_cache* c) {
@@ -904,6 +906,11 @@ splat_status splat_sparse_mhsa_bwd(splat_acsr_t h, splat_dtype dtype, int32_t B,
 }
 
 splat_status splat_rotary_build(const splat_rotary_desc* desc, splat_rotary_t* out) {
+  return splat_rotary_build_axes(desc, nullptr, out);
+}
+
+splat_status splat_rotary_build_axes(const splat_rotary_desc* desc, const splat_rotary_axes* axes,
+                                     splat_rotary_t* out) {
   if (!desc || !out) return fail(SPLAT_ERR_INVALID_ARG, "desc and out must be non-NULL");
   splat_rotary* r = new (std::nothrow) splat_rotary();
   if (!r) return fail(SPLAT_ERR_OOM, "host allocation failed");
@@ -914,7 +921,7 @@ splat_status splat_rotary_build(const splat_rotary_desc* desc, splat_rotary_t* o
   };
   try {
     std::string err;
-    const splat_status s = splat::rotary_build(*desc, r->host, err);
+    const splat_status s = splat::rotary_build(*desc, axes, r->host, err);
     if (s != SPLAT_OK) return drop(s, err.c_str(), "");
     int n = 0;
     if (hipGetDeviceCount(&n) != hipSuccess || n == 0) {
@@ -925,13 +932,17 @@ splat_status splat_rotary_build(const splat_rotary_desc* desc, splat_rotary_t* o
     const std::vector<float> table = splat::rotary_table(r->host);
     hipError_t e = hipGetDevice(&r->device);
     if (e != hipSuccess) return drop(SPLAT_ERR_HIP, "hipGetDevice", hipGetErrorString(e));
-    e = hipMalloc((void**)&r->dmem, table.size() * sizeof(float));
+    const size_t angles = table.size() * sizeof(float);
+    e = hipMalloc((void**)&r->dmem, angles + r->host.axis.size());
     if (e != hipSuccess) {
       (void)hipGetLastError();
       r->dmem = nullptr;
       return drop(SPLAT_ERR_OOM, "hipMalloc for the rotary table", hipGetErrorString(e));
     }
-    e = hipMemcpy(r->dmem, table.data(), table.size() * sizeof(float), hipMemcpyHostToDevice);
+    e = hipMemcpy(r->dmem, table.data(), angles, hipMemcpyHostToDevice);
+    if (e == hipSuccess)
+      e = hipMemcpy((char*)r->dmem + angles, r->host.axis.data(), r->host.axis.size(),
+                    hipMemcpyHostToDevice);
     if (e != hipSuccess)
       return drop(SPLAT_ERR_HIP, "hipMemcpy of the rotary table", hipGetErrorString(e));
   } catch (const std::bad_alloc&) {
@@ -976,7 +987,9 @@ splat_status splat_rotary_apply(splat_rotary_t r, splat_dtype dtype, int32_t B, 
     if (x[k].x->heads != y[k].x->heads)
       return fail(SPLAT_ERR_INVALID_ARG, "%s and %s differ in heads", x[k].name, y[k].name);
   }
-  const size_t pos_bytes = (size_t)B * T * 4;
+  if (r->host.axes > 1 && !positions)
+    return fail(SPLAT_ERR_INVALID_ARG, "a rotation with several axes needs positions");
+  const size_t pos_bytes = (size_t)r->host.axes * B * T * 4;
   for (int k = 0; k < n; ++k) {
     for (int i = 0; i < n; ++i)
       if (!(i == k && y[k].same(x[k]))) CHECK(check_apart(y[k], x[i]));
@@ -997,10 +1010,20 @@ splat_status splat_cache_append(splat_rotary_t r, splat_dtype dtype, int32_t B, 
                                 const splat_cache* cache, const int32_t* start,
                                 const int32_t* counts, const splat_heads* kvq, int32_t n,
                                 void* stream) {
+  return splat_cache_append_at(r, dtype, B, T, d, cache, start, counts, nullptr, kvq, n, stream);
+}
+
+splat_status splat_cache_append_at(splat_rotary_t r, splat_dtype dtype, int32_t B, int32_t T, int32_t d,
+                                   const splat_cache* cache, const int32_t* start,
+                                   const int32_t* counts, const int32_t* positions,
+                                   const splat_heads* kvq, int32_t n, void* stream) {
   CHECK(check_dtype(dtype, "dtype"));
   CHECK(check_d(d));
   CHECK(check_tokens(B, T));
   if (r) CHECK(check_rotary(r, d));
+  if (positions && !r) return fail(SPLAT_ERR_INVALID_ARG, "positions need a rotation");
+  if (r && r->host.axes > 1 && !positions)
+    return fail(SPLAT_ERR_INVALID_ARG, "a rotation with several axes needs positions");
   CHECK(check_cache(cache));
   if (!start) return fail(SPLAT_ERR_INVALID_ARG, "start is NULL");
   if (!kvq || (n != 2 && n != 4))
@@ -1029,7 +1052,8 @@ splat_status splat_cache_append(splat_rotary_t r, splat_dtype dtype, int32_t B, 
   }
   const Span ints[] = {{cache->table, (size_t)B * cache->max_pages * 4, "the cache's table"},
                        {start, (size_t)B * 4, "start"},
-                       {counts, (size_t)B * 4, "counts"}};
+                       {counts, (size_t)B * 4, "counts"},
+                       {positions, positions ? (size_t)r->host.axes * B * T * 4 : 0, "positions"}};
   for (const Span& c : own) {
     for (const View* x : {&k, &v, &q, &qr})
       if (x->x && meet(c.p, c.bytes, x->at(), x->extent()))
@@ -1048,7 +1072,7 @@ splat_status splat_cache_append(splat_rotary_t r, splat_dtype dtype, int32_t B, 
   for (int i = 0; i < 2; ++i) a.job[i].y = (char*)own[i].p, a.job[i].paged = true;
   if (Q) a.job[a.n_jobs++] = heads_job(q, &qr, r != nullptr);
   if (r) use_rotary(a, r);
-  a.first = start, a.counts = counts, a.pages = cache->table;
+  a.first = start, a.counts = counts, a.positions = positions, a.pages = cache->table;
   a.max_pages = (int32_t)cache->max_pages, a.n_pages = (int32_t)cache->n_pages;
   a.page_shift = log2_of(cache->page);
   return launched(splat::launch_heads(a, dtype, d, (hipStream_t)stream), "cache_append");

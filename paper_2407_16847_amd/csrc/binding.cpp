@@ -109,6 +109,11 @@ struct Call {
   const int32_t* ints(const Tensor& x, const char* name, at::IntArrayRef sizes) const {
     return (const int32_t*)want(x, name, at::kInt, sizes);
   }
+  // of the tokens of x [B, heads, T, d], as the rotation's axes ask for
+  const int32_t* positions(const Opt& p, int64_t axes, at::IntArrayRef x) const {
+    if (!p) return nullptr;
+    return axes > 1 ? ints(*p, "positions", {axes, x[0], x[2]}) : ints(*p, "positions", {x[0], x[2]});
+  }
   splat_cache cache(const Tensor& k, const Tensor& v, const Tensor& table, int64_t B, int64_t d) const {
     on_gpu(k, "k_cache");
     if (k.dim() != 4 || k.size(3) != d)
@@ -178,7 +183,7 @@ py::tuple bwd(int64_t handle, const Tensor& Q, const Tensor& K, const Tensor& V,
 }
 
 py::object rotary(int64_t handle, const Tensor& X, const Opt& X2, const Opt& positions, bool inverse,
-                  const Opt& Y, const Opt& Y2, int64_t device, int64_t stream) {
+                  const Opt& Y, const Opt& Y2, int64_t axes, int64_t device, int64_t stream) {
   const Call c(X, "X", device, stream);
   const auto s = X.sizes();
   if (!X2 && Y2) value_error("Y2 needs X2");
@@ -190,7 +195,7 @@ py::object rotary(int64_t handle, const Tensor& X, const Opt& X2, const Opt& pos
     xy[2] = c.heads(*X2, "X2", s);
     xy[3] = c.turned(*X2, Y2, "Y2", y[1]);
   }
-  const int32_t* const pos = positions ? c.ints(*positions, "positions", {s[0], s[2]}) : nullptr;
+  const int32_t* const pos = c.positions(positions, axes, s);
   check(splat_rotary_apply(rotary_of(handle), c.dtype(), s[0], s[2], s[3], pos, xy, X2 ? 2 : 1,
                            inverse, c.stream));
   written({given(Y), given(Y2)});
@@ -200,7 +205,8 @@ py::object rotary(int64_t handle, const Tensor& X, const Opt& X2, const Opt& pos
 
 py::object cache_append(int64_t rot, const Tensor& k_cache, const Tensor& v_cache, const Tensor& table,
                         const Tensor& start, const Tensor& K, const Tensor& V, const Opt& counts,
-                        const Opt& Q, const Opt& Qr, int64_t device, int64_t stream) {
+                        const Opt& Q, const Opt& Qr, const Opt& positions, int64_t axes,
+                        int64_t device, int64_t stream) {
   const Call c(K, "K", device, stream);
   const auto s = K.sizes();
   if (!Q && Qr) value_error("Qr needs Q");
@@ -211,12 +217,13 @@ py::object cache_append(int64_t rot, const Tensor& k_cache, const Tensor& v_cach
   const splat_cache cache = c.cache(k_cache, v_cache, table, s[0], s[3]);
   const int32_t* const at = c.ints(start, "start", {s[0]});
   const int32_t* const n = counts ? c.ints(*counts, "counts", {s[0]}) : nullptr;
+  const int32_t* const pos = c.positions(positions, axes, s);
   if (Q) {
     kvq[2] = c.heads(*Q, "Q", s);
     kvq[3] = c.turned(*Q, Qr, "Qr", q);
   }
-  check(splat_cache_append(rotary_of(rot), c.dtype(), s[0], s[2], s[3], &cache, at, n, kvq, Q ? 4 : 2,
-                           c.stream));
+  check(splat_cache_append_at(rotary_of(rot), c.dtype(), s[0], s[2], s[3], &cache, at, n, pos, kvq,
+                              Q ? 4 : 2, c.stream));
   written({&k_cache, &v_cache, given(Qr)});
   if (!Q) return py::none();
   return py::cast(q);

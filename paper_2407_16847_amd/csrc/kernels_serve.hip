@@ -5,6 +5,7 @@
 
 #include <algorithm>
 
+#include "../../include/splat.h"
 #include "serve_core.hpp"
 #include "slice_ops.hpp"
 
@@ -41,7 +42,8 @@ struct Chunk<__bf16> {
   typedef bf16x8_t vec_t;
 };
 
-template <typename T, int D, bool INTER>
+// Several axes (AXES): each pair's angle stands in its axis's row of the table.
+template <typename T, int D, bool INTER, bool AXES>
 __global__ __launch_bounds__(kThreads) void k_heads(const HeadsArgs x, int per_block) {
   constexpr int E = Chunk<T>::E, U = D / (2 * E), TB = kThreads / U;
   using vec_t = typename Chunk<T>::vec_t;
@@ -49,7 +51,7 @@ __global__ __launch_bounds__(kThreads) void k_heads(const HeadsArgs x, int per_b
   const int64_t n = (int64_t)blockIdx.x * TB + threadIdx.x / U;
   if (n >= (int64_t)x.B * x.T) return;
   const int b = (int)(n / x.T), t = (int)(n - (int64_t)b * x.T);
-  const int64_t pos = x.positions ? x.positions[n] : (int64_t)(x.first ? x.first[b] : 0) + t;
+  const int64_t place = (int64_t)(x.first ? x.first[b] : 0) + t;
   const bool counts = !x.counts || t < x.counts[b];
 
   // where the unit's chunks lie, and its turn
@@ -57,7 +59,22 @@ __global__ __launch_bounds__(kThreads) void k_heads(const HeadsArgs x, int per_b
   const int c0 = (turns && !INTER ? u * E : 2 * u * E) * (int)sizeof(T);
   const int step = (turns && !INTER ? x.rot / 2 : E) * (int)sizeof(T);
   float co[E], si[E];
-  if (turns) {
+  if (AXES && turns) {
+    int at[SPLAT_ROTARY_MAX_AXES];
+#pragma unroll
+    for (int a = 0; a < SPLAT_ROTARY_MAX_AXES; ++a)
+      at[a] = x.positions[(int64_t)min(a, x.axes - 1) * x.B * x.T + n];
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const int a = x.axis[u * E + e];
+      const int pos = a == 0 ? at[0] : a == 1 ? at[1] : a == 2 ? at[2] : at[3];
+      const bool inside = pos >= 0 && pos < x.max_len;
+      const f32x2_t v = *(const f32x2_t*)(x.angles + (int64_t)(inside ? pos : 0) * (x.rot / 2) + u * E + e);
+      co[e] = inside ? v[0] : NAN, si[e] = inside ? (x.inverse ? -v[1] : v[1]) : NAN;
+    }
+  }
+  if (!AXES && turns) {
+    const int64_t pos = x.positions ? x.positions[n] : place;
     const bool inside = pos >= 0 && pos < x.max_len;
     const f32x4_t* a = (const f32x4_t*)(x.angles + (inside ? pos : 0) * (x.rot / 2) + u * E);
 #pragma unroll
@@ -73,7 +90,7 @@ __global__ __launch_bounds__(kThreads) void k_heads(const HeadsArgs x, int per_b
   }
   // the token's page in the cache, -1 if it has none
   const int page =
-      x.pages && counts ? page_of(x.pages, b, x.max_pages, x.n_pages, x.page_shift, pos) : -1;
+      x.pages && counts ? page_of(x.pages, b, x.max_pages, x.n_pages, x.page_shift, place) : -1;
 
   // blockIdx.y: a run of one tensor's heads
   int j = 0, run = blockIdx.y;
@@ -86,7 +103,7 @@ __global__ __launch_bounds__(kThreads) void k_heads(const HeadsArgs x, int per_b
   int64_t next = job.yh;                // to the next head
   if (job.paged) {
     if (page < 0) return;
-    to += (size_t)cache_row(page, job.heads, first, x.page_shift, pos) * (D * sizeof(T));
+    to += (size_t)cache_row(page, job.heads, first, x.page_shift, place) * (D * sizeof(T));
     next = ((int64_t)D * (int)sizeof(T)) << x.page_shift;
   } else {
     to += b * job.yb + t * job.yt + first * job.yh;
@@ -142,10 +159,9 @@ hipError_t heads_launch(const HeadsArgs& x, hipStream_t st) {
   int64_t runs = 0;
   for (int k = 0; k < x.n_jobs; ++k) runs += (x.job[k].heads + per - 1) / per;
   const dim3 grid((unsigned)blocks, (unsigned)runs);
-  if (x.interleaved)
-    hipLaunchKernelGGL((k_heads<T, D, true>), grid, dim3(kThreads), 0, st, x, (int)per);
-  else
-    hipLaunchKernelGGL((k_heads<T, D, false>), grid, dim3(kThreads), 0, st, x, (int)per);
+  auto* const k = x.axis ? (x.interleaved ? k_heads<T, D, true, true> : k_heads<T, D, false, true>)
+                         : (x.interleaved ? k_heads<T, D, true, false> : k_heads<T, D, false, false>);
+  hipLaunchKernelGGL(k, grid, dim3(kThreads), 0, st, x, (int)per);
   return hipGetLastError();
 }
 

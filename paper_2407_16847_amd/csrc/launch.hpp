@@ -131,7 +131,9 @@ struct HeadsArgs {
   const float2* angles;       // [max_len, rot / 2] (cosine, sine)
   int32_t max_len, rot;       // rot 0: nothing turns
   bool interleaved, inverse;
-  const int32_t* positions;   // [B, T], or null: first[b] + t (first null: t)
+  const uint8_t* axis;        // [rot / 2] each pair's axis, or null: one axis
+  int32_t axes;
+  const int32_t* positions;   // [axes, B, T], or null: first[b] + t (first null: t)
   const int32_t* first;
   const int32_t* counts;      // tokens of each sequence that count, or null: all
   const int32_t* pages;       // [B, max_pages]
