@@ -616,6 +616,28 @@ splat_status splat_sparse_mhsa_decode(splat_acsr_t h, splat_dtype dtype, int32_t
                                       void* stream);
 
 /*
+ * splat_cache_evict -- brings sequences of more than `budget` tokens back to it.  Of
+ * each head of the cache the first `first` and the last `recent` places stay and, of those
+ * between, the ones of largest weight (equal weights: the lowest place), budget in all; the
+ * weights are fp32 [n_pages, heads, page], paged as the cache is.  They keep their order
+ * and become places 0 .. budget - 1, the heads each for themselves, K, V and the
+ * weight; of a sequence of at most `budget` tokens all places stay.
+ * kept: int32 [B, heads, budget], the places that stayed, ascending, -1 behind the
+ * last.  left: int32 [B], the new lengths.
+ * to: int32 [B, max_to], the pages that the tokens move to, of the same cache; none of
+ * them is a page that the call's tables name in `table` or name twice (shared pages
+ * stay as they were).  NULL: in place, and then no two sequences share a page below
+ * their lengths.  A token without a page in either table is not moved, and its weight counts as
+ * less than any other; NaN counts as the largest.  A length outside [0, SPLAT_MAX_L] or past the
+ * table: nothing moves, left = -1.  Bits are moved, not rounded.  The weights, kept and left share no
+ * memory with another argument (INVALID_ARG).
+ */
+splat_status splat_cache_evict(splat_dtype dtype, int32_t B, int32_t d, const splat_cache* cache,
+                               float* weights, const int32_t* lengths, int32_t budget, int32_t first,
+                               int32_t recent, const int32_t* to, int32_t max_to, int32_t* kept,
+                               int32_t* left, void* stream);
+
+/*
  * splat_debug_bounds -- index checks of a checked build (built with
  * -DSPLAT_DEBUG_BOUNDS: libsplat_checked.so beside libsplat.so; a debugging
  * aid, not part of the method).  In a checked build every kernel checks the

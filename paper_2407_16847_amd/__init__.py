@@ -29,7 +29,7 @@ __all__ = [
     "sparse_mhsa_fwd", "MAX_RUNS", "MAX_TERMS", "PLAN_NO_SPAN", "NO_SPAN_MAX_L", "PLAN_COLUMNS",
     "DENSE_ALPHA", "transpose_colmajor", "rspmm_colmajor", "sparse_mhsa_unfused",
     "sparse_mhsa_fwd_lse", "sparse_mhsa_bwd", "PLAN_GRAD", "Rotary", "rotary", "cache_append",
-    "sparse_mhsa_decode", "decode_workspace",
+    "sparse_mhsa_decode", "decode_workspace", "cache_evict",
 ]
 
 MAX_TERMS = 8
@@ -156,6 +156,7 @@ def _open(path: str) -> ctypes.CDLL:
         "splat_cache_append_at": [vp, i32, i32, i32, i32, vp, vp, vp, vp, vp, i32, vp],
         "splat_decode_workspace": [vp, i32, i32, i32, i32, P(i64)],
         "splat_sparse_mhsa_decode": [vp, i32, i32, i32, i32, vp, vp, vp, f32, vp, vp, vp],
+        "splat_cache_evict": [i32, i32, i32, vp, vp, vp, i32, i32, i32, vp, i32, vp, vp, vp],
         "splat_sparse_mhsa_unfused_noalloc": [vp, i32, i32, i32, i32, vp, vp, vp, f32, vp, i32, f32,
                                               P(i32), vp],
         "splat_acsr_export_csc": [vp, vp, vp],
@@ -720,6 +721,20 @@ def sparse_mhsa_decode(acsr: Acsr, Q: torch.Tensor, k_cache: torch.Tensor, v_cac
     the call unless given."""
     return native().decode(acsr.handle.value, Q, k_cache, v_cache, table, lengths, scale, O, workspace,
                            *_where())
+
+
+def cache_evict(k_cache: torch.Tensor, v_cache: torch.Tensor, weights: torch.Tensor, table: torch.Tensor,
+                lengths: torch.Tensor, budget: int, *, first: int = 0, recent: int = 0,
+                to: Optional[torch.Tensor] = None, kept: Optional[torch.Tensor] = None,
+                left: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Brings sequences of more than `budget` tokens back to it: each head of the
+    cache keeps its first `first` and last `recent` places and the heaviest between
+    (weights fp32 [pages, heads, page]; equal ones: the lowest place), in their
+    order, as places 0 .. budget - 1.  to: int32 [B, pages], the free pages that they
+    move to; without it they move in place.  Returns (kept int32 [B, heads, budget],
+    the places that stayed, -1 behind the last; left int32 [B], the new lengths)."""
+    return native().cache_evict(k_cache, v_cache, weights, table, lengths, operator.index(budget),
+                                operator.index(first), operator.index(recent), to, kept, left, *_where())
 
 
 def _values(x: torch.Tensor, name: str, acsr: Acsr, B: int, H: int) -> None:

@@ -1125,6 +1125,54 @@ splat_status splat_sparse_mhsa_decode(splat_acsr_t h, splat_dtype dtype, int32_t
                   "sparse_mhsa_decode");
 }
 
+splat_status splat_cache_evict(splat_dtype dtype, int32_t B, int32_t d, const splat_cache* cache,
+                               float* weights, const int32_t* lengths, int32_t budget, int32_t first,
+                               int32_t recent, const int32_t* to, int32_t max_to, int32_t* kept,
+                               int32_t* left, void* stream) {
+  CHECK(check_dtype(dtype, "dtype"));
+  CHECK(check_d(d));
+  CHECK(check_cache(cache));
+  if (B < 1 || B * cache->heads > 65535)
+    return fail(SPLAT_ERR_INVALID_ARG, "B and the cache's heads must have B >= 1 and B*heads <= 65535");
+  if (budget < 1 || budget > SPLAT_MAX_L)
+    return fail(SPLAT_ERR_INVALID_ARG, "budget must be in [1, %d], got %d", SPLAT_MAX_L, budget);
+  if (first < 0 || recent < 0 || (int64_t)first + recent > budget)
+    return fail(SPLAT_ERR_INVALID_ARG, "first and recent must be 0 or more and at most the budget in all");
+  if (!lengths) return fail(SPLAT_ERR_INVALID_ARG, "lengths is NULL");
+  if (to && max_to < 1) return fail(SPLAT_ERR_INVALID_ARG, "max_to must be 1 or more");
+  if (to && (int64_t)max_to * cache->page < std::min<int64_t>(budget, cache->max_pages * cache->page))
+    return fail(SPLAT_ERR_INVALID_ARG, "the pages to move to hold less than the budget");
+  const size_t rows = (size_t)cache->n_pages * cache->heads * cache->page;
+  const size_t bytes = rows * d * (dtype == SPLAT_BF16 ? 2 : 4);
+  const Span in[] = {{cache->table, (size_t)B * cache->max_pages * 4, "the cache's table"},
+                     {lengths, (size_t)B * 4, "lengths"},
+                     {to, to ? (size_t)B * max_to * 4 : 0, "to"}};
+  const Span out[] = {{cache->k, bytes, "the cache's k"},
+                      {cache->v, bytes, "the cache's v"},
+                      {weights, rows * 4, "weights"},
+                      {kept, (size_t)B * cache->heads * budget * 4, "kept"},
+                      {left, (size_t)B * 4, "left"}};
+  for (int k = 2; k < 5; ++k)
+    if (!out[k].p || (uintptr_t)out[k].p % 4 != 0)
+      return fail(SPLAT_ERR_INVALID_ARG, "%s must be device memory at 4 bytes", out[k].name);
+  for (int k = 0; k < 5; ++k) {
+    for (const Span& i : in)
+      if (meet(out[k].p, out[k].bytes, i.p, i.bytes))
+        return fail(SPLAT_ERR_INVALID_ARG, "%s must not overlap %s", out[k].name, i.name);
+    for (int i = 0; i < k; ++i)
+      if (meet(out[k].p, out[k].bytes, out[i].p, out[i].bytes))
+        return fail(SPLAT_ERR_INVALID_ARG, "%s must not overlap %s", out[k].name, out[i].name);
+  }
+  splat::EvictArgs x{};
+  x.k = (char*)cache->k, x.v = (char*)cache->v, x.w = weights;
+  x.pages = cache->table, x.to = to, x.lengths = lengths, x.kept = kept, x.left = left;
+  x.B = B, x.heads = (int32_t)cache->heads, x.max_pages = (int32_t)cache->max_pages, x.max_to = max_to;
+  x.n_pages = (int32_t)cache->n_pages, x.page_shift = log2_of(cache->page);
+  x.budget = budget, x.first = first, x.recent = recent;
+  return launched(splat::launch_evict(x, d * (dtype == SPLAT_BF16 ? 2 : 4), (hipStream_t)stream),
+                  "cache_evict");
+}
+
 splat_status splat_sparse_mhsa_unfused(splat_acsr_t h, splat_dtype dtype, int32_t B, int32_t H,
                                        int32_t d, const void* Q, const void* K, const void* V,
                                        float scale, float* S, float* Pt, void* O,

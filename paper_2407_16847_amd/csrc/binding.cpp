@@ -259,6 +259,38 @@ Tensor decode(int64_t handle, const Tensor& Q, const Tensor& k_cache, const Tens
   return O;
 }
 
+py::tuple cache_evict(const Tensor& k_cache, const Tensor& v_cache, const Tensor& weights,
+                      const Tensor& table, const Tensor& lengths, int64_t budget, int64_t first,
+                      int64_t recent, const Opt& to, const Opt& kept_, const Opt& left_, int64_t device,
+                      int64_t stream) {
+  const Call c(k_cache, "k_cache", device, stream);
+  if (table.dim() != 2) value_error("table must be [B, max_pages], got " + text(table.sizes()));
+  const int64_t B = table.size(0), heads = k_cache.size(1);
+  const splat_cache cache = c.cache(k_cache, v_cache, table, B, k_cache.size(3));
+  float* const w = (float*)c.want(weights, "weights", at::kFloat, k_cache.sizes().slice(0, 3));
+  const int32_t* const n = c.ints(lengths, "lengths", {B});
+  for (int64_t x : {B, budget, first, recent})
+    if (x < 0 || x > INT32_MAX)
+      value_error("B, budget, first and recent must be 0 or more and fit 32 bits");
+  const int32_t* dst = nullptr;
+  int64_t max_to = 0;
+  if (to) {
+    if (to->dim() != 2 || to->size(1) > INT32_MAX)
+      value_error("to must be [B, max_to], got " + text(to->sizes()));
+    max_to = to->size(1);
+    dst = c.ints(*to, "to", {B, max_to});
+    if (max_to == 0) value_error("to has no pages");
+  }
+  // what the call itself refuses needs no memory
+  const int64_t most = budget <= SPLAT_MAX_L ? budget : 0;
+  const Tensor kept = c.out(kept_, "kept", at::kInt, {B, heads, most}, k_cache);
+  const Tensor left = c.out(left_, "left", at::kInt, {B}, k_cache);
+  check(splat_cache_evict(c.dtype(), B, k_cache.size(3), &cache, w, n, budget, first, recent, dst, max_to,
+                          (int32_t*)kept.data_ptr(), (int32_t*)left.data_ptr(), c.stream));
+  written({&k_cache, &v_cache, &weights, given(kept_), given(left_)});
+  return py::make_tuple(kept, left);
+}
+
 }  // namespace
 
 PYBIND11_MODULE(_native, m) {
@@ -267,4 +299,5 @@ PYBIND11_MODULE(_native, m) {
   m.def("rotary", &rotary);
   m.def("cache_append", &cache_append);
   m.def("decode", &decode);
+  m.def("cache_evict", &cache_evict);
 }

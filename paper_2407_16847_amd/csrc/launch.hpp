@@ -155,6 +155,17 @@ int64_t decode_workspace(const DevAcsr& a, int B, int H, int heads, int d);
 hipError_t launch_decode(const DevAcsr& a, int dtype, int d, const DecodeArgs& x, hipStream_t st);
 hipError_t prepare_decode();
 
+// A cache brought back to a budget.  to: the pages that the kept keys move to, or
+// null: in place.
+struct EvictArgs {
+  char *k, *v;
+  float* w;                   // [n_pages, heads, page]
+  const int32_t *pages, *to, *lengths;
+  int32_t *kept, *left;       // [B, heads, budget], [B]
+  int32_t B, heads, max_pages, max_to, n_pages, page_shift, budget, first, recent;
+};
+hipError_t launch_evict(const EvictArgs& x, int row_bytes, hipStream_t st);
+
 // Allows the fused kernels their dynamic LDS (above the default limit at
 // d = 128) on the current device.  Called once per handle at build time, on
 // the handle's device, so launches never change kernel attributes.
