@@ -616,6 +616,32 @@ splat_status splat_sparse_mhsa_decode(splat_acsr_t h, splat_dtype dtype, int32_t
                                       void* stream);
 
 /*
+ * splat_sparse_mhsa_chunk -- the attention of a chunk of new tokens a sequence over
+ * the paged cache, which already holds them: sequence b has lengths[b] tokens, of which the
+ * last counts[b] (NULL: T) are the chunk's; token t of them has the mask's row
+ * lengths[b] - counts[b] + t, of which the columns below lengths[b] count.  So a
+ * chunk of one token is splat_sparse_mhsa_decode, and one of a whole sequence of L tokens the
+ * fused forward.  q, o: [B, H, T, d] of `dtype` by their strides; lse: fp32 [B, H, T], the rows'
+ * log-sum-exp.  H is a multiple of the cache's heads: query head h reads head
+ * h / (H / heads).  A row without columns: O = 0, lse = -inf, and so in the rows of
+ * padding (t >= counts[b]; a count is taken into [0, T]).  A length below the count,
+ * above L or past the table: NaN in the rows of that sequence that are not padding.  A row
+ * with a key whose page lies outside [0, n_pages): NaN.  Only a row's own keys
+ * count, whatever the others hold; a row whose scores are all -inf gets NaN (and lse -inf).
+ * Scores, softmax and sums in fp32 in a fixed order, one rounding of O; for blocks of
+ * many bf16 rows the probabilities are rounded to nearest even bf16 before they meet V.
+ * O and lse share no memory with the inputs or each other (INVALID_ARG).
+ * workspace: splat_chunk_workspace() bytes, 16-byte aligned, that the call writes
+ * and reads (calls that may run at the same time need one each); NULL if 0.
+ */
+splat_status splat_chunk_workspace(splat_acsr_t h, splat_dtype dtype, int32_t B, int32_t H,
+                                   int32_t heads, int32_t T, int32_t d, int64_t* bytes);
+splat_status splat_sparse_mhsa_chunk(splat_acsr_t h, splat_dtype dtype, int32_t B, int32_t T, int32_t d,
+                                     const splat_heads* q, const splat_cache* cache,
+                                     const int32_t* lengths, const int32_t* counts, float scale,
+                                     const splat_heads* o, float* lse, void* workspace, void* stream);
+
+/*
  * splat_cache_evict -- brings sequences of more than `budget` tokens back to it.  Of
  * each head of the cache the first `first` and the last `recent` places stay and, of those
  * between, the ones of largest weight (equal weights: the lowest place), budget in all; the

@@ -29,7 +29,8 @@ __all__ = [
     "sparse_mhsa_fwd", "MAX_RUNS", "MAX_TERMS", "PLAN_NO_SPAN", "NO_SPAN_MAX_L", "PLAN_COLUMNS",
     "DENSE_ALPHA", "transpose_colmajor", "rspmm_colmajor", "sparse_mhsa_unfused",
     "sparse_mhsa_fwd_lse", "sparse_mhsa_bwd", "PLAN_GRAD", "Rotary", "rotary", "cache_append",
-    "sparse_mhsa_decode", "decode_workspace", "cache_evict",
+    "sparse_mhsa_decode", "decode_workspace", "sparse_mhsa_chunk", "chunk_workspace",
+    "cache_evict",
 ]
 
 MAX_TERMS = 8
@@ -156,6 +157,8 @@ def _open(path: str) -> ctypes.CDLL:
         "splat_cache_append_at": [vp, i32, i32, i32, i32, vp, vp, vp, vp, vp, i32, vp],
         "splat_decode_workspace": [vp, i32, i32, i32, i32, P(i64)],
         "splat_sparse_mhsa_decode": [vp, i32, i32, i32, i32, vp, vp, vp, f32, vp, vp, vp],
+        "splat_chunk_workspace": [vp, i32, i32, i32, i32, i32, i32, P(i64)],
+        "splat_sparse_mhsa_chunk": [vp, i32, i32, i32, i32, vp, vp, vp, vp, f32, vp, vp, vp, vp],
         "splat_cache_evict": [i32, i32, i32, vp, vp, vp, i32, i32, i32, vp, i32, vp, vp, vp],
         "splat_sparse_mhsa_unfused_noalloc": [vp, i32, i32, i32, i32, vp, vp, vp, f32, vp, i32, f32,
                                               P(i32), vp],
@@ -721,6 +724,31 @@ def sparse_mhsa_decode(acsr: Acsr, Q: torch.Tensor, k_cache: torch.Tensor, v_cac
     the call unless given."""
     return native().decode(acsr.handle.value, Q, k_cache, v_cache, table, lengths, scale, O, workspace,
                            *_where())
+
+
+def chunk_workspace(acsr: Acsr, dtype: torch.dtype, B: int, H: int, heads: int, T: int, d: int) -> int:
+    """Bytes of workspace that sparse_mhsa_chunk takes (0: none)."""
+    n = ctypes.c_int64()
+    _check(acsr._lib.splat_chunk_workspace(acsr.handle, _DT[dtype], _int32(B, "B"), _int32(H, "H"),
+                                           _int32(heads, "heads"), _int32(T, "T"), _int32(d, "d"),
+                                           ctypes.byref(n)))
+    return n.value
+
+
+def sparse_mhsa_chunk(acsr: Acsr, Q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor,
+                      table: torch.Tensor, lengths: torch.Tensor, scale: float, *,
+                      counts: Optional[torch.Tensor] = None, O: Optional[torch.Tensor] = None,
+                      lse: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None
+                      ) -> Tuple[torch.Tensor, torch.Tensor]:
+    """A chunk of T new tokens a sequence, Q [B, H, T, d] (any strides, contiguous
+    features), over the paged cache that already holds them: the last counts[b]
+    (default T; int32 [B]) of sequence b's lengths[b] tokens are the chunk's, token t
+    of them has the mask's row lengths[b] - counts[b] + t, its columns below
+    lengths[b].  The cache's heads divide H.  Returns (O in the inputs' dtype, lse
+    fp32 [B, H, T]); rows of padding have 0 and -inf.  workspace: at least
+    chunk_workspace() bytes, made by the call unless given."""
+    return native().chunk(acsr.handle.value, Q, k_cache, v_cache, table, lengths, scale, counts, O, lse,
+                          workspace, *_where())
 
 
 def cache_evict(k_cache: torch.Tensor, v_cache: torch.Tensor, weights: torch.Tensor, table: torch.Tensor,

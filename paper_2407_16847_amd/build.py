@@ -29,7 +29,7 @@ ARCH = "gfx950"
 
 SOURCES = ["acsr_host.cpp", "tiling.cpp", "rotary_host.cpp", "api.hip", "kernels_mfma.hip", "kernels_tiles.hip",
            "kernels_slices.hip", "kernels_grad.hip", "kernels_grad_tiles.hip",
-           "kernels_serve.hip", "kernels_evict.hip"]
+           "kernels_serve.hip", "kernels_evict.hip", "kernels_chunk.hip"]
 
 COMMON = ["-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function", "-Wno-unknown-pragmas"]
 # Packed fp32 instructions stay off: plain float code must not be turned into

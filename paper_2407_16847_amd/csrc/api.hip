@@ -107,6 +107,8 @@ splat_status upload(splat_acsr* h) {
     return fail(SPLAT_ERR_HIP, "hipFuncSetAttribute (fused kernel LDS): %s", hipGetErrorString(e));
   if ((e = splat::prepare_decode()) != hipSuccess)
     return fail(SPLAT_ERR_HIP, "hipFuncSetAttribute (decode kernel LDS): %s", hipGetErrorString(e));
+  if ((e = splat::prepare_chunk()) != hipSuccess)
+    return fail(SPLAT_ERR_HIP, "hipFuncSetAttribute (chunk kernels' LDS): %s", hipGetErrorString(e));
   if (h->host.has_grad && (e = splat::prepare_bwd()) != hipSuccess)
     return fail(SPLAT_ERR_HIP, "hipFuncSetAttribute (backward kernels' LDS): %s",
                 hipGetErrorString(e));
@@ -1125,6 +1127,75 @@ splat_status splat_sparse_mhsa_decode(splat_acsr_t h, splat_dtype dtype, int32_t
                   "sparse_mhsa_decode");
 }
 
+splat_status splat_chunk_workspace(splat_acsr_t h, splat_dtype dtype, int32_t B, int32_t H,
+                                   int32_t heads, int32_t T, int32_t d, int64_t* bytes) {
+  if (!h || !bytes) return fail(SPLAT_ERR_INVALID_ARG, "handle and bytes must be non-NULL");
+  CHECK(check_batch(B, H));
+  CHECK(check_dtype(dtype, "dtype"));
+  CHECK(check_d(d));
+  if (heads < 1 || H % heads != 0)
+    return fail(SPLAT_ERR_INVALID_ARG, "H must be a multiple of the cache's heads (got %d, %d)", H, heads);
+  CHECK(check_tokens(B, T));
+  // rows are counted in 32 bits, and a wavefront may take each
+  if ((int64_t)B * H * T > (1 << 24))
+    return fail(SPLAT_ERR_UNSUPPORTED, "B*H*T must be at most 2^24 (got %lld)", (long long)B * H * T);
+  *bytes = splat::chunk_workspace(splat::chunk_shape(h->dev, dtype, B, H, heads, T, d), B, H, T, d) * 4;
+  return ok();
+}
+
+splat_status splat_sparse_mhsa_chunk(splat_acsr_t h, splat_dtype dtype, int32_t B, int32_t T, int32_t d,
+                                     const splat_heads* q, const splat_cache* cache,
+                                     const int32_t* lengths, const int32_t* counts, float scale,
+                                     const splat_heads* o, float* lse, void* workspace, void* stream) {
+  if (!q || !o) return fail(SPLAT_ERR_INVALID_ARG, "q and o must be non-NULL");
+  const int32_t H = int32_of(q->heads);
+  CHECK(check_handle(h, B, H));
+  CHECK(check_cache(cache));
+  int64_t need = 0;
+  const int32_t heads = (int32_t)cache->heads;
+  CHECK(splat_chunk_workspace(h, dtype, B, H, heads, T, d, &need));
+  if (!lengths) return fail(SPLAT_ERR_INVALID_ARG, "lengths is NULL");
+  const int32_t e = dtype == SPLAT_BF16 ? 2 : 4;
+  const View qv{q, "q", B, T, d, e}, ov{o, "o", B, T, d, e};
+  CHECK(check_view(qv, false));
+  CHECK(check_view(ov, true));
+  if (o->heads != q->heads) return fail(SPLAT_ERR_INVALID_ARG, "q and o differ in heads");
+  if (!lse || (uintptr_t)lse % 4 != 0)
+    return fail(SPLAT_ERR_INVALID_ARG, "lse must be device memory at 4 bytes");
+  if (need > 0) CHECK(check_ptr(workspace, "workspace"));
+  const size_t bytes = (size_t)cache->n_pages * cache->heads * cache->page * d * e;
+  CHECK(check_apart(ov, qv));
+  const Span in[] = {{cache->k, bytes, "the cache's k"},
+                     {cache->v, bytes, "the cache's v"},
+                     {cache->table, (size_t)B * cache->max_pages * 4, "the cache's table"},
+                     {lengths, (size_t)B * 4, "lengths"},
+                     {counts, (size_t)B * 4, "counts"}};
+  const Span out[] = {{ov.at(), (size_t)ov.extent(), "o"},
+                      {lse, (size_t)B * H * T * 4, "lse"},
+                      {need > 0 ? workspace : nullptr, (size_t)need, "workspace"}};
+  for (int k = 0; k < 3; ++k) {
+    for (const Span& i : in)
+      if (meet(out[k].p, out[k].bytes, i.p, i.bytes))
+        return fail(SPLAT_ERR_INVALID_ARG, "%s must not overlap %s", out[k].name, i.name);
+    if (k > 0 && meet(out[k].p, out[k].bytes, qv.at(), qv.extent()))
+      return fail(SPLAT_ERR_INVALID_ARG, "%s must not overlap q", out[k].name);
+    for (int i = 0; i < k; ++i)
+      if (meet(out[k].p, out[k].bytes, out[i].p, out[i].bytes))
+        return fail(SPLAT_ERR_INVALID_ARG, "%s must not overlap %s", out[k].name, out[i].name);
+  }
+  const splat::ChunkShape s = splat::chunk_shape(h->dev, dtype, B, H, heads, T, d);
+  splat::ChunkArgs x{};
+  x.Q = q->data, x.K = cache->k, x.V = cache->v, x.O = o->data, x.lse = lse;
+  x.pages = cache->table, x.lengths = lengths, x.counts = counts;
+  x.qb = q->stride_b, x.qh = q->stride_h, x.qt = q->stride_t;
+  x.ob = o->stride_b, x.oh = o->stride_h, x.ot = o->stride_t;
+  x.B = B, x.H = H, x.heads = heads, x.group = H / heads, x.T = T;
+  x.max_pages = (int32_t)cache->max_pages, x.n_pages = (int32_t)cache->n_pages;
+  x.page_shift = log2_of(cache->page);
+  x.blocks = s.blocks, x.splits = s.splits, x.scale = scale, x.ws = (float*)workspace;
+  return launched(splat::launch_chunk(h->dev, dtype, d, x, (hipStream_t)stream), "sparse_mhsa_chunk");
+}
+
 splat_status splat_cache_evict(splat_dtype dtype, int32_t B, int32_t d, const splat_cache* cache,
                                float* weights, const int32_t* lengths, int32_t budget, int32_t first,
                                int32_t recent, const int32_t* to, int32_t max_to, int32_t* kept,
@@ -1253,6 +1324,7 @@ splat_status splat_debug_bounds(uint32_t* flags, int32_t clear) {
   if (e == hipSuccess) e = splat::bounds_collect_grad(&bits, clear != 0);
   if (e == hipSuccess) e = splat::bounds_collect_grad_tiles(&bits, clear != 0);
   if (e == hipSuccess) e = splat::bounds_collect_serve(&bits, clear != 0);
+  if (e == hipSuccess) e = splat::bounds_collect_chunk(&bits, clear != 0);
   if (e != hipSuccess) return fail(SPLAT_ERR_HIP, "splat_debug_bounds: %s", hipGetErrorString(e));
   *flags = bits;
   return SPLAT_OK;

@@ -87,6 +87,15 @@ struct Call {
     want(*x, name, t, sizes);
     return *x;
   }
+  // x as given, if it holds `need` bytes, or a new tensor where there is need
+  Tensor workspace(const Opt& x, int64_t need, const Tensor& like) const {
+    if (!x) return need ? at::empty({need / 4}, like.options().dtype(at::kFloat).requires_grad(false)) : Tensor();
+    on_gpu(*x, "workspace");
+    here(*x, "workspace");
+    if ((int64_t)x->nbytes() < need || !x->is_contiguous())
+      value_error("workspace must be contiguous and hold " + std::to_string(need) + " bytes");
+    return *x;
+  }
   // x [B, heads, T, d] by its strides
   splat_heads heads(const Tensor& x, const char* name, at::IntArrayRef like) const {
     on_gpu(x, name);
@@ -243,20 +252,33 @@ Tensor decode(int64_t handle, const Tensor& Q, const Tensor& k_cache, const Tens
   int64_t need = 0;
   check(splat_decode_workspace(h, s[0], s[1], (int32_t)std::min<int64_t>(cache.heads, INT32_MAX), s[3],
                                &need));
-  Tensor ws;
-  if (workspace) {
-    Call::on_gpu(*workspace, "workspace");
-    c.here(*workspace, "workspace");
-    if ((int64_t)workspace->nbytes() < need || !workspace->is_contiguous())
-      value_error("workspace must be contiguous and hold " + std::to_string(need) + " bytes");
-    ws = *workspace;
-  } else if (need) {
-    ws = at::empty({need / 4}, Q.options().dtype(at::kFloat).requires_grad(false));
-  }
+  const Tensor ws = c.workspace(workspace, need, Q);
   check(splat_sparse_mhsa_decode(h, c.dtype(), s[0], s[1], s[3], Q.data_ptr(), &cache, n, (float)scale,
                                  O.data_ptr(), need ? ws.data_ptr() : nullptr, c.stream));
   written({given(O_), need ? given(workspace) : nullptr});
   return O;
+}
+
+py::tuple chunk(int64_t handle, const Tensor& Q, const Tensor& k_cache, const Tensor& v_cache,
+                const Tensor& table, const Tensor& lengths, double scale, const Opt& counts,
+                const Opt& O_, const Opt& lse_, const Opt& workspace, int64_t device, int64_t stream) {
+  const Call c(Q, "Q", device, stream);
+  const splat_acsr_t h = acsr_of(handle);
+  const auto s = Q.sizes();
+  const splat_cache cache = c.cache(k_cache, v_cache, table, s[0], s[3]);
+  const int32_t* const n = c.ints(lengths, "lengths", {s[0]});
+  const int32_t* const m = counts ? c.ints(*counts, "counts", {s[0]}) : nullptr;
+  Tensor O;
+  const splat_heads q = c.heads(Q, "Q", s), o = c.turned(Q, O_, "O", O);
+  const Tensor lse = c.out(lse_, "lse", at::kFloat, s.slice(0, 3), Q);
+  int64_t need = 0;
+  check(splat_chunk_workspace(h, c.dtype(), s[0], s[1], (int32_t)std::min<int64_t>(cache.heads, INT32_MAX),
+                              s[2], s[3], &need));
+  const Tensor ws = c.workspace(workspace, need, Q);
+  check(splat_sparse_mhsa_chunk(h, c.dtype(), s[0], s[2], s[3], &q, &cache, n, m, (float)scale, &o,
+                                (float*)lse.data_ptr(), need ? ws.data_ptr() : nullptr, c.stream));
+  written({given(O_), given(lse_), need ? given(workspace) : nullptr});
+  return py::make_tuple(O, lse);
 }
 
 py::tuple cache_evict(const Tensor& k_cache, const Tensor& v_cache, const Tensor& weights,
@@ -299,5 +321,6 @@ PYBIND11_MODULE(_native, m) {
   m.def("rotary", &rotary);
   m.def("cache_append", &cache_append);
   m.def("decode", &decode);
+  m.def("chunk", &chunk);
   m.def("cache_evict", &cache_evict);
 }

@@ -1,0 +1,182 @@
+// chunk_plan.hpp -- which keys a block of consecutive mask rows needs, found by a
+// workgroup in LDS from the rows' runs.
+//
+// Keys are counted in words of 32 (a word is a unit of work).  A dense run covers whole words,
+// counted by their two ends and summed up, and leaves bits in the two at its rims; a strided run leaves
+// bits.  A word is then empty, full (every row has all its keys), partial, or, with at
+// most kSparseKeys bits and no whole cover, sparse.  Where that saves half of them at least,
+// the sparse words' keys are gathered into units of 32.
+#pragma once
+
+#include "../../include/splat.h"
+#include "slice_ops.hpp"
+
+namespace splat {
+namespace {
+
+constexpr int kSparseKeys = 8;
+constexpr uint32_t kFullUnit = 0x8000u;
+
+// bytes of LDS for masks of L rows: the words' bits and cover, later the gathered
+// keys and the units
+__host__ __device__ constexpr int plan_words(int L) { return (L + 31) / 32; }
+__host__ __device__ constexpr int plan_bytes(int L) { return (8 * plan_words(L) + 4 + 15) / 16 * 16; }
+
+struct RowsPlan {
+  const uint16_t* units;   // words of the key axis, kFullUnit set on full ones
+  const uint16_t* keys;    // gathered keys
+  int dense, gathered;     // units of words, keys gathered
+  __device__ __forceinline__ int n() const { return dense + (gathered + kUnit - 1) / kUnit; }
+};
+
+// 64-bit sums over the workgroup's threads before this one; `all`: the total.
+template <int THREADS>
+__device__ __forceinline__ uint64_t sums_before(uint64_t own, uint64_t* part, uint64_t& all) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  uint64_t sum = own;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const uint64_t y = __shfl_up((unsigned long long)sum, o, 64);
+    if (lane >= o) sum += y;
+  }
+  if (lane == 63) part[wave] = sum;
+  __syncthreads();
+  uint64_t before = 0;
+  all = 0;
+#pragma unroll
+  for (int w = 0; w < THREADS / 64; ++w) {
+    if (w < wave) before += part[w];
+    all += part[w];
+  }
+  return before + sum - own;
+}
+
+// Rows p0 .. p0 + nt - 1 of the mask, keys below len (0 < len <= L).  Called by the
+// whole workgroup; lds: plan_bytes(L); part: 2 * THREADS / 64 values.
+template <int THREADS>
+__device__ RowsPlan plan_rows(char* lds, uint64_t* part, int L, const RowRuns* runs, int p0, int nt,
+                              int len) {
+  constexpr int kMost = SPLAT_MAX_L / 32 / THREADS;     // words a thread
+  const int words = plan_words(L), W = (len + 31) >> 5, tid = threadIdx.x;
+  uint32_t* const bits = (uint32_t*)lds;
+  int* const cover = (int*)lds + words;
+  for (int i = tid; i < W; i += THREADS) bits[i] = 0;
+  for (int i = tid; i <= W; i += THREADS) cover[i] = 0;
+  __syncthreads();
+  for (int k = tid; k < nt * SPLAT_MAX_RUNS; k += THREADS) {
+    const int row = dbg::idx(p0 + k / SPLAT_MAX_RUNS, L, dbg::kRow), slot = k % SPLAT_MAX_RUNS;
+    const Run r = runs[row].r[slot];
+    if (r.count <= 0 || r.start >= len) continue;
+    if (r.stride == 1 || r.count == 1) {
+      const int s = r.start, e = imin(r.start + r.count - 1, len - 1);
+      const int ws = (s + 31) >> 5, we = (e + 1) >> 5;
+      if (ws < we) atomicAdd(&cover[ws], 1), atomicAdd(&cover[we], -1);
+      if (ws >= we && (s >> 5) == (e >> 5)) {
+        atomicOr(&bits[s >> 5], (~0u << (s & 31)) & (~0u >> (31 - (e & 31))));
+      } else {
+        if (s & 31) atomicOr(&bits[s >> 5], ~0u << (s & 31));
+        if ((e + 1) & 31) atomicOr(&bits[(e + 1) >> 5], (1u << ((e + 1) & 31)) - 1u);
+      }
+      continue;
+    }
+    // a run that the next row's continues is that one's to mark
+    if (row + 1 < p0 + nt) {
+      const Run q = runs[row + 1].r[slot];
+      if (q.start == r.start && q.stride == r.stride && q.count >= r.count) continue;
+    }
+    const int last = imin(r.start + r.stride * (r.count - 1), len - 1);
+    int word = r.start >> 5;
+    uint32_t have = 0;
+    for (int j = r.start; j <= last; j += r.stride) {
+      if (j >> 5 != word) {
+        atomicOr(&bits[word], have);
+        word = j >> 5, have = 0;
+      }
+      have |= 1u << (j & 31);
+    }
+    atomicOr(&bits[word], have);
+  }
+  __syncthreads();
+  // this thread's words
+  const int per = (W + THREADS - 1) / THREADS, w0 = tid * per;
+  uint32_t b[kMost];
+  int c[kMost], sum = 0;
+#pragma unroll
+  for (int i = 0; i < kMost; ++i) {
+    const bool in = i < per && w0 + i < W;
+    b[i] = in ? bits[w0 + i] : 0u;
+    c[i] = in ? cover[w0 + i] : 0;
+    sum += c[i];
+  }
+  uint64_t all;
+  int covered = (int)sums_before<THREADS>((uint64_t)(int64_t)sum, part, all);
+  // dense units, sparse words and their keys, 16 bits each
+  uint64_t own = 0;
+#pragma unroll
+  for (int i = 0; i < kMost; ++i) {
+    covered += c[i];
+    c[i] = covered;       // rows that have the whole word
+    const int n = __popc(b[i]);
+    if (i >= per || w0 + i >= W || (c[i] == 0 && n == 0)) {
+      c[i] = -1;
+    } else if (c[i] == 0 && n <= kSparseKeys) {
+      c[i] = -2;
+      own += (1ull << 16) + ((uint64_t)n << 32);
+    } else {
+      own += 1;
+    }
+  }
+  const uint64_t before = sums_before<THREADS>(own, part + THREADS / 64, all);
+  const int sparse = (int)(all >> 16 & 0xffff), keys = (int)(all >> 32);
+  const bool gather = keys <= 2 * words && 2 * ((keys + kUnit - 1) / kUnit) <= sparse;
+  // every thread has read its words (the barrier of the second sum): units and keys take their place
+  uint16_t* const to_units = (uint16_t*)cover;
+  uint16_t* const to_keys = (uint16_t*)bits;
+  int u = (int)(before & 0xffff) + (gather ? 0 : (int)(before >> 16 & 0xffff)), k = (int)(before >> 32);
+#pragma unroll
+  for (int i = 0; i < kMost; ++i) {
+    if (c[i] == -1) continue;
+    if (c[i] == -2 && gather) {
+      for (uint32_t x = b[i]; x; x &= x - 1) to_keys[k++] = (uint16_t)(32 * (w0 + i) + __ffs((int)x) - 1);
+    } else {
+      to_units[u++] = (uint16_t)((w0 + i) | (c[i] == nt ? kFullUnit : 0u));
+    }
+  }
+  __syncthreads();
+  RowsPlan plan;
+  plan.units = to_units, plan.keys = to_keys;
+  plan.dense = (int)(all & 0xffff) + (gather ? 0 : sparse);
+  plan.gathered = gather ? keys : 0;
+  return plan;
+}
+
+// A row's 16 keys of a gathered unit, as the scores' registers hold them: bit r is
+// key 8 (r / 4) + 4 h + r % 4 of the unit.
+__device__ __forceinline__ uint32_t gathered_bits(const RowRuns& rr, const uint16_t* keys, int n, int h) {
+  uint32_t bits = 0;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) {
+    const int k = 8 * (r >> 2) + 4 * h + (r & 3);
+    const int j = keys[imin(k, n - 1)];
+    bool in = false;
+#pragma unroll
+    for (int q = 0; q < SPLAT_MAX_RUNS; ++q) {
+      const Run run = rr.r[q];
+      const int off = j - run.start;
+      // a multiple's quotient, below 2^16, is exact to 2^-7 before it is rounded
+      const int t = (int)__builtin_rintf((float)off * __builtin_amdgcn_rcpf((float)run.stride));
+      in = in || (run.count > 0 && off >= 0 && t < run.count && t * run.stride == off);
+    }
+    bits |= (uint32_t)(in && k < n) << r;
+  }
+  return bits;
+}
+
+// A word's bits (bit k: key k) in the registers' order.
+__device__ __forceinline__ uint32_t register_bits(uint32_t word, int h) {
+  const uint32_t x = word >> (4 * h);
+  return (x & 0xf) | (x >> 4 & 0xf0) | (x >> 8 & 0xf00) | (x >> 12 & 0xf000);
+}
+
+}  // namespace
+}  // namespace splat

@@ -1,0 +1,404 @@
+// kernels_chunk.hip -- the attention of a chunk of new tokens over the paged cache.
+//
+// The chunk's n tokens are the last n of their sequence; token t has the mask's row
+// p = length - n + t and its columns below the length:
+//
+//     s_ij = scale q_i.k_j    lse_i = ln sum_j exp(s_ij)    O_i = sum_j exp(s_ij - lse_i) v_j
+//
+// The query heads that share a head of the cache are rows of one block, token by
+// token: row r of the sequence is token r / G, head r % G of the group of G.  A
+// workgroup finds the keys that its rows need (chunk_plan.hpp) and walks them in
+// units of 32.
+#include <hip/hip_runtime.h>
+#include <math.h>
+
+#include <algorithm>
+
+#include "chunk_plan.hpp"
+#include "serve_core.hpp"
+
+namespace splat {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+
+// One sequence's rows.
+struct Chunk {
+  int n, len, p0;     // tokens that count, the length, the first token's position
+  bool bad;           // a length that is none
+};
+__device__ __forceinline__ Chunk chunk_of(const ChunkArgs& x, int L, int b) {
+  Chunk c;
+  c.n = x.counts ? min(max(x.counts[b], 0), x.T) : x.T;
+  c.len = x.lengths[b];
+  c.bad = c.len < c.n || c.len > L || c.len > ((int64_t)x.max_pages << x.page_shift);
+  c.p0 = c.len - c.n;
+  return c;
+}
+
+// O and lse of one row by one wavefront, from the row's own keys alone.
+template <typename T, int D>
+__device__ __noinline__ void row_alone(const ChunkArgs& x, const RowRuns& rr, int b, int kh, int len,
+                                       const T* q, T* o, float* lse) {
+  constexpr int NC = D / 64;
+  const int lane = threadIdx.x & 63, n = count_lt(rr, len);
+  float m = -__FLT_MAX__, l = n > 0 ? 0.f : 1.f, acc[NC];
+  bool bad = false;
+#pragma unroll
+  for (int c = 0; c < NC; ++c) acc[c] = 0.f;
+#pragma unroll 1
+  for (int k0 = 0; k0 < n; k0 += 64) {
+    const bool valid = k0 + lane < n;
+    unsigned slot = 0;
+    float s = -INFINITY;
+    if (valid) {
+      const int j = col_of(rr, k0 + lane);
+      const int p = page_of(x.pages, b, x.max_pages, x.n_pages, x.page_shift, j);
+      bad = bad || p < 0;
+      slot = cache_row(max(p, 0), x.heads, kh, x.page_shift, j);
+      s = dense_dot<T, D>(q, (const T*)x.K + (size_t)slot * D) * x.scale;
+    }
+    const float mn = fmaxf(m, wave_max(s));
+    const float alpha = expf(m - mn), p = valid ? expf(s - mn) : 0.f;
+    l = l * alpha + wave_sum(p);
+#pragma unroll
+    for (int c = 0; c < NC; ++c) acc[c] *= alpha;
+#pragma unroll 1
+    for (int t = 0; t < min(64, n - k0); ++t) {
+      const float pt = __shfl(p, t, 64);
+      const T* const v = (const T*)x.V + (size_t)(unsigned)__shfl((int)slot, t, 64) * D;
+#pragma unroll
+      for (int c = 0; c < NC; ++c) acc[c] = fmaf(pt, (float)v[64 * c + lane], acc[c]);
+    }
+    m = mn;
+  }
+  if (__any(bad)) l = NAN;
+  // keys that all score -inf: 0 / 0, and lse -inf
+  if (lane == 0) *lse = n == 0 ? -INFINITY : m + logf(l);
+#pragma unroll
+  for (int c = 0; c < NC; ++c) store1(o + 64 * c + lane, acc[c] / l);
+}
+
+template <typename T, int D>
+__device__ __forceinline__ void redo_row(const ChunkArgs& x, const RowRuns* runs, int L, int b, int kh,
+                                         const Chunk& c, int t, int g) {
+  const int head = kh * x.group + g;
+  const RowRuns rr = runs[dbg::idx(c.p0 + t, L, dbg::kRow)];
+  row_alone<T, D>(x, rr, b, kh, c.len, (const T*)x.Q + b * x.qb + head * x.qh + t * x.qt,
+                  (T*)x.O + b * x.ob + head * x.oh + t * x.ot,
+                  x.lse + ((int64_t)b * x.H + head) * x.T + t);
+}
+
+// ------------------------------------------------------------------ slices
+// A workgroup per 32 rows; its wavefronts take every fourth unit of the rows' keys
+// and join at the end, and so do workgroups that share out a block's units.
+constexpr int kRows = 32;
+
+template <typename T, int D>
+constexpr int kStage = kUnit * D * (int)sizeof(T);       // K or V of a unit
+template <typename T, int D>
+constexpr int kSliceLds =
+    4 * (2 * kStage<T, D> > kRows * (D + 4) * 4 ? 2 * kStage<T, D> : kRows * (D + 4) * 4) +
+    4 * 2 * kRows * 4;
+
+template <typename T, int D>
+__global__ __launch_bounds__(kThreads) void k_chunk_slices(const RowRuns* __restrict__ runs, int L,
+                                                           const ChunkArgs x) {
+  using M = Mat<T, D>;
+  constexpr int NB = D / 32, RB = D * (int)sizeof(T), CPR = RB / 16, RPL = 64 / CPR;
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  __shared__ uint64_t part[2 * kThreads / 64];
+  __shared__ uint32_t redo;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int qi = lane & 31, h = lane >> 5;
+  const int bh = blockIdx.x % (x.B * x.heads), block = x.blocks - 1 - blockIdx.x / (x.B * x.heads);
+  const int kh = bh % x.heads, b = bh / x.heads;
+  const int split = blockIdx.y, splits = x.splits, G = x.group;
+  const Chunk ch = chunk_of(x, L, b);
+  const int r0 = block * kRows, rows = min(kRows, ch.n * G - r0);   // rows that count
+  if (splits > 1 && rows <= 0) return;                 // the joining kernel clears the padding
+
+  const int i = r0 + min(qi, max(rows - 1, 0)), t = i / G, g = i - t * G;
+  RowsPlan plan{nullptr, nullptr, 0, 0};
+  char* const stage = lds + plan_bytes(L);
+  int u0 = 0, u1 = 0;
+  RowRuns rr;
+  typename M::Row q;
+  if (rows > 0 && !ch.bad && ch.len > 0) {
+    const int t0 = r0 / G, t1 = (r0 + rows - 1) / G;
+    rr = runs[dbg::idx(ch.p0 + t, L, dbg::kRow)];
+    load_row<T, D>(q, (const char*)((const T*)x.Q + b * x.qb + (kh * G + g) * x.qh + t * x.qt), 16u * h);
+    plan = plan_rows<kThreads>(lds, part, L, runs, ch.p0 + t0, t1 - t0 + 1, ch.len);
+    u0 = (int)((int64_t)plan.n() * split / splits), u1 = (int)((int64_t)plan.n() * (split + 1) / splits);
+  }
+  Slice s;
+  s.lane = lane, s.qi = qi, s.h = h;
+  f32x16_t o[NB];
+#pragma unroll
+  for (int c = 0; c < NB; ++c)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[c][r] = 0.f;
+  const float sl2 = x.scale * kLog2e;
+  float m = -INFINITY, l = 0.f;
+  bool bad = ch.bad;
+
+  char* const sk = stage + wave * 2 * kStage<T, D>;
+  char* const sv = sk + kStage<T, D>;
+  // the row of the cache that holds this lane's key of unit u, and whether it has one
+  auto slot_of = [&](int u, bool& found) {
+    int j;
+    if (u < plan.dense)
+      j = min(32 * (plan.units[u] & (kFullUnit - 1)) + qi, ch.len - 1);
+    else
+      j = plan.keys[min(32 * (u - plan.dense) + qi, plan.gathered - 1)];
+    const int p = page_of(x.pages, b, x.max_pages, x.n_pages, x.page_shift, dbg::idx(j, L, dbg::kKey));
+    found = p >= 0;
+    return cache_row(max(p, 0), x.heads, kh, x.page_shift, j);
+  };
+  int u = u0 + wave;
+  bool found = true;
+  unsigned slot = u < u1 ? slot_of(u, found) : 0;
+  for (; u < u1; u += 4) {
+    wait_lds();   // the unit before it has left the rows that these loads fill
+#pragma unroll
+    for (int k = 0; k < kUnit / RPL; ++k) {
+      const int r = RPL * k + lane / CPR;
+      const size_t row = (size_t)(unsigned)__shfl((int)slot, r, 64) * RB;
+      const int c = 16 * ((lane % CPR) ^ swz_row<CPR>(r));
+      dma16((const char*)x.K + row + c, sk + kDmaBlock * k);
+      dma16((const char*)x.V + row + c, sv + kDmaBlock * k);
+    }
+    // which of the unit's keys are the row's: bit r, the key of register r
+    uint32_t mine = 0xffff;
+    if (u >= plan.dense) {
+      const int c = u - plan.dense;
+      mine = gathered_bits(rr, plan.keys + 32 * c, min(32, plan.gathered - 32 * c), h);
+    } else if (!(plan.units[u] & kFullUnit)) {
+      const int kb = 32 * plan.units[u];
+      mine = register_bits((uint32_t)tile_row_bits(rr, kb, 1, min(32, ch.len - kb)), h);
+    }
+    const uint32_t lost = (uint32_t)__ballot(!found);   // keys without a page
+    if (lost) bad = bad || (mine & register_bits(lost, h));
+    if (u + 4 < u1) slot = slot_of(u + 4, found);
+    wait_loads();
+    const f32x16_t sc = dot_staged<T, D>(sk, s, q);
+    float p[16], mx = -INFINITY;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      p[r] = mine >> r & 1 ? sc[r] * sl2 : -INFINITY;
+      mx = fmaxf(mx, p[r]);
+    }
+    mx = fmaxf(mx, lane_xor32(mx));
+    const float mn = fmaxf(m, mx);
+    const float mu = mn == -INFINITY ? 0.f : mn;   // every score so far -inf: weights 0
+    if (__any(mn > m)) {
+      const float alpha = exp2_hw(m - mu);
+      l *= alpha;
+#pragma unroll
+      for (int c = 0; c < NB; ++c)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[c][r] *= alpha;
+      m = mn;
+    }
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      p[r] = exp2_hw(p[r] - mu);
+      l += p[r];
+    }
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      typename M::V v;
+      load_staged<T, D>(v, sv, s, j);
+      M::pv(o, v, p, j);
+    }
+  }
+  if (bad) l = NAN;
+  l += lane_xor32(l);
+
+  // the wavefronts' (m, l, O) to one
+  constexpr int OS = D + 4;
+  float* const stat = (float*)(stage + kSliceLds<T, D> - 4 * 2 * kRows * 4);
+  if (threadIdx.x == 0) redo = 0;
+  __syncthreads();
+  float* const sum = (float*)stage + wave * kRows * OS;
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+#pragma unroll
+    for (int c = 0; c < NB; ++c) {
+      f32x4_t v;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = o[(4 * c + e) % NB][4 * k + (4 * c + e) / NB];
+      *(f32x4_t*)(sum + qi * OS + NB * (8 * k + 4 * h) + 4 * c) = v;
+    }
+  if (h == 0) stat[wave * 64 + qi] = m, stat[wave * 64 + 32 + qi] = l;
+  __syncthreads();
+  const int r = threadIdx.x >> 3, ri = r0 + r, rt = ri / G, rg = ri - rt * G;
+  float mt = stat[r], f[4], lt = 0.f;
+#pragma unroll
+  for (int w = 1; w < 4; ++w) mt = fmaxf(mt, stat[w * 64 + r]);
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const float mw = stat[w * 64 + r];
+    f[w] = mw == -INFINITY ? 0.f : exp2_hw(mw - mt);
+    lt += stat[w * 64 + 32 + r] * (mw == -INFINITY ? 1.f : f[w]);
+  }
+  const int64_t head = (int64_t)b * x.H + kh * G + rg;
+  if (splits > 1) {
+    if (r >= rows) return;
+    float* const to = x.ws + ((head * x.T + rt) * splits + split) * (D + 2);
+#pragma unroll
+    for (int k = 0; k < NB; ++k) {
+      const int c = 4 * (threadIdx.x & 7) + 32 * k;
+      f32x4_t v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < 4; ++w) v += *(const f32x4_t*)((const float*)stage + (w * kRows + r) * OS + c) * f[w];
+      *(f32x2_t*)(to + 2 + c) = f32x2_t{v[0], v[1]};
+      *(f32x2_t*)(to + 4 + c) = f32x2_t{v[2], v[3]};
+    }
+    if ((threadIdx.x & 7) == 0) *(f32x2_t*)to = f32x2_t{mt, lt};
+    return;
+  }
+  if (ri < x.T * G) {
+    T* const O = (T*)x.O + b * x.ob + (kh * G + rg) * x.oh + rt * x.ot;
+    // a row without weight has no key, or is formed again
+    const float inv = lt == 0.f ? 0.f : 1.f / lt;
+    bool fine = r >= rows || ch.bad || (lt > 0.f && lt < INFINITY);
+#pragma unroll
+    for (int k = 0; k < NB; ++k) {
+      const int c = 4 * (threadIdx.x & 7) + 32 * k;
+      f32x4_t v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < 4; ++w) v += *(const f32x4_t*)((const float*)stage + (w * kRows + r) * OS + c) * f[w];
+      v *= inv;
+      if (r >= rows) v = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) fine = fine && (r >= rows || ch.bad || fabsf(v[e]) < INFINITY);
+      store4<T>(O + c, v[0], v[1], v[2], v[3]);
+    }
+    if ((threadIdx.x & 7) == 0)
+      x.lse[head * x.T + rt] = r >= rows || lt == 0.f ? -INFINITY : kLn2 * (mt + log2f(lt));
+    if (!fine) atomicOr(&redo, 1u << r);
+  }
+  __syncthreads();
+  // rows that are not finite, or have no weight, from their own keys: what another
+  // row's key holds does not reach them
+  const uint32_t again = redo;
+  for (int k = wave; k < kRows; k += 4)
+    if (again >> k & 1) redo_row<T, D>(x, runs, L, b, kh, ch, (r0 + k) / G, (r0 + k) % G);
+}
+
+// One wavefront per row (all T of them): the parts (m, l, O) of the workgroups that
+// shared out its block's units to O and lse, eight parts' loads in flight at a time.
+template <typename T, int D>
+__global__ __launch_bounds__(64) void k_chunk_join(const RowRuns* __restrict__ runs, int L,
+                                                   const ChunkArgs x) {
+  constexpr int STEP = 8;
+  const int lane = threadIdx.x, splits = x.splits;
+  const int64_t row = blockIdx.x;
+  const int t = (int)(row % x.T), head = (int)(row / x.T % x.H), b = (int)(row / x.T / x.H);
+  const Chunk ch = chunk_of(x, L, b);
+  T* const O = (T*)x.O + b * x.ob + head * x.oh + t * x.ot;
+  if (t >= ch.n) {
+#pragma unroll
+    for (int c = 0; c < D / 64; ++c) store1(O + 64 * c + lane, 0.f);
+    if (lane == 0) x.lse[row] = -INFINITY;
+    return;
+  }
+  const float* const part = x.ws + row * splits * (D + 2);
+  float m = -INFINITY, l = 0.f;
+  if (lane < splits) {
+    const f32x2_t ml = *(const f32x2_t*)(part + lane * (D + 2));
+    m = ml[0], l = ml[1];
+  }
+  float acc[D / 64], v[STEP][D / 64];
+#pragma unroll
+  for (int c = 0; c < D / 64; ++c) acc[c] = 0.f;
+  auto load = [&](int s0) {
+#pragma unroll
+    for (int k = 0; k < STEP; ++k)
+#pragma unroll
+      for (int c = 0; c < D / 64; ++c)
+        v[k][c] = part[min(s0 + k, splits - 1) * (D + 2) + 2 + 64 * c + lane];
+  };
+  load(0);
+  const float mt = wave_max(m), f = m == -INFINITY ? 0.f : exp2_hw(m - mt);
+  const float lt = wave_sum(m == -INFINITY ? l : l * f);
+  const float inv = lt == 0.f ? 0.f : 1.f / lt;
+  for (int s0 = 0; s0 < splits; s0 += STEP) {
+    if (s0) load(s0);
+#pragma unroll
+    for (int k = 0; k < STEP; ++k) {
+      if (s0 + k >= splits) continue;
+      const float fk = __builtin_bit_cast(
+          float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, f), s0 + k));
+#pragma unroll
+      for (int c = 0; c < D / 64; ++c) acc[c] = fmaf(v[k][c], fk, acc[c]);
+    }
+  }
+  bool fine = lt > 0.f && lt < INFINITY;
+#pragma unroll
+  for (int c = 0; c < D / 64; ++c) {
+    acc[c] *= inv;
+    fine = fine && fabsf(acc[c]) < INFINITY;
+    store1(O + 64 * c + lane, acc[c]);
+  }
+  if (lane == 0) x.lse[row] = lt == 0.f ? -INFINITY : kLn2 * (mt + log2f(lt));
+  if (__any(!fine) && !ch.bad) redo_row<T, D>(x, runs, L, b, head / x.group, ch, t, head % x.group);
+}
+
+template <typename T, int D>
+hipError_t chunk_launch(const DevAcsr& a, const ChunkArgs& x, hipStream_t st) {
+  const dim3 grid((unsigned)((int64_t)x.blocks * x.B * x.heads), x.splits);
+  hipLaunchKernelGGL((k_chunk_slices<T, D>), grid, dim3(kThreads), (plan_bytes(a.L) + kSliceLds<T, D>),
+                     st, a.runs, a.L, x);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || x.splits == 1) return e;
+  hipLaunchKernelGGL((k_chunk_join<T, D>), dim3((unsigned)((int64_t)x.B * x.H * x.T)), dim3(64), 0, st,
+                     a.runs, a.L, x);
+  return hipGetLastError();
+}
+
+template <typename T, int D>
+hipError_t allow_lds() {
+  return hipFuncSetAttribute((const void*)k_chunk_slices<T, D>,
+                             hipFuncAttributeMaxDynamicSharedMemorySize,
+                             plan_bytes(SPLAT_MAX_L) + kSliceLds<T, D>);
+}
+
+}  // namespace
+
+hipError_t bounds_collect_chunk(uint32_t* bits, bool clear) { return dbg::collect(bits, clear); }
+
+hipError_t prepare_chunk() {
+  hipError_t e = allow_lds<float, 64>();
+  if (e == hipSuccess) e = allow_lds<float, 128>();
+  if (e == hipSuccess) e = allow_lds<__bf16, 64>();
+  if (e == hipSuccess) e = allow_lds<__bf16, 128>();
+  return e;
+}
+
+// As many parts of a block's units as fill the chip with two workgroups a CU while
+// each wavefront keeps two units.
+ChunkShape chunk_shape(const DevAcsr& a, int dtype, int B, int H, int heads, int T, int d) {
+  ChunkShape s;
+  const int64_t rows = (int64_t)T * (H / heads);
+  s.blocks = (int32_t)((rows + kRows - 1) / kRows);
+  const int64_t units = (std::min(a.max_row_nnz + kRows, a.L) + kUnit - 1) / kUnit;
+  const int64_t groups = (int64_t)s.blocks * B * heads;
+  const int64_t n = std::min((512 + groups - 1) / groups, (units + 7) / 8);
+  s.splits = (int32_t)std::min<int64_t>(std::max<int64_t>(n, 1), 64);
+  return s;
+}
+
+int64_t chunk_workspace(const ChunkShape& s, int B, int H, int T, int d) {
+  return s.splits == 1 ? 0 : (int64_t)B * H * T * s.splits * (d + 2);
+}
+
+hipError_t launch_chunk(const DevAcsr& a, int dtype, int d, const ChunkArgs& x, hipStream_t st) {
+  if (dtype == 0)
+    return d == 64 ? chunk_launch<float, 64>(a, x, st) : chunk_launch<float, 128>(a, x, st);
+  return d == 64 ? chunk_launch<__bf16, 64>(a, x, st) : chunk_launch<__bf16, 128>(a, x, st);
+}
+
+}  // namespace splat

@@ -155,6 +155,26 @@ int64_t decode_workspace(const DevAcsr& a, int B, int H, int heads, int d);
 hipError_t launch_decode(const DevAcsr& a, int dtype, int d, const DecodeArgs& x, hipStream_t st);
 hipError_t prepare_decode();
 
+// A chunk of new tokens over the paged cache; strides in elements.
+struct ChunkArgs {
+  const void *Q, *K, *V;
+  void* O;
+  float* lse;                 // [B, H, T]
+  const int32_t *pages, *lengths, *counts;
+  int64_t qb, qh, qt, ob, oh, ot;
+  int32_t B, H, heads, group, T, max_pages, n_pages, page_shift;
+  int32_t blocks, splits;     // of a (sequence, head of the cache)'s rows, of a block's keys
+  float scale;
+  float* ws;
+};
+struct ChunkShape {
+  int32_t blocks, splits;
+};
+ChunkShape chunk_shape(const DevAcsr& a, int dtype, int B, int H, int heads, int T, int d);
+int64_t chunk_workspace(const ChunkShape& s, int B, int H, int T, int d);   // floats
+hipError_t launch_chunk(const DevAcsr& a, int dtype, int d, const ChunkArgs& x, hipStream_t st);
+hipError_t prepare_chunk();
+
 // A cache brought back to a budget.  to: the pages that the kept keys move to, or
 // null: in place.
 struct EvictArgs {
@@ -181,6 +201,7 @@ hipError_t bounds_collect_slices(uint32_t* bits, bool clear);
 hipError_t bounds_collect_grad(uint32_t* bits, bool clear);
 hipError_t bounds_collect_grad_tiles(uint32_t* bits, bool clear);
 hipError_t bounds_collect_serve(uint32_t* bits, bool clear);
+hipError_t bounds_collect_chunk(uint32_t* bits, bool clear);
 // One check of `index` against [0, n) as kind `kind`, run on the device
 // (allocates and frees one int); *result = the checked index.
 hipError_t bounds_probe(int kind, int index, int n, int* result);
