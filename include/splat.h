@@ -642,6 +642,28 @@ splat_status splat_sparse_mhsa_chunk(splat_acsr_t h, splat_dtype dtype, int32_t 
                                      const splat_heads* o, float* lse, void* workspace, void* stream);
 
 /*
+ * splat_cache_weights -- adds the attention weight that each key of the cache took
+ * from a chunk's queries to what it has gathered: with q, lengths, counts and scale as
+ * given to splat_sparse_mhsa_chunk, and the lse that it left,
+ *
+ *     out_j = decay w_j + sum over the chunk's tokens t and the query heads of j's head
+ *             of exp(s_tj - lse_t),  j in row t
+ *
+ * for every place j below lengths[b]; the chunk's own places start from 0 instead of
+ * decay w_j (what w holds there does not matter), and a sequence whose count is 0
+ * keeps its weights undecayed.  w and out: fp32 [n_pages, heads, page], paged as the cache is;
+ * places past the lengths are not written.  out may be w itself.  A row whose lse is -inf adds
+ * nothing, one of NaN makes its keys' weights NaN.  A place without a page is not
+ * written; a sequence of bad length (as there) is left out.  No two sequences share a page
+ * below their lengths in out.  fp32 arithmetic in a fixed order.  cache->v is not read.  out
+ * otherwise shares no memory with the inputs (INVALID_ARG).
+ */
+splat_status splat_cache_weights(splat_acsr_t h, splat_dtype dtype, int32_t B, int32_t T, int32_t d,
+                                 const splat_heads* q, const float* lse, const splat_cache* cache,
+                                 const int32_t* lengths, const int32_t* counts, float scale,
+                                 float decay, const float* w, float* out, void* stream);
+
+/*
  * splat_cache_evict -- brings sequences of more than `budget` tokens back to it.  Of
  * each head of the cache the first `first` and the last `recent` places stay and, of those
  * between, the ones of largest weight (equal weights: the lowest place), budget in all; the

@@ -30,7 +30,7 @@ __all__ = [
     "DENSE_ALPHA", "transpose_colmajor", "rspmm_colmajor", "sparse_mhsa_unfused",
     "sparse_mhsa_fwd_lse", "sparse_mhsa_bwd", "PLAN_GRAD", "Rotary", "rotary", "cache_append",
     "sparse_mhsa_decode", "decode_workspace", "sparse_mhsa_chunk", "chunk_workspace",
-    "cache_evict",
+    "cache_weights", "cache_evict",
 ]
 
 MAX_TERMS = 8
@@ -159,6 +159,7 @@ def _open(path: str) -> ctypes.CDLL:
         "splat_sparse_mhsa_decode": [vp, i32, i32, i32, i32, vp, vp, vp, f32, vp, vp, vp],
         "splat_chunk_workspace": [vp, i32, i32, i32, i32, i32, i32, P(i64)],
         "splat_sparse_mhsa_chunk": [vp, i32, i32, i32, i32, vp, vp, vp, vp, f32, vp, vp, vp, vp],
+        "splat_cache_weights": [vp, i32, i32, i32, i32, vp, vp, vp, vp, vp, f32, f32, vp, vp, vp],
         "splat_cache_evict": [i32, i32, i32, vp, vp, vp, i32, i32, i32, vp, i32, vp, vp, vp],
         "splat_sparse_mhsa_unfused_noalloc": [vp, i32, i32, i32, i32, vp, vp, vp, f32, vp, i32, f32,
                                               P(i32), vp],
@@ -749,6 +750,18 @@ def sparse_mhsa_chunk(acsr: Acsr, Q: torch.Tensor, k_cache: torch.Tensor, v_cach
     chunk_workspace() bytes, made by the call unless given."""
     return native().chunk(acsr.handle.value, Q, k_cache, v_cache, table, lengths, scale, counts, O, lse,
                           workspace, *_where())
+
+
+def cache_weights(acsr: Acsr, Q: torch.Tensor, lse: torch.Tensor, k_cache: torch.Tensor,
+                  table: torch.Tensor, lengths: torch.Tensor, weights: torch.Tensor, scale: float, *,
+                  counts: Optional[torch.Tensor] = None, decay: float = 1.0,
+                  out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Adds the attention weight that each cached key took from a chunk's queries to
+    `weights` (fp32 [pages, heads, page]), after decaying it; the chunk's own keys
+    start from 0.  Q, table, lengths, counts and scale as given to
+    sparse_mhsa_chunk, lse as it returned it.  In place, or into out."""
+    return native().cache_weights(acsr.handle.value, Q, lse, k_cache, table, lengths, weights, scale, counts,
+                                  decay, out, *_where())
 
 
 def cache_evict(k_cache: torch.Tensor, v_cache: torch.Tensor, weights: torch.Tensor, table: torch.Tensor,

@@ -1196,6 +1196,51 @@ splat_status splat_sparse_mhsa_chunk(splat_acsr_t h, splat_dtype dtype, int32_t 
   return launched(splat::launch_chunk(h->dev, dtype, d, x, (hipStream_t)stream), "sparse_mhsa_chunk");
 }
 
+splat_status splat_cache_weights(splat_acsr_t h, splat_dtype dtype, int32_t B, int32_t T, int32_t d,
+                                 const splat_heads* q, const float* lse, const splat_cache* cache,
+                                 const int32_t* lengths, const int32_t* counts, float scale,
+                                 float decay, const float* w, float* out, void* stream) {
+  if (!q) return fail(SPLAT_ERR_INVALID_ARG, "q must be non-NULL");
+  const int32_t H = int32_of(q->heads);
+  CHECK(check_handle(h, B, H));
+  CHECK(check_cache(cache));
+  int64_t need = 0;
+  const int32_t heads = (int32_t)cache->heads;
+  CHECK(splat_chunk_workspace(h, dtype, B, H, heads, T, d, &need));
+  if (!lengths) return fail(SPLAT_ERR_INVALID_ARG, "lengths is NULL");
+  const int32_t e = dtype == SPLAT_BF16 ? 2 : 4;
+  const View qv{q, "q", B, T, d, e};
+  CHECK(check_view(qv, false));
+  if (!(decay >= 0.f) || decay > 3e38f)
+    return fail(SPLAT_ERR_INVALID_ARG, "decay must be a finite number of at least 0");
+  const void* const floats[] = {lse, w, out};
+  for (const void* p : floats)
+    if (!p || (uintptr_t)p % 4 != 0)
+      return fail(SPLAT_ERR_INVALID_ARG, "lse, w and out must be device memory at 4 bytes");
+  const size_t rows = (size_t)cache->n_pages * cache->heads * cache->page;
+  const Span in[] = {{cache->k, rows * d * e, "the cache's k"},
+                     {cache->table, (size_t)B * cache->max_pages * 4, "the cache's table"},
+                     {lengths, (size_t)B * 4, "lengths"},
+                     {counts, (size_t)B * 4, "counts"},
+                     {lse, (size_t)B * H * T * 4, "lse"},
+                     {qv.at(), (size_t)qv.extent(), "q"},
+                     {w == out ? nullptr : w, rows * 4, "w"}};
+  for (const Span& i : in)
+    if (meet(out, rows * 4, i.p, i.bytes))
+      return fail(SPLAT_ERR_INVALID_ARG, "out must not overlap %s", i.name);
+  splat::WeighArgs x{};
+  splat::ChunkArgs& c = x.c;
+  c.Q = q->data, c.K = cache->k, c.lse = (float*)lse;
+  c.pages = cache->table, c.lengths = lengths, c.counts = counts;
+  c.qb = q->stride_b, c.qh = q->stride_h, c.qt = q->stride_t;
+  c.B = B, c.H = H, c.heads = heads, c.group = H / heads, c.T = T;
+  c.max_pages = (int32_t)cache->max_pages, c.n_pages = (int32_t)cache->n_pages;
+  c.page_shift = log2_of(cache->page);
+  c.scale = scale;
+  x.w = w, x.out = out, x.decay = decay;
+  return launched(splat::launch_weigh(h->dev, dtype, d, x, (hipStream_t)stream), "cache_weights");
+}
+
 splat_status splat_cache_evict(splat_dtype dtype, int32_t B, int32_t d, const splat_cache* cache,
                                float* weights, const int32_t* lengths, int32_t budget, int32_t first,
                                int32_t recent, const int32_t* to, int32_t max_to, int32_t* kept,

@@ -281,6 +281,26 @@ py::tuple chunk(int64_t handle, const Tensor& Q, const Tensor& k_cache, const Te
   return py::make_tuple(O, lse);
 }
 
+Tensor cache_weights(int64_t handle, const Tensor& Q, const Tensor& lse, const Tensor& k_cache,
+                     const Tensor& table, const Tensor& lengths, const Tensor& weights, double scale,
+                     const Opt& counts, double decay, const Opt& out, int64_t device, int64_t stream) {
+  const Call c(Q, "Q", device, stream);
+  const auto s = Q.sizes();
+  const splat_cache cache = c.cache(k_cache, k_cache, table, s[0], s[3]);
+  const int32_t* const n = c.ints(lengths, "lengths", {s[0]});
+  const int32_t* const m = counts ? c.ints(*counts, "counts", {s[0]}) : nullptr;
+  const splat_heads q = c.heads(Q, "Q", s);
+  const float* const l = (const float*)c.want(lse, "lse", at::kFloat, s.slice(0, 3));
+  const auto places = k_cache.sizes().slice(0, 3);
+  float* const w = (float*)c.want(weights, "weights", at::kFloat, places);
+  float* const to = out ? (float*)c.want(*out, "out", at::kFloat, places) : w;
+  check(splat_cache_weights(acsr_of(handle), c.dtype(), s[0], s[2], s[3], &q, l, &cache, n, m, (float)scale,
+                            (float)decay, w, to, c.stream));
+  const Tensor& result = out ? *out : weights;
+  written({&result});
+  return result;
+}
+
 py::tuple cache_evict(const Tensor& k_cache, const Tensor& v_cache, const Tensor& weights,
                       const Tensor& table, const Tensor& lengths, int64_t budget, int64_t first,
                       int64_t recent, const Opt& to, const Opt& kept_, const Opt& left_, int64_t device,
@@ -322,5 +342,6 @@ PYBIND11_MODULE(_native, m) {
   m.def("cache_append", &cache_append);
   m.def("decode", &decode);
   m.def("chunk", &chunk);
+  m.def("cache_weights", &cache_weights);
   m.def("cache_evict", &cache_evict);
 }

@@ -359,6 +359,82 @@ hipError_t chunk_launch(const DevAcsr& a, const ChunkArgs& x, hipStream_t st) {
   return hipGetLastError();
 }
 
+// ------------------------------------------------------------ weights of keys
+// w_j = decay w_j + sum over the chunk's rows and the group's heads of
+// exp(s_ij - lse_i), the probabilities formed again from the rows' log-sum-exp.  A
+// wavefront has a unit of 32 keys and goes over the rows, 32 at a time; each lane
+// sums its row's 16 keys of the unit, and the lanes' sums meet at the end.
+template <typename T, int D>
+__global__ __launch_bounds__(kThreads) void k_weigh(const RowRuns* __restrict__ runs, int L,
+                                                    const WeighArgs x) {
+  using M = Mat<T, D>;
+  constexpr int RB = D * (int)sizeof(T), CPR = RB / 16, RPL = 64 / CPR;
+  __shared__ __attribute__((aligned(16))) char lds[4 * kStage<T, D>];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int qi = lane & 31, h = lane >> 5, G = x.c.group;
+  const int bh = blockIdx.x, kh = bh % x.c.heads, b = bh / x.c.heads;
+  const Chunk ch = chunk_of(x.c, L, b);
+  if (ch.bad) return;
+  Slice s;
+  s.lane = lane, s.qi = qi, s.h = h;
+  char* const sk = lds + wave * kStage<T, D>;
+  const float sl2 = x.c.scale * kLog2e, fade = ch.n > 0 ? x.decay : 1.f;
+  for (int u = blockIdx.y * 4 + wave; 32 * u < ch.len; u += gridDim.y * 4) {
+    const int kb = 32 * u, nk = min(32, ch.len - kb);
+    const int j = min(kb + qi, ch.len - 1);
+    const int page = page_of(x.c.pages, b, x.c.max_pages, x.c.n_pages, x.c.page_shift, j);
+    const unsigned slot = cache_row(max(page, 0), x.c.heads, kh, x.c.page_shift, j);
+    wait_lds();
+#pragma unroll
+    for (int k = 0; k < kUnit / RPL; ++k) {
+      const int r = RPL * k + lane / CPR;
+      const size_t row = (size_t)(unsigned)__shfl((int)slot, r, 64) * RB;
+      dma16((const char*)x.c.K + row + 16 * ((lane % CPR) ^ swz_row<CPR>(r)), sk + kDmaBlock * k);
+    }
+    wait_loads();
+    float acc[16];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) acc[r] = 0.f;
+    for (int r0 = 0; r0 < ch.n * G; r0 += kRows) {
+      const int i = min(r0 + qi, ch.n * G - 1), t = i / G, head = kh * G + i - t * G;
+      const RowRuns rr = runs[dbg::idx(ch.p0 + t, L, dbg::kRow)];
+      const uint32_t word = r0 + qi < ch.n * G ? (uint32_t)tile_row_bits(rr, kb, 1, nk) : 0u;
+      if (!__any(word != 0)) continue;
+      typename M::Row q;
+      load_row<T, D>(q, (const char*)((const T*)x.c.Q + b * x.c.qb + head * x.c.qh + t * x.c.qt), 16u * h);
+      const float lse = x.c.lse[((int64_t)b * x.c.H + head) * x.c.T + t] * kLog2e;
+      const uint32_t mine = lse == -INFINITY ? 0u : register_bits(word, h);
+      const f32x16_t sc = dot_staged<T, D>(sk, s, q);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[r] += mine >> r & 1 ? exp2_hw(sc[r] * sl2 - lse) : 0.f;
+    }
+    // register r's sum over the rows comes to the lanes whose low bits are r
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1)
+#pragma unroll
+      for (int r = 0; r < o; ++r) {
+        const bool up = lane & o;
+        const float give = up ? acc[r] : acc[r + o], keep = up ? acc[r + o] : acc[r];
+        acc[r] = keep + __shfl_xor(give, o, 64);
+      }
+    const float sum = acc[0] + __shfl_xor(acc[0], 16, 64);
+    const int r = lane & 15, k = 8 * (r >> 2) + 4 * h + (r & 3);
+    const unsigned at = (unsigned)__shfl((int)slot, k, 64);
+    if (__shfl(page, k, 64) >= 0 && (lane & 16) == 0 && k < nk)
+      x.out[at] = (kb + k < ch.p0 ? x.w[at] * fade : 0.f) + sum;
+  }
+}
+
+template <typename T, int D>
+hipError_t weigh_launch(const DevAcsr& a, const WeighArgs& x, hipStream_t st) {
+  const int64_t room = std::min<int64_t>((int64_t)x.c.max_pages << x.c.page_shift, a.L);
+  const int64_t groups = (int64_t)x.c.B * x.c.heads;
+  const int64_t parts = std::min((room + 4 * kUnit - 1) / (4 * kUnit), (4096 + groups - 1) / groups);
+  hipLaunchKernelGGL((k_weigh<T, D>), dim3((unsigned)groups, (unsigned)parts), dim3(kThreads), 0, st,
+                     a.runs, a.L, x);
+  return hipGetLastError();
+}
+
 template <typename T, int D>
 hipError_t allow_lds() {
   return hipFuncSetAttribute((const void*)k_chunk_slices<T, D>,
@@ -399,6 +475,12 @@ hipError_t launch_chunk(const DevAcsr& a, int dtype, int d, const ChunkArgs& x, 
   if (dtype == 0)
     return d == 64 ? chunk_launch<float, 64>(a, x, st) : chunk_launch<float, 128>(a, x, st);
   return d == 64 ? chunk_launch<__bf16, 64>(a, x, st) : chunk_launch<__bf16, 128>(a, x, st);
+}
+
+hipError_t launch_weigh(const DevAcsr& a, int dtype, int d, const WeighArgs& x, hipStream_t st) {
+  if (dtype == 0)
+    return d == 64 ? weigh_launch<float, 64>(a, x, st) : weigh_launch<float, 128>(a, x, st);
+  return d == 64 ? weigh_launch<__bf16, 64>(a, x, st) : weigh_launch<__bf16, 128>(a, x, st);
 }
 
 }  // namespace splat

@@ -175,6 +175,15 @@ int64_t chunk_workspace(const ChunkShape& s, int B, int H, int T, int d);   // f
 hipError_t launch_chunk(const DevAcsr& a, int dtype, int d, const ChunkArgs& x, hipStream_t st);
 hipError_t prepare_chunk();
 
+// The weight that the cache's keys take from a chunk (O, V and ws are not used).
+struct WeighArgs {
+  ChunkArgs c;
+  const float* w;             // [n_pages, heads, page]
+  float* out;                 // the same, or w itself
+  float decay;
+};
+hipError_t launch_weigh(const DevAcsr& a, int dtype, int d, const WeighArgs& x, hipStream_t st);
+
 // A cache brought back to a budget.  to: the pages that the kept keys move to, or
 // null: in place.
 struct EvictArgs {
