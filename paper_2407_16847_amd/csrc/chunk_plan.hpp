@@ -150,26 +150,61 @@ __device__ RowsPlan plan_rows(char* lds, uint64_t* part, int L, const RowRuns* r
   return plan;
 }
 
-// A row's 16 keys of a gathered unit, as the scores' registers hold them: bit r is
-// key 8 (r / 4) + 4 h + r % 4 of the unit.
-__device__ __forceinline__ uint32_t gathered_bits(const RowRuns& rr, const uint16_t* keys, int n, int h) {
-  uint32_t bits = 0;
+// A row's runs as a lane keeps them: both ends of each, and whether all have stride 1.
+struct RowEnds {
+  int first[SPLAT_MAX_RUNS], last[SPLAT_MAX_RUNS];
+  const Run* runs = nullptr;
+  bool dense = true;
+  __device__ __forceinline__ void open(const RowRuns* row) {
+    runs = row->r;
+    dense = true;
 #pragma unroll
-  for (int r = 0; r < 16; ++r) {
-    const int k = 8 * (r >> 2) + 4 * h + (r & 3);
-    const int j = keys[imin(k, n - 1)];
-    bool in = false;
-#pragma unroll
-    for (int q = 0; q < SPLAT_MAX_RUNS; ++q) {
-      const Run run = rr.r[q];
-      const int off = j - run.start;
-      // a multiple's quotient, below 2^16, is exact to 2^-7 before it is rounded
-      const int t = (int)__builtin_rintf((float)off * __builtin_amdgcn_rcpf((float)run.stride));
-      in = in || (run.count > 0 && off >= 0 && t < run.count && t * run.stride == off);
+    for (int k = 0; k < SPLAT_MAX_RUNS; ++k) {
+      const Run r = runs[k];
+      dense = dense && (r.stride == 1 || r.count <= 1);
+      first[k] = r.start, last[k] = r.count > 0 ? r.start + r.stride * (r.count - 1) : -1;
     }
-    bits |= (uint32_t)(in && k < n) << r;
   }
-  return bits;
+};
+
+// The row's keys of unit u, bit k key k; simple: every run in the wavefront has
+// stride 1.
+__device__ __forceinline__ uint32_t unit_word(const RowsPlan& plan, int u, const RowEnds& row, bool simple,
+                                              int len) {
+  uint32_t word = 0;
+  if (u < plan.dense) {
+    const uint32_t unit = plan.units[u];
+    if (unit & kFullUnit) return ~0u;
+    const int kb = 32 * unit, nk = imin(32, len - kb);
+    if (simple) {
+#pragma unroll
+      for (int k = 0; k < SPLAT_MAX_RUNS; ++k) {
+        const int lo = imax(row.first[k] - kb, 0), hi = imin(row.last[k] - kb, nk - 1);
+        if (lo <= hi) word |= (~0u << lo) & (~0u >> (31 - hi));
+      }
+    } else {
+#pragma unroll 1
+      for (int k = 0; k < SPLAT_MAX_RUNS; ++k)
+        word |= (uint32_t)run_tile_bits(row.runs[k], kb, 1, nk);
+    }
+    return word;
+  }
+  const uint16_t* const keys = plan.keys + 32 * (u - plan.dense);
+  const int n = imin(32, plan.gathered - 32 * (u - plan.dense));
+#pragma unroll 1
+  for (int q = 0; q < SPLAT_MAX_RUNS; ++q) {
+    const Run run = row.runs[q];
+    if (run.count <= 0) continue;
+    const float inv = __builtin_amdgcn_rcpf((float)run.stride);
+#pragma unroll 4
+    for (int k = 0; k < 32; ++k) {
+      const int off = keys[imin(k, n - 1)] - run.start;
+      // a multiple's quotient, below 2^16, is exact to 2^-7 before it is rounded
+      const int t = (int)__builtin_rintf((float)off * inv);
+      word |= (uint32_t)(off >= 0 && t < run.count && t * run.stride == off) << k;
+    }
+  }
+  return word & (~0u >> (32 - n));
 }
 
 // A word's bits (bit k: key k) in the registers' order.

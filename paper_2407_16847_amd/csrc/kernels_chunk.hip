@@ -39,7 +39,7 @@ __device__ __forceinline__ Chunk chunk_of(const ChunkArgs& x, int L, int b) {
 
 // O and lse of one row by one wavefront, from the row's own keys alone.
 template <typename T, int D>
-__device__ __noinline__ void row_alone(const ChunkArgs& x, const RowRuns& rr, int b, int kh, int len,
+__device__ __forceinline__ void row_alone(const ChunkArgs& x, const RowRuns& rr, int b, int kh, int len,
                                        const T* q, T* o, float* lse) {
   constexpr int NC = D / 64;
   const int lane = threadIdx.x & 63, n = count_lt(rr, len);
@@ -57,7 +57,14 @@ __device__ __noinline__ void row_alone(const ChunkArgs& x, const RowRuns& rr, in
       const int p = page_of(x.pages, b, x.max_pages, x.n_pages, x.page_shift, j);
       bad = bad || p < 0;
       slot = cache_row(max(p, 0), x.heads, kh, x.page_shift, j);
-      s = dense_dot<T, D>(q, (const T*)x.K + (size_t)slot * D) * x.scale;
+      // rare: few registers instead of many loads in flight
+      const T* const k = (const T*)x.K + (size_t)slot * D;
+      float dot = 0.f;
+#pragma unroll 1
+      for (int c = 0; c < D; c += 8)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) dot = fmaf((float)q[c + e], (float)k[c + e], dot);
+      s = dot * x.scale;
     }
     const float mn = fmaxf(m, wave_max(s));
     const float alpha = expf(m - mn), p = valid ? expf(s - mn) : 0.f;
@@ -103,7 +110,7 @@ constexpr int kSliceLds =
     4 * 2 * kRows * 4;
 
 template <typename T, int D>
-__global__ __launch_bounds__(kThreads) void k_chunk_slices(const RowRuns* __restrict__ runs, int L,
+__global__ __launch_bounds__(kThreads, sizeof(T) * D > 256 ? 1 : 2) void k_chunk_slices(const RowRuns* __restrict__ runs, int L,
                                                            const ChunkArgs x) {
   using M = Mat<T, D>;
   constexpr int NB = D / 32, RB = D * (int)sizeof(T), CPR = RB / 16, RPL = 64 / CPR;
@@ -123,15 +130,16 @@ __global__ __launch_bounds__(kThreads) void k_chunk_slices(const RowRuns* __rest
   RowsPlan plan{nullptr, nullptr, 0, 0};
   char* const stage = lds + plan_bytes(L);
   int u0 = 0, u1 = 0;
-  RowRuns rr;
+  RowEnds row;
   typename M::Row q;
   if (rows > 0 && !ch.bad && ch.len > 0) {
     const int t0 = r0 / G, t1 = (r0 + rows - 1) / G;
-    rr = runs[dbg::idx(ch.p0 + t, L, dbg::kRow)];
+    row.open(runs + dbg::idx(ch.p0 + t, L, dbg::kRow));
     load_row<T, D>(q, (const char*)((const T*)x.Q + b * x.qb + (kh * G + g) * x.qh + t * x.qt), 16u * h);
     plan = plan_rows<kThreads>(lds, part, L, runs, ch.p0 + t0, t1 - t0 + 1, ch.len);
     u0 = (int)((int64_t)plan.n() * split / splits), u1 = (int)((int64_t)plan.n() * (split + 1) / splits);
   }
+  const bool simple = __all(row.dense);
   Slice s;
   s.lane = lane, s.qi = qi, s.h = h;
   f32x16_t o[NB];
@@ -170,14 +178,7 @@ __global__ __launch_bounds__(kThreads) void k_chunk_slices(const RowRuns* __rest
       dma16((const char*)x.V + row + c, sv + kDmaBlock * k);
     }
     // which of the unit's keys are the row's: bit r, the key of register r
-    uint32_t mine = 0xffff;
-    if (u >= plan.dense) {
-      const int c = u - plan.dense;
-      mine = gathered_bits(rr, plan.keys + 32 * c, min(32, plan.gathered - 32 * c), h);
-    } else if (!(plan.units[u] & kFullUnit)) {
-      const int kb = 32 * plan.units[u];
-      mine = register_bits((uint32_t)tile_row_bits(rr, kb, 1, min(32, ch.len - kb)), h);
-    }
+    const uint32_t mine = register_bits(unit_word(plan, u, row, simple, ch.len), h);
     const uint32_t lost = (uint32_t)__ballot(!found);   // keys without a page
     if (lost) bad = bad || (mine & register_bits(lost, h));
     if (u + 4 < u1) slot = slot_of(u + 4, found);
@@ -288,6 +289,280 @@ __global__ __launch_bounds__(kThreads) void k_chunk_slices(const RowRuns* __rest
     if (again >> k & 1) redo_row<T, D>(x, runs, L, b, kh, ch, (r0 + k) / G, (r0 + k) % G);
 }
 
+// ------------------------------------------------------------------- tiles
+// bf16, many rows: a workgroup per 128 rows, 32 a wavefront, which share tiles of two
+// units (64 keys) of K and V through a two-slot LDS ring, the next tile's loads
+// in flight while this one is computed.  Products on v_mfma_f32_32x32x16_bf16:
+// S^T = K Q^T, so that a lane has 32 scores of one row, and O^T += V^T P^T with P^T
+// taken from the score registers.  A row's reference m stays while its tiles' sums
+// stay below kSumLimit, without a look at the maximum: a tile past it (and a row's first)
+// takes the exact maximum and rescales.
+constexpr int kTileRows = 128;
+constexpr float kSumLimit = 4096.f;
+
+// Waits until at most N of this wavefront's LDS reads are on their way; the operands
+// of a block read before them depend on it.
+template <int N>
+__device__ __forceinline__ void block_wait(bf16x8_t (&v)[4]) {
+  asm volatile("s_waitcnt lgkmcnt(%4)" : "+v"(v[0]), "+v"(v[1]), "+v"(v[2]), "+v"(v[3]) : "n"(N));
+}
+
+template <int D>
+struct Ring {
+  static constexpr int RB = 2 * D, CPR = RB / 16;       // bytes, 16-byte chunks of a row
+  static constexpr int TB = 2 * kUnit * RB;             // bytes of a tile of K or V
+  static constexpr int RPL = 64 / CPR;                  // rows a load
+  static constexpr int N = 2 * kUnit / RPL / 4;         // loads a wavefront and tile of each
+  static constexpr int LDS = 4 * TB;
+};
+
+template <int D>
+__global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void k_chunk_tiles(
+    const RowRuns* __restrict__ runs, int L, const ChunkArgs x) {
+  using R = Ring<D>;
+  constexpr int NKS = D / 16, NDB = D / 32, RB = R::RB;
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  __shared__ uint64_t part[2 * kThreads / 64];
+  __shared__ uint32_t redo[4], lost;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int qi = lane & 31, h = lane >> 5;
+  const int bh = blockIdx.x % (x.B * x.heads), block = x.blocks - 1 - blockIdx.x / (x.B * x.heads);
+  const int kh = bh % x.heads, b = bh / x.heads;
+  const int split = blockIdx.y, splits = x.splits, G = x.group;
+  const Chunk ch = chunk_of(x, L, b);
+  const int r0 = block * kTileRows, rows = min(kTileRows, ch.n * G - r0);   // rows that count
+  if (splits > 1 && rows <= 0) return;                 // the joining kernel clears the padding
+
+  const int mine = wave * 32 + qi;                     // this lane's row of the block
+  const int i = r0 + min(mine, max(rows - 1, 0)), t = i / G, g = i - t * G;
+  RowsPlan plan{nullptr, nullptr, 0, 0};
+  int u0 = 0, u1 = 0;
+  RowEnds row;
+  bf16x8_t q[NKS];
+  char* const ring = lds + plan_bytes(L);
+  if (rows > 0 && !ch.bad && ch.len > 0) {
+    const int t0 = r0 / G, t1 = (r0 + rows - 1) / G;
+    const __bf16* const from = (const __bf16*)x.Q + b * x.qb + (kh * G + g) * x.qh + t * x.qt;
+#pragma unroll
+    for (int k = 0; k < NKS; ++k) q[k] = *(const bf16x8_t*)(from + 16 * k + 8 * h);
+    row.open(runs + dbg::idx(ch.p0 + t, L, dbg::kRow));
+    plan = plan_rows<kThreads>(lds, part, L, runs, ch.p0 + t0, t1 - t0 + 1, ch.len);
+    u0 = (int)((int64_t)plan.n() * split / splits), u1 = (int)((int64_t)plan.n() * (split + 1) / splits);
+  }
+  const bool simple = __all(row.dense);
+  if (threadIdx.x < 4) redo[threadIdx.x] = 0;
+  if (threadIdx.x == 0) lost = 0;
+
+  // K operand of key 32 * half + qi, chunk 2 * ks + h; V^T operand by transposing reads
+  const int koff = qi * RB + 16 * (h ^ swz_k(qi));
+  int voff[NDB];
+  v_operand_offsets<D>(lane, voff);
+  f32x16_t o[NDB];
+#pragma unroll
+  for (int c = 0; c < NDB; ++c)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[c][r] = 0.f;
+  const float sl2 = x.scale * kLog2e;
+  float m = 0.f, l = 0.f;
+  bool set = false, found = true;          // the row has a reference; every page was one
+
+  // The rows of the cache that this lane loads of unit u's keys: those of load k are
+  // r = RPL * (wave + 4 k) + lane / CPR of the tile.
+  constexpr int NU = R::N / 2;             // loads of each a unit
+  auto slots_of = [&](int u, unsigned (&slot)[NU]) {
+    u = min(u, u1 - 1);
+    if (u < plan.dense && x.page_shift >= 5) {          // one page
+      const int kb = 32 * (__builtin_amdgcn_readfirstlane((int)plan.units[u]) & (int)(kFullUnit - 1));
+      const int p = page_of(x.pages, b, x.max_pages, x.n_pages, x.page_shift, kb);
+      found = found && p >= 0;
+      const unsigned row = cache_row(max(p, 0), x.heads, kh, x.page_shift, kb);
+#pragma unroll
+      for (int k = 0; k < NU; ++k)
+        slot[k] = row + min((R::RPL * (wave + 4 * k)) % 32 + lane / R::CPR, ch.len - 1 - kb);
+      return;
+    }
+#pragma unroll
+    for (int k = 0; k < NU; ++k) {
+      const int r = (R::RPL * (wave + 4 * k)) % 32 + lane / R::CPR;
+      int j;
+      if (u < plan.dense)
+        j = min(32 * (plan.units[u] & (int)(kFullUnit - 1)) + r, ch.len - 1);
+      else
+        j = plan.keys[min(32 * (u - plan.dense) + r, plan.gathered - 1)];
+      const int p = page_of(x.pages, b, x.max_pages, x.n_pages, x.page_shift, dbg::idx(j, L, dbg::kKey));
+      found = found && p >= 0;
+      slot[k] = cache_row(max(p, 0), x.heads, kh, x.page_shift, j);
+    }
+  };
+  auto issue = [&](char* to, const unsigned (&slot)[2][NU]) {
+#pragma unroll
+    for (int k = 0; k < R::N; ++k) {
+      const int bk = wave + 4 * k, r = bk * R::RPL + lane / R::CPR, c = lane % R::CPR;
+      const size_t row = (size_t)slot[k / NU][k % NU] * RB;
+      dma16((const char*)x.K + row + 16 * (c ^ swz_k(r)), to + bk * kDmaBlock);
+      dma16((const char*)x.V + row + 16 * (c ^ swz_v(r)), to + R::TB + bk * kDmaBlock);
+    }
+  };
+  unsigned slot[2][NU];
+  const int nt = (u1 - u0 + 1) / 2;
+  if (nt > 0) {
+    slots_of(u0, slot[0]), slots_of(u0 + 1, slot[1]);
+    issue(ring, slot);
+    slots_of(u0 + 2, slot[0]), slots_of(u0 + 3, slot[1]);
+    ring_sync<0>();
+  }
+  for (int it = 0; it < nt; ++it) {
+    const int u = u0 + 2 * it;
+    const char* const sk = ring + (it & 1) * 2 * R::TB;
+    if (it + 1 < nt) issue(ring + (~it & 1) * 2 * R::TB, slot);
+    slots_of(u + 4, slot[0]), slots_of(u + 5, slot[1]);
+    // which of the tile's keys are the row's: bit r of 16 h', the key of register r of
+    // half h'; the lanes' halves form a unit's word each
+    uint32_t word = 0;
+    if (u + h < u1) word = unit_word(plan, u + h, row, simple, ch.len);
+    const uint32_t other = __builtin_bit_cast(uint32_t, lane_xor32(__builtin_bit_cast(float, word)));
+    const uint32_t bits = register_bits(h ? other : word, h) | register_bits(h ? word : other, h) << 16;
+    if (__any(bits != 0)) {
+      f32x16_t s[2];
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        bf16x8_t ka[NKS];
+#pragma unroll
+        for (int ks = 0; ks < NKS; ++ks) 
+          ka[ks] = *(const bf16x8_t*)(sk + (koff ^ (32 * (ks & 3))) + half * 32 * RB + 128 * (ks >> 2));
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[half][r] = 0.f;
+#pragma unroll
+        for (int ks = 0; ks < NKS; ++ks) s[half] = mfma32(ka[ks], q[ks], s[half]);
+      }
+      if (__any(~bits != 0)) {
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[half][r] = keep_if_bit(s[half][r] * sl2, bits, 16 * half + r);
+      } else {
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[half][r] *= sl2;
+      }
+      bf16x8_t pf[4];
+      auto exps = [&](float ref) {
+        float l0 = 0.f, l1 = 0.f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          float e8[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) e8[e] = exp2_hw(s[j >> 1][(j & 1) * 8 + e] - ref);
+          l0 += (e8[0] + e8[1]) + (e8[2] + e8[3]);
+          l1 += (e8[4] + e8[5]) + (e8[6] + e8[7]);
+          pf[j] = __builtin_bit_cast(bf16x8_t, u32x4_t{pack_bf16_rn(e8[0], e8[1]), pack_bf16_rn(e8[2], e8[3]),
+                                                       pack_bf16_rn(e8[4], e8[5]), pack_bf16_rn(e8[6], e8[7])});
+        }
+        return l0 + l1;
+      };
+      float lt = exps(m);
+      // (both halves of the lanes decide alike: a row's sum and its keys are theirs together)
+      const float both = lt + lane_xor32(lt);
+      if (__any(!(both <= kSumLimit) || (!set && (word | other) != 0))) {
+        float mx = -INFINITY;
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[half][r]);
+        mx = fmaxf(mx, lane_xor32(mx));
+        // a row without weight has no reference yet
+        const float mn = !set ? (mx == -INFINITY ? 0.f : mx) : fmaxf(m, mx);
+        const float alpha = set ? exp2_hw(m - mn) : 0.f;
+        l *= alpha;
+#pragma unroll
+        for (int c = 0; c < NDB; ++c)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) o[c][r] *= alpha;
+        set = set || mx != -INFINITY;
+        m = mn;
+        lt = exps(m);
+      }
+      l += lt;
+      // V^T a block of 32 features at a time, the next one's reads in flight
+      const unsigned sv = lds_addr(sk + R::TB);
+      bf16x8_t va[2][4];
+      read_v_block<D>(sv + voff[0], va[0]);
+#pragma unroll
+      for (int c = 0; c < NDB; ++c) {
+        if (c + 1 < NDB) {
+          read_v_block<D>(sv + voff[(c + 1) % NDB], va[(c + 1) & 1]);
+          block_wait<8>(va[c & 1]);
+        } else {
+          block_wait<0>(va[c & 1]);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) o[c] = mfma32(va[c & 1][j], pf[j], o[c]);
+      }
+    }
+    ring_sync<0>();
+  }
+  l += lane_xor32(l);
+  if (__any(!found)) lost = 1;
+  __syncthreads();
+  // a page that is none: every row of the block is formed again from its own keys
+  if (ch.bad || lost) l = NAN;
+  const bool counts = mine < rows;
+  const int64_t head = (int64_t)b * x.H + kh * G + g;
+  if (splits > 1) {
+    if (!counts) return;
+    float* const to = x.ws + ((head * x.T + t) * splits + split) * (D + 2);
+    if (h == 0) *(f32x2_t*)to = f32x2_t{set ? m : -INFINITY, l};
+#pragma unroll
+    for (int c = 0; c < NDB; ++c)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        float* const at = to + 2 + 32 * c + 8 * k + 4 * h;
+        *(f32x2_t*)at = f32x2_t{o[c][4 * k], o[c][4 * k + 1]};
+        *(f32x2_t*)(at + 2) = f32x2_t{o[c][4 * k + 2], o[c][4 * k + 3]};
+      }
+    return;
+  }
+  // whole rows by way of the ring
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  bool fine = l > 0.f && l < INFINITY;
+  constexpr int OS = RB + 16;
+  char* const stage = ring + wave * 32 * OS;
+#pragma unroll
+  for (int c = 0; c < NDB; ++c)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      float v[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        v[e] = counts ? o[c][4 * k + e] * inv : 0.f;
+        fine = fine && fabsf(v[e]) < INFINITY;
+      }
+      store4<__bf16>((__bf16*)(stage + qi * OS) + 32 * c + 8 * k + 4 * h, v[0], v[1], v[2], v[3]);
+    }
+  const uint64_t again = __ballot(counts && !ch.bad && !fine);
+  if (lane == 0) redo[wave] = (uint32_t)again | (uint32_t)(again >> 32);
+  if (h == 0 && r0 + mine < x.T * G) {
+    const int ri = r0 + mine, rt = ri / G;
+    x.lse[((int64_t)b * x.H + kh * G + ri - rt * G) * x.T + rt] =
+        !counts || l == 0.f ? -INFINITY : kLn2 * (m + log2f(l));
+  }
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < 32 / R::RPL; ++k) {
+    const int r = k * R::RPL + lane / R::CPR, ri = r0 + wave * 32 + r, rt = ri / G;
+    if (ri >= x.T * G) continue;
+    *(u32x4_t*)((char*)((__bf16*)x.O + b * x.ob + (kh * G + ri - rt * G) * x.oh + rt * x.ot) +
+                16 * (lane % R::CPR)) = *(const u32x4_t*)(stage + r * OS + 16 * (lane % R::CPR));
+  }
+  __syncthreads();
+  for (int k = 0; k < 32; ++k)
+    if (redo[wave] >> k & 1) {
+      const int ri = r0 + wave * 32 + k;
+      redo_row<__bf16, D>(x, runs, L, b, kh, ch, ri / G, ri % G);
+    }
+}
+
 // One wavefront per row (all T of them): the parts (m, l, O) of the workgroups that
 // shared out its block's units to O and lse, eight parts' loads in flight at a time.
 template <typename T, int D>
@@ -350,8 +625,14 @@ __global__ __launch_bounds__(64) void k_chunk_join(const RowRuns* __restrict__ r
 template <typename T, int D>
 hipError_t chunk_launch(const DevAcsr& a, const ChunkArgs& x, hipStream_t st) {
   const dim3 grid((unsigned)((int64_t)x.blocks * x.B * x.heads), x.splits);
-  hipLaunchKernelGGL((k_chunk_slices<T, D>), grid, dim3(kThreads), (plan_bytes(a.L) + kSliceLds<T, D>),
-                     st, a.runs, a.L, x);
+  if constexpr (sizeof(T) == 2) {
+    if (x.tiles)
+      hipLaunchKernelGGL((k_chunk_tiles<D>), grid, dim3(kThreads), plan_bytes(a.L) + Ring<D>::LDS, st,
+                         a.runs, a.L, x);
+  }
+  if (!x.tiles)
+    hipLaunchKernelGGL((k_chunk_slices<T, D>), grid, dim3(kThreads), (plan_bytes(a.L) + kSliceLds<T, D>),
+                       st, a.runs, a.L, x);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || x.splits == 1) return e;
   hipLaunchKernelGGL((k_chunk_join<T, D>), dim3((unsigned)((int64_t)x.B * x.H * x.T)), dim3(64), 0, st,
@@ -442,6 +723,12 @@ hipError_t allow_lds() {
                              plan_bytes(SPLAT_MAX_L) + kSliceLds<T, D>);
 }
 
+template <int D>
+hipError_t allow_tiles_lds() {
+  return hipFuncSetAttribute((const void*)k_chunk_tiles<D>, hipFuncAttributeMaxDynamicSharedMemorySize,
+                             plan_bytes(SPLAT_MAX_L) + Ring<D>::LDS);
+}
+
 }  // namespace
 
 hipError_t bounds_collect_chunk(uint32_t* bits, bool clear) { return dbg::collect(bits, clear); }
@@ -451,6 +738,8 @@ hipError_t prepare_chunk() {
   if (e == hipSuccess) e = allow_lds<float, 128>();
   if (e == hipSuccess) e = allow_lds<__bf16, 64>();
   if (e == hipSuccess) e = allow_lds<__bf16, 128>();
+  if (e == hipSuccess) e = allow_tiles_lds<64>();
+  if (e == hipSuccess) e = allow_tiles_lds<128>();
   return e;
 }
 
@@ -459,8 +748,10 @@ hipError_t prepare_chunk() {
 ChunkShape chunk_shape(const DevAcsr& a, int dtype, int B, int H, int heads, int T, int d) {
   ChunkShape s;
   const int64_t rows = (int64_t)T * (H / heads);
-  s.blocks = (int32_t)((rows + kRows - 1) / kRows);
-  const int64_t units = (std::min(a.max_row_nnz + kRows, a.L) + kUnit - 1) / kUnit;
+  s.tiles = dtype == 1 && rows > 64;
+  const int of = s.tiles ? kTileRows : kRows;
+  s.blocks = (int32_t)((rows + of - 1) / of);
+  const int64_t units = (std::min(a.max_row_nnz + of, a.L) + kUnit - 1) / kUnit;
   const int64_t groups = (int64_t)s.blocks * B * heads;
   const int64_t n = std::min((512 + groups - 1) / groups, (units + 7) / 8);
   s.splits = (int32_t)std::min<int64_t>(std::max<int64_t>(n, 1), 64);

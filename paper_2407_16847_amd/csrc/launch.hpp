@@ -163,11 +163,13 @@ struct ChunkArgs {
   const int32_t *pages, *lengths, *counts;
   int64_t qb, qh, qt, ob, oh, ot;
   int32_t B, H, heads, group, T, max_pages, n_pages, page_shift;
+  bool tiles;                 // blocks of 128 rows, not 32
   int32_t blocks, splits;     // of a (sequence, head of the cache)'s rows, of a block's keys
   float scale;
   float* ws;
 };
 struct ChunkShape {
+  bool tiles;
   int32_t blocks, splits;
 };
 ChunkShape chunk_shape(const DevAcsr& a, int dtype, int B, int H, int heads, int T, int d);
