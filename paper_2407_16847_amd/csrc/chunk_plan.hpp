@@ -23,9 +23,15 @@ __host__ __device__ constexpr int plan_words(int L) { return (L + 31) / 32; }
 __host__ __device__ constexpr int plan_bytes(int L) { return (8 * plan_words(L) + 4 + 15) / 16 * 16; }
 
 struct RowsPlan {
-  const uint16_t* units;   // words of the key axis, kFullUnit set on full ones
-  const uint16_t* keys;    // gathered keys
+  char* lds;
+  int words;
   int dense, gathered;     // units of words, keys gathered
+  // nothing yet; the arrays' addresses stay in sight of the compiler as ones in LDS
+  __device__ __forceinline__ RowsPlan(char* at, int L)
+      : lds(at), words(plan_words(L)), dense(0), gathered(0) {}
+  // words of the key axis, kFullUnit set on full ones; gathered keys
+  __device__ __forceinline__ uint16_t* units() const { return (uint16_t*)((int*)lds + words); }
+  __device__ __forceinline__ uint16_t* keys() const { return (uint16_t*)lds; }
   __device__ __forceinline__ int n() const { return dense + (gathered + kUnit - 1) / kUnit; }
 };
 
@@ -52,14 +58,14 @@ __device__ __forceinline__ uint64_t sums_before(uint64_t own, uint64_t* part, ui
 }
 
 // Rows p0 .. p0 + nt - 1 of the mask, keys below len (0 < len <= L).  Called by the
-// whole workgroup; lds: plan_bytes(L); part: 2 * THREADS / 64 values.
+// whole workgroup; plan.lds: plan_bytes(L); part: 2 * THREADS / 64 values.
 template <int THREADS>
-__device__ RowsPlan plan_rows(char* lds, uint64_t* part, int L, const RowRuns* runs, int p0, int nt,
-                              int len) {
+__device__ __forceinline__ void plan_rows(RowsPlan& plan, uint64_t* part, int L, const RowRuns* runs,
+                                          int p0, int nt, int len) {
   constexpr int kMost = SPLAT_MAX_L / 32 / THREADS;     // words a thread
-  const int words = plan_words(L), W = (len + 31) >> 5, tid = threadIdx.x;
-  uint32_t* const bits = (uint32_t*)lds;
-  int* const cover = (int*)lds + words;
+  const int words = plan.words, W = (len + 31) >> 5, tid = threadIdx.x;
+  uint32_t* const bits = (uint32_t*)plan.lds;
+  int* const cover = (int*)plan.lds + words;
   for (int i = tid; i < W; i += THREADS) bits[i] = 0;
   for (int i = tid; i <= W; i += THREADS) cover[i] = 0;
   __syncthreads();
@@ -130,8 +136,7 @@ __device__ RowsPlan plan_rows(char* lds, uint64_t* part, int L, const RowRuns* r
   const int sparse = (int)(all >> 16 & 0xffff), keys = (int)(all >> 32);
   const bool gather = keys <= 2 * words && 2 * ((keys + kUnit - 1) / kUnit) <= sparse;
   // every thread has read its words (the barrier of the second sum): units and keys take their place
-  uint16_t* const to_units = (uint16_t*)cover;
-  uint16_t* const to_keys = (uint16_t*)bits;
+  uint16_t *const to_units = plan.units(), *const to_keys = plan.keys();
   int u = (int)(before & 0xffff) + (gather ? 0 : (int)(before >> 16 & 0xffff)), k = (int)(before >> 32);
 #pragma unroll
   for (int i = 0; i < kMost; ++i) {
@@ -143,11 +148,8 @@ __device__ RowsPlan plan_rows(char* lds, uint64_t* part, int L, const RowRuns* r
     }
   }
   __syncthreads();
-  RowsPlan plan;
-  plan.units = to_units, plan.keys = to_keys;
   plan.dense = (int)(all & 0xffff) + (gather ? 0 : sparse);
   plan.gathered = gather ? keys : 0;
-  return plan;
 }
 
 // A row's runs as a lane keeps them: both ends of each, and whether all have stride 1.
@@ -173,7 +175,7 @@ __device__ __forceinline__ uint32_t unit_word(const RowsPlan& plan, int u, const
                                               int len) {
   uint32_t word = 0;
   if (u < plan.dense) {
-    const uint32_t unit = plan.units[u];
+    const uint32_t unit = plan.units()[u];
     if (unit & kFullUnit) return ~0u;
     const int kb = 32 * unit, nk = imin(32, len - kb);
     if (simple) {
@@ -189,7 +191,7 @@ __device__ __forceinline__ uint32_t unit_word(const RowsPlan& plan, int u, const
     }
     return word;
   }
-  const uint16_t* const keys = plan.keys + 32 * (u - plan.dense);
+  const uint16_t* const keys = plan.keys() + 32 * (u - plan.dense);
   const int n = imin(32, plan.gathered - 32 * (u - plan.dense));
 #pragma unroll 1
   for (int q = 0; q < SPLAT_MAX_RUNS; ++q) {

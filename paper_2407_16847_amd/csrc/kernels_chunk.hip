@@ -127,7 +127,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) * D > 256 ? 1 : 2) void k_chunk
   if (splits > 1 && rows <= 0) return;                 // the joining kernel clears the padding
 
   const int i = r0 + min(qi, max(rows - 1, 0)), t = i / G, g = i - t * G;
-  RowsPlan plan{nullptr, nullptr, 0, 0};
+  RowsPlan plan(lds, L);
   char* const stage = lds + plan_bytes(L);
   int u0 = 0, u1 = 0;
   RowEnds row;
@@ -136,7 +136,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) * D > 256 ? 1 : 2) void k_chunk
     const int t0 = r0 / G, t1 = (r0 + rows - 1) / G;
     row.open(runs + dbg::idx(ch.p0 + t, L, dbg::kRow));
     load_row<T, D>(q, (const char*)((const T*)x.Q + b * x.qb + (kh * G + g) * x.qh + t * x.qt), 16u * h);
-    plan = plan_rows<kThreads>(lds, part, L, runs, ch.p0 + t0, t1 - t0 + 1, ch.len);
+    plan_rows<kThreads>(plan, part, L, runs, ch.p0 + t0, t1 - t0 + 1, ch.len);
     u0 = (int)((int64_t)plan.n() * split / splits), u1 = (int)((int64_t)plan.n() * (split + 1) / splits);
   }
   const bool simple = __all(row.dense);
@@ -157,9 +157,9 @@ __global__ __launch_bounds__(kThreads, sizeof(T) * D > 256 ? 1 : 2) void k_chunk
   auto slot_of = [&](int u, bool& found) {
     int j;
     if (u < plan.dense)
-      j = min(32 * (plan.units[u] & (kFullUnit - 1)) + qi, ch.len - 1);
+      j = min(32 * (plan.units()[u] & (kFullUnit - 1)) + qi, ch.len - 1);
     else
-      j = plan.keys[min(32 * (u - plan.dense) + qi, plan.gathered - 1)];
+      j = plan.keys()[min(32 * (u - plan.dense) + qi, plan.gathered - 1)];
     const int p = page_of(x.pages, b, x.max_pages, x.n_pages, x.page_shift, dbg::idx(j, L, dbg::kKey));
     found = p >= 0;
     return cache_row(max(p, 0), x.heads, kh, x.page_shift, j);
@@ -335,7 +335,7 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void k_chunk_tiles(
 
   const int mine = wave * 32 + qi;                     // this lane's row of the block
   const int i = r0 + min(mine, max(rows - 1, 0)), t = i / G, g = i - t * G;
-  RowsPlan plan{nullptr, nullptr, 0, 0};
+  RowsPlan plan(lds, L);
   int u0 = 0, u1 = 0;
   RowEnds row;
   bf16x8_t q[NKS];
@@ -346,7 +346,7 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void k_chunk_tiles(
 #pragma unroll
     for (int k = 0; k < NKS; ++k) q[k] = *(const bf16x8_t*)(from + 16 * k + 8 * h);
     row.open(runs + dbg::idx(ch.p0 + t, L, dbg::kRow));
-    plan = plan_rows<kThreads>(lds, part, L, runs, ch.p0 + t0, t1 - t0 + 1, ch.len);
+    plan_rows<kThreads>(plan, part, L, runs, ch.p0 + t0, t1 - t0 + 1, ch.len);
     u0 = (int)((int64_t)plan.n() * split / splits), u1 = (int)((int64_t)plan.n() * (split + 1) / splits);
   }
   const bool simple = __all(row.dense);
@@ -366,32 +366,45 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void k_chunk_tiles(
   float m = 0.f, l = 0.f;
   bool set = false, found = true;          // the row has a reference; every page was one
 
-  // The rows of the cache that this lane loads of unit u's keys: those of load k are
-  // r = RPL * (wave + 4 k) + lane / CPR of the tile.
+  // Of unit u's keys this lane loads rows r = RPL * (wave + 4 k) % 32 + lane / CPR, k <
+  // NU.  Their pages are looked up a tile before they are needed (`pages_of`), ahead
+  // of the tile's loads: nothing then waits for those.
   constexpr int NU = R::N / 2;             // loads of each a unit
-  auto slots_of = [&](int u, unsigned (&slot)[NU]) {
+  const int r_lane = lane / R::CPR;
+  const int32_t* const table = x.pages + (int64_t)b * x.max_pages;
+  auto key_of = [&](int u, int k) {        // the key of load k
+    const int r = (R::RPL * (wave + 4 * k)) % 32 + r_lane;
+    const int j = u < plan.dense ? min(32 * (plan.units()[u] & (int)(kFullUnit - 1)) + r, ch.len - 1)
+                                 : (int)plan.keys()[min(32 * (u - plan.dense) + r, plan.gathered - 1)];
+    return dbg::idx(j, L, dbg::kKey);
+  };
+  auto pages_of = [&](int u, int (&p)[NU]) {
     u = min(u, u1 - 1);
     if (u < plan.dense && x.page_shift >= 5) {          // one page
-      const int kb = 32 * (__builtin_amdgcn_readfirstlane((int)plan.units[u]) & (int)(kFullUnit - 1));
-      const int p = page_of(x.pages, b, x.max_pages, x.n_pages, x.page_shift, kb);
-      found = found && p >= 0;
-      const unsigned row = cache_row(max(p, 0), x.heads, kh, x.page_shift, kb);
+      p[0] = table[32 * (plan.units()[u] & (int)(kFullUnit - 1)) >> x.page_shift];
+      return;
+    }
+#pragma unroll
+    for (int k = 0; k < NU; ++k) p[k] = table[key_of(u, k) >> x.page_shift];
+  };
+  auto slots_of = [&](int u, const int (&p)[NU], unsigned (&slot)[NU]) {
+    u = min(u, u1 - 1);
+    if (u < plan.dense && x.page_shift >= 5) {
+      const int kb = 32 * (__builtin_amdgcn_readfirstlane((int)plan.units()[u]) & (int)(kFullUnit - 1));
+      const int page = __builtin_amdgcn_readfirstlane(p[0]);
+      const bool ok = page >= 0 && page < x.n_pages;
+      found = found && ok;
+      const unsigned first = cache_row(ok ? page : 0, x.heads, kh, x.page_shift, kb);
 #pragma unroll
       for (int k = 0; k < NU; ++k)
-        slot[k] = row + min((R::RPL * (wave + 4 * k)) % 32 + lane / R::CPR, ch.len - 1 - kb);
+        slot[k] = first + min((R::RPL * (wave + 4 * k)) % 32 + r_lane, ch.len - 1 - kb);
       return;
     }
 #pragma unroll
     for (int k = 0; k < NU; ++k) {
-      const int r = (R::RPL * (wave + 4 * k)) % 32 + lane / R::CPR;
-      int j;
-      if (u < plan.dense)
-        j = min(32 * (plan.units[u] & (int)(kFullUnit - 1)) + r, ch.len - 1);
-      else
-        j = plan.keys[min(32 * (u - plan.dense) + r, plan.gathered - 1)];
-      const int p = page_of(x.pages, b, x.max_pages, x.n_pages, x.page_shift, dbg::idx(j, L, dbg::kKey));
-      found = found && p >= 0;
-      slot[k] = cache_row(max(p, 0), x.heads, kh, x.page_shift, j);
+      const bool ok = p[k] >= 0 && p[k] < x.n_pages;
+      found = found && ok;
+      slot[k] = cache_row(ok ? p[k] : 0, x.heads, kh, x.page_shift, key_of(u, k));
     }
   };
   auto issue = [&](char* to, const unsigned (&slot)[2][NU]) {
@@ -404,18 +417,26 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void k_chunk_tiles(
     }
   };
   unsigned slot[2][NU];
+  int page[2][NU];
   const int nt = (u1 - u0 + 1) / 2;
   if (nt > 0) {
-    slots_of(u0, slot[0]), slots_of(u0 + 1, slot[1]);
+#pragma unroll
+    for (int e = 0; e < 2; ++e) pages_of(u0 + e, page[e]), slots_of(u0 + e, page[e], slot[e]);
+#pragma unroll
+    for (int e = 0; e < 2; ++e) pages_of(u0 + 2 + e, page[e]);
     issue(ring, slot);
-    slots_of(u0 + 2, slot[0]), slots_of(u0 + 3, slot[1]);
     ring_sync<0>();
   }
   for (int it = 0; it < nt; ++it) {
     const int u = u0 + 2 * it;
     const char* const sk = ring + (it & 1) * 2 * R::TB;
-    if (it + 1 < nt) issue(ring + (~it & 1) * 2 * R::TB, slot);
-    slots_of(u + 4, slot[0]), slots_of(u + 5, slot[1]);
+    if (it + 1 < nt) {
+#pragma unroll
+      for (int e = 0; e < 2; ++e) slots_of(u + 2 + e, page[e], slot[e]);
+#pragma unroll
+      for (int e = 0; e < 2; ++e) pages_of(u + 4 + e, page[e]);
+      issue(ring + (~it & 1) * 2 * R::TB, slot);
+    }
     // which of the tile's keys are the row's: bit r of 16 h', the key of register r of
     // half h'; the lanes' halves form a unit's word each
     uint32_t word = 0;
