@@ -37,6 +37,20 @@ __device__ __forceinline__ Chunk chunk_of(const ChunkArgs& x, int L, int b) {
   return c;
 }
 
+// The k-th longest sequence (the k-th, of more than 64): workgroups are dealt out in
+// their grid's order, and the long ones had better not come last.
+__device__ __forceinline__ int by_length(const int32_t* lengths, int B, int k) {
+  if (B == 1 || B > 64) return k;
+  const int lane = threadIdx.x & 63;
+  const int len = lane < B ? lengths[lane] : 0;
+  int rank = 0;
+  for (int i = 0; i < B; ++i) {
+    const int other = __builtin_amdgcn_readlane(len, i);
+    rank += other > len || (other == len && i < lane);
+  }
+  return __builtin_ctzll(__ballot(lane < B && rank == k));
+}
+
 // O and lse of one row by one wavefront, from the row's own keys alone.
 template <typename T, int D>
 __device__ __forceinline__ void row_alone(const ChunkArgs& x, const RowRuns& rr, int b, int kh, int len,
@@ -307,6 +321,14 @@ __device__ __forceinline__ void block_wait(bf16x8_t (&v)[4]) {
   asm volatile("s_waitcnt lgkmcnt(%4)" : "+v"(v[0]), "+v"(v[1]), "+v"(v[2]), "+v"(v[3]) : "n"(N));
 }
 
+// A tile's rows lie unpadded in LDS, their 16-byte chunks XOR-swizzled: K is read 16
+// rows, one chunk each at a time, V 4 rows, 4 chunks each (transposed).  Rows of 256 bytes
+// need a row's own place for that; two rows of 128 bytes share the banks (swz_k, swz_v).
+template <int D>
+__device__ __forceinline__ int place_k(int r) { return D == 128 ? r & 15 : swz_k(r); }
+template <int D>
+__device__ __forceinline__ int place_v(int r) { return D == 128 ? (r & 3) << 2 : swz_v(r); }
+
 template <int D>
 struct Ring {
   static constexpr int RB = 2 * D, CPR = RB / 16;       // bytes, 16-byte chunks of a row
@@ -326,8 +348,9 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void k_chunk_tiles(
   __shared__ uint32_t redo[4], lost;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int qi = lane & 31, h = lane >> 5;
-  const int bh = blockIdx.x % (x.B * x.heads), block = x.blocks - 1 - blockIdx.x / (x.B * x.heads);
-  const int kh = bh % x.heads, b = bh / x.heads;
+  // the longest sequence's blocks first, of each the last (longest) first
+  const int kh = blockIdx.x % x.heads, rest = blockIdx.x / x.heads;
+  const int block = x.blocks - 1 - rest % x.blocks, b = by_length(x.lengths, x.B, rest / x.blocks);
   const int split = blockIdx.y, splits = x.splits, G = x.group;
   const Chunk ch = chunk_of(x, L, b);
   const int r0 = block * kTileRows, rows = min(kTileRows, ch.n * G - r0);   // rows that count
@@ -354,9 +377,9 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void k_chunk_tiles(
   if (threadIdx.x == 0) lost = 0;
 
   // K operand of key 32 * half + qi, chunk 2 * ks + h; V^T operand by transposing reads
-  const int koff = qi * RB + 16 * (h ^ swz_k(qi));
-  int voff[NDB];
-  v_operand_offsets<D>(lane, voff);
+  const int koff = qi * RB + 16 * (h ^ place_k<D>(qi));
+  const int vr = 4 * h + ((lane & 15) >> 2);
+  const int voff = vr * RB + 16 * ((2 * (lane >> 4 & 1) + (lane >> 1 & 1)) ^ place_v<D>(vr)) + 8 * (lane & 1);
   f32x16_t o[NDB];
 #pragma unroll
   for (int c = 0; c < NDB; ++c)
@@ -412,8 +435,8 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void k_chunk_tiles(
     for (int k = 0; k < R::N; ++k) {
       const int bk = wave + 4 * k, r = bk * R::RPL + lane / R::CPR, c = lane % R::CPR;
       const size_t row = (size_t)slot[k / NU][k % NU] * RB;
-      dma16((const char*)x.K + row + 16 * (c ^ swz_k(r)), to + bk * kDmaBlock);
-      dma16((const char*)x.V + row + 16 * (c ^ swz_v(r)), to + R::TB + bk * kDmaBlock);
+      dma16((const char*)x.K + row + 16 * (c ^ place_k<D>(r)), to + bk * kDmaBlock);
+      dma16((const char*)x.V + row + 16 * (c ^ place_v<D>(r)), to + R::TB + bk * kDmaBlock);
     }
   };
   unsigned slot[2][NU];
@@ -450,31 +473,31 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void k_chunk_tiles(
         bf16x8_t ka[NKS];
 #pragma unroll
         for (int ks = 0; ks < NKS; ++ks) 
-          ka[ks] = *(const bf16x8_t*)(sk + (koff ^ (32 * (ks & 3))) + half * 32 * RB + 128 * (ks >> 2));
+          ka[ks] = *(const bf16x8_t*)(sk + (koff ^ (32 * ks)) + half * 32 * RB);
 #pragma unroll
         for (int r = 0; r < 16; ++r) s[half][r] = 0.f;
 #pragma unroll
         for (int ks = 0; ks < NKS; ++ks) s[half] = mfma32(ka[ks], q[ks], s[half]);
       }
+      // against the row's reference, in powers of 2
+#pragma unroll
+      for (int half = 0; half < 2; ++half)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[half][r] = fmaf(s[half][r], sl2, -m);
       if (__any(~bits != 0)) {
 #pragma unroll
         for (int half = 0; half < 2; ++half)
 #pragma unroll
-          for (int r = 0; r < 16; ++r) s[half][r] = keep_if_bit(s[half][r] * sl2, bits, 16 * half + r);
-      } else {
-#pragma unroll
-        for (int half = 0; half < 2; ++half)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) s[half][r] *= sl2;
+          for (int r = 0; r < 16; ++r) s[half][r] = keep_if_bit(s[half][r], bits, 16 * half + r);
       }
       bf16x8_t pf[4];
-      auto exps = [&](float ref) {
+      auto exps = [&]() {
         float l0 = 0.f, l1 = 0.f;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           float e8[8];
 #pragma unroll
-          for (int e = 0; e < 8; ++e) e8[e] = exp2_hw(s[j >> 1][(j & 1) * 8 + e] - ref);
+          for (int e = 0; e < 8; ++e) e8[e] = exp2_hw(s[j >> 1][(j & 1) * 8 + e]);
           l0 += (e8[0] + e8[1]) + (e8[2] + e8[3]);
           l1 += (e8[4] + e8[5]) + (e8[6] + e8[7]);
           pf[j] = __builtin_bit_cast(bf16x8_t, u32x4_t{pack_bf16_rn(e8[0], e8[1]), pack_bf16_rn(e8[2], e8[3]),
@@ -482,7 +505,7 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void k_chunk_tiles(
         }
         return l0 + l1;
       };
-      float lt = exps(m);
+      float lt = exps();
       // (both halves of the lanes decide alike: a row's sum and its keys are theirs together)
       const float both = lt + lane_xor32(lt);
       if (__any(!(both <= kSumLimit) || (!set && (word | other) != 0))) {
@@ -493,26 +516,30 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void k_chunk_tiles(
           for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[half][r]);
         mx = fmaxf(mx, lane_xor32(mx));
         // a row without weight has no reference yet
-        const float mn = !set ? (mx == -INFINITY ? 0.f : mx) : fmaxf(m, mx);
-        const float alpha = set ? exp2_hw(m - mn) : 0.f;
+        const float up = !set ? (mx == -INFINITY ? 0.f : mx) : fmaxf(0.f, mx);
+        const float alpha = set ? exp2_hw(-up) : 0.f;
         l *= alpha;
 #pragma unroll
         for (int c = 0; c < NDB; ++c)
 #pragma unroll
           for (int r = 0; r < 16; ++r) o[c][r] *= alpha;
         set = set || mx != -INFINITY;
-        m = mn;
-        lt = exps(m);
+        m += up;
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[half][r] -= up;
+        lt = exps();
       }
       l += lt;
       // V^T a block of 32 features at a time, the next one's reads in flight
       const unsigned sv = lds_addr(sk + R::TB);
       bf16x8_t va[2][4];
-      read_v_block<D>(sv + voff[0], va[0]);
+      read_v_block<D>(sv + voff, va[0]);
 #pragma unroll
       for (int c = 0; c < NDB; ++c) {
         if (c + 1 < NDB) {
-          read_v_block<D>(sv + voff[(c + 1) % NDB], va[(c + 1) & 1]);
+          read_v_block<D>(sv + (voff ^ (64 * (c + 1))), va[(c + 1) & 1]);
           block_wait<8>(va[c & 1]);
         } else {
           block_wait<0>(va[c & 1]);
