@@ -152,42 +152,47 @@ __device__ __forceinline__ void plan_rows(RowsPlan& plan, uint64_t* part, int L,
   plan.gathered = gather ? keys : 0;
 }
 
-// A row's runs as a lane keeps them: both ends of each, and whether all have stride 1.
+// A row's runs as a lane finds them, in LDS since registers are short: both ends of
+// each, 16 bits apiece, and the row's number.
 struct RowEnds {
-  int first[SPLAT_MAX_RUNS], last[SPLAT_MAX_RUNS];
-  const Run* runs = nullptr;
-  bool dense = true;
-  __device__ __forceinline__ void open(const RowRuns* row) {
-    runs = row->r;
-    dense = true;
+  u32x4_t ends;
+  int row;
+  // whether all of the row's runs have stride 1
+  __device__ __forceinline__ bool open(const RowRuns* runs, int at) {
+    bool dense = true;
+    u32x4_t e;
 #pragma unroll
     for (int k = 0; k < SPLAT_MAX_RUNS; ++k) {
-      const Run r = runs[k];
+      const Run r = runs[at].r[k];
       dense = dense && (r.stride == 1 || r.count <= 1);
-      first[k] = r.start, last[k] = r.count > 0 ? r.start + r.stride * (r.count - 1) : -1;
+      e[k] = r.count > 0 ? (uint32_t)r.start | (uint32_t)(r.start + r.stride * (r.count - 1)) << 16 : 1u;
     }
+    ends = e, row = at;
+    return dense;
   }
 };
+static_assert(SPLAT_MAX_RUNS == 4 && SPLAT_MAX_L <= 65536, "a run's ends are 16 bits");
 
 // The row's keys of unit u, bit k key k; simple: every run in the wavefront has
 // stride 1.
-__device__ __forceinline__ uint32_t unit_word(const RowsPlan& plan, int u, const RowEnds& row, bool simple,
-                                              int len) {
+__device__ __forceinline__ uint32_t unit_word(const RowsPlan& plan, int u, const RowRuns* runs,
+                                              const RowEnds& row, bool simple, int len) {
   uint32_t word = 0;
   if (u < plan.dense) {
     const uint32_t unit = plan.units()[u];
     if (unit & kFullUnit) return ~0u;
     const int kb = 32 * unit, nk = imin(32, len - kb);
     if (simple) {
+      const u32x4_t ends = row.ends;
 #pragma unroll
       for (int k = 0; k < SPLAT_MAX_RUNS; ++k) {
-        const int lo = imax(row.first[k] - kb, 0), hi = imin(row.last[k] - kb, nk - 1);
+        const int lo = imax((int)(ends[k] & 0xffff) - kb, 0), hi = imin((int)(ends[k] >> 16) - kb, nk - 1);
         if (lo <= hi) word |= (~0u << lo) & (~0u >> (31 - hi));
       }
     } else {
+      const Run* const r = runs[row.row].r;
 #pragma unroll 1
-      for (int k = 0; k < SPLAT_MAX_RUNS; ++k)
-        word |= (uint32_t)run_tile_bits(row.runs[k], kb, 1, nk);
+      for (int k = 0; k < SPLAT_MAX_RUNS; ++k) word |= (uint32_t)run_tile_bits(r[k], kb, 1, nk);
     }
     return word;
   }
@@ -195,7 +200,7 @@ __device__ __forceinline__ uint32_t unit_word(const RowsPlan& plan, int u, const
   const int n = imin(32, plan.gathered - 32 * (u - plan.dense));
 #pragma unroll 1
   for (int q = 0; q < SPLAT_MAX_RUNS; ++q) {
-    const Run run = row.runs[q];
+    const Run run = runs[row.row].r[q];
     if (run.count <= 0) continue;
     const float inv = __builtin_amdgcn_rcpf((float)run.stride);
 #pragma unroll 4

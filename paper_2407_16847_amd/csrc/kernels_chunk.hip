@@ -131,6 +131,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) * D > 256 ? 1 : 2) void k_chunk
   extern __shared__ __attribute__((aligned(16))) char lds[];
   __shared__ uint64_t part[2 * kThreads / 64];
   __shared__ uint32_t redo;
+  __shared__ RowEnds ends[4 * kRows];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int qi = lane & 31, h = lane >> 5;
   const int bh = blockIdx.x % (x.B * x.heads), block = x.blocks - 1 - blockIdx.x / (x.B * x.heads);
@@ -144,16 +145,17 @@ __global__ __launch_bounds__(kThreads, sizeof(T) * D > 256 ? 1 : 2) void k_chunk
   RowsPlan plan(lds, L);
   char* const stage = lds + plan_bytes(L);
   int u0 = 0, u1 = 0;
-  RowEnds row;
+  RowEnds& row = ends[wave * kRows + qi];
+  bool dense = true;
   typename M::Row q;
   if (rows > 0 && !ch.bad && ch.len > 0) {
     const int t0 = r0 / G, t1 = (r0 + rows - 1) / G;
-    row.open(runs + dbg::idx(ch.p0 + t, L, dbg::kRow));
+    dense = row.open(runs, dbg::idx(ch.p0 + t, L, dbg::kRow));
     load_row<T, D>(q, (const char*)((const T*)x.Q + b * x.qb + (kh * G + g) * x.qh + t * x.qt), 16u * h);
     plan_rows<kThreads>(plan, part, L, runs, ch.p0 + t0, t1 - t0 + 1, ch.len);
     u0 = (int)((int64_t)plan.n() * split / splits), u1 = (int)((int64_t)plan.n() * (split + 1) / splits);
   }
-  const bool simple = __all(row.dense);
+  const bool simple = __all(dense);
   Slice s;
   s.lane = lane, s.qi = qi, s.h = h;
   f32x16_t o[NB];
@@ -192,7 +194,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) * D > 256 ? 1 : 2) void k_chunk
       dma16((const char*)x.V + row + c, sv + kDmaBlock * k);
     }
     // which of the unit's keys are the row's: bit r, the key of register r
-    const uint32_t mine = register_bits(unit_word(plan, u, row, simple, ch.len), h);
+    const uint32_t mine = register_bits(unit_word(plan, u, runs, row, simple, ch.len), h);
     const uint32_t lost = (uint32_t)__ballot(!found);   // keys without a page
     if (lost) bad = bad || (mine & register_bits(lost, h));
     if (u + 4 < u1) slot = slot_of(u + 4, found);
@@ -346,6 +348,7 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void k_chunk_tiles(
   extern __shared__ __attribute__((aligned(16))) char lds[];
   __shared__ uint64_t part[2 * kThreads / 64];
   __shared__ uint32_t redo[4], lost;
+  __shared__ RowEnds ends[kTileRows];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int qi = lane & 31, h = lane >> 5;
   // the longest sequence's blocks first, of each the last (longest) first
@@ -356,23 +359,24 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void k_chunk_tiles(
   const int r0 = block * kTileRows, rows = min(kTileRows, ch.n * G - r0);   // rows that count
   if (splits > 1 && rows <= 0) return;                 // the joining kernel clears the padding
 
-  const int mine = wave * 32 + qi;                     // this lane's row of the block
-  const int i = r0 + min(mine, max(rows - 1, 0)), t = i / G, g = i - t * G;
+  int mine = wave * 32 + qi;                           // this lane's row of the block
   RowsPlan plan(lds, L);
   int u0 = 0, u1 = 0;
-  RowEnds row;
+  RowEnds& row = ends[mine];
+  bool dense = true;
   bf16x8_t q[NKS];
   char* const ring = lds + plan_bytes(L);
   if (rows > 0 && !ch.bad && ch.len > 0) {
     const int t0 = r0 / G, t1 = (r0 + rows - 1) / G;
+    const int i = r0 + min(mine, rows - 1), t = i / G, g = i - t * G;
     const __bf16* const from = (const __bf16*)x.Q + b * x.qb + (kh * G + g) * x.qh + t * x.qt;
 #pragma unroll
     for (int k = 0; k < NKS; ++k) q[k] = *(const bf16x8_t*)(from + 16 * k + 8 * h);
-    row.open(runs + dbg::idx(ch.p0 + t, L, dbg::kRow));
+    dense = row.open(runs, dbg::idx(ch.p0 + t, L, dbg::kRow));
     plan_rows<kThreads>(plan, part, L, runs, ch.p0 + t0, t1 - t0 + 1, ch.len);
     u0 = (int)((int64_t)plan.n() * split / splits), u1 = (int)((int64_t)plan.n() * (split + 1) / splits);
   }
-  const bool simple = __all(row.dense);
+  const bool simple = __all(dense);
   if (threadIdx.x < 4) redo[threadIdx.x] = 0;
   if (threadIdx.x == 0) lost = 0;
 
@@ -463,10 +467,10 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void k_chunk_tiles(
     // which of the tile's keys are the row's: bit r of 16 h', the key of register r of
     // half h'; the lanes' halves form a unit's word each
     uint32_t word = 0;
-    if (u + h < u1) word = unit_word(plan, u + h, row, simple, ch.len);
+    if (u + h < u1) word = unit_word(plan, u + h, runs, row, simple, ch.len);
     const uint32_t other = __builtin_bit_cast(uint32_t, lane_xor32(__builtin_bit_cast(float, word)));
-    const uint32_t bits = register_bits(h ? other : word, h) | register_bits(h ? word : other, h) << 16;
-    if (__any(bits != 0)) {
+    if (__any(word != 0)) {
+      const bool whole = __all(word == ~0u);
       f32x16_t s[2];
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
@@ -484,7 +488,8 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void k_chunk_tiles(
       for (int half = 0; half < 2; ++half)
 #pragma unroll
         for (int r = 0; r < 16; ++r) s[half][r] = fmaf(s[half][r], sl2, -m);
-      if (__any(~bits != 0)) {
+      if (!whole) {
+        const uint32_t bits = register_bits(h ? other : word, h) | register_bits(h ? word : other, h) << 16;
 #pragma unroll
         for (int half = 0; half < 2; ++half)
 #pragma unroll
@@ -532,20 +537,22 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void k_chunk_tiles(
         lt = exps();
       }
       l += lt;
-      // V^T a block of 32 features at a time, the next one's reads in flight
+      // V^T a block of 32 features at a time, the next one's reads in flight where
+      // registers allow (d = 64 has four wavefronts a SIMD instead)
       const unsigned sv = lds_addr(sk + R::TB);
-      bf16x8_t va[2][4];
-      read_v_block<D>(sv + voff, va[0]);
+      constexpr int AHEAD = D == 64 ? 0 : 1;
+      bf16x8_t va[AHEAD + 1][4];
+      if (AHEAD) read_v_block<D>(sv + voff, va[0]);
 #pragma unroll
       for (int c = 0; c < NDB; ++c) {
-        if (c + 1 < NDB) {
-          read_v_block<D>(sv + (voff ^ (64 * (c + 1))), va[(c + 1) & 1]);
-          block_wait<8>(va[c & 1]);
-        } else {
-          block_wait<0>(va[c & 1]);
-        }
+        constexpr int N = AHEAD + 1;
+        if (c + AHEAD < NDB) read_v_block<D>(sv + (voff ^ (64 * (c + AHEAD))), va[(c + AHEAD) % N]);
+        if (AHEAD && c + 1 < NDB)
+          block_wait<8>(va[c % N]);
+        else
+          block_wait<0>(va[c % N]);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) o[c] = mfma32(va[c & 1][j], pf[j], o[c]);
+        for (int j = 0; j < 4; ++j) o[c] = mfma32(va[c % N][j], pf[j], o[c]);
       }
     }
     ring_sync<0>();
@@ -555,11 +562,13 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void k_chunk_tiles(
   __syncthreads();
   // a page that is none: every row of the block is formed again from its own keys
   if (ch.bad || lost) l = NAN;
+  asm volatile("" : "+v"(mine));     // formed again, not kept through the loop
   const bool counts = mine < rows;
-  const int64_t head = (int64_t)b * x.H + kh * G + g;
+  const int ri = r0 + mine, rt = ri / G;
+  const int64_t place = ((int64_t)b * x.H + kh * G + ri - rt * G) * x.T + rt;   // of lse
   if (splits > 1) {
     if (!counts) return;
-    float* const to = x.ws + ((head * x.T + t) * splits + split) * (D + 2);
+    float* const to = x.ws + (place * splits + split) * (D + 2);
     if (h == 0) *(f32x2_t*)to = f32x2_t{set ? m : -INFINITY, l};
 #pragma unroll
     for (int c = 0; c < NDB; ++c)
@@ -590,11 +599,8 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void k_chunk_tiles(
     }
   const uint64_t again = __ballot(counts && !ch.bad && !fine);
   if (lane == 0) redo[wave] = (uint32_t)again | (uint32_t)(again >> 32);
-  if (h == 0 && r0 + mine < x.T * G) {
-    const int ri = r0 + mine, rt = ri / G;
-    x.lse[((int64_t)b * x.H + kh * G + ri - rt * G) * x.T + rt] =
-        !counts || l == 0.f ? -INFINITY : kLn2 * (m + log2f(l));
-  }
+  if (h == 0 && ri < x.T * G)
+    x.lse[place] = !counts || l == 0.f ? -INFINITY : kLn2 * (m + log2f(l));
   __syncthreads();
 #pragma unroll
   for (int k = 0; k < 32 / R::RPL; ++k) {
