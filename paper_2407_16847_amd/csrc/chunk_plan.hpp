@@ -18,19 +18,21 @@ constexpr int kSparseKeys = 8;
 constexpr uint32_t kFullUnit = 0x8000u;
 
 // bytes of LDS for masks of L rows: the words' bits and cover, later the gathered
-// keys and the units
+// keys (or 2^sub values of the caller's a unit) and the units
 __host__ __device__ constexpr int plan_words(int L) { return (L + 31) / 32; }
-__host__ __device__ constexpr int plan_bytes(int L) { return (8 * plan_words(L) + 4 + 15) / 16 * 16; }
+__host__ __device__ constexpr int plan_bytes(int L, int sub = 0) {
+  return (4 * (plan_words(L) << sub) + 4 * plan_words(L) + 4 + 15) / 16 * 16;
+}
 
 struct RowsPlan {
   char* lds;
-  int words;
+  int words, front;        // words of the key axis; 32-bit values ahead of the units
   int dense, gathered;     // units of words, keys gathered
   // nothing yet; the arrays' addresses stay in sight of the compiler as ones in LDS
-  __device__ __forceinline__ RowsPlan(char* at, int L)
-      : lds(at), words(plan_words(L)), dense(0), gathered(0) {}
+  __device__ __forceinline__ RowsPlan(char* at, int L, int sub = 0)
+      : lds(at), words(plan_words(L)), front(words << sub), dense(0), gathered(0) {}
   // words of the key axis, kFullUnit set on full ones; gathered keys
-  __device__ __forceinline__ uint16_t* units() const { return (uint16_t*)((int*)lds + words); }
+  __device__ __forceinline__ uint16_t* units() const { return (uint16_t*)((int*)lds + front); }
   __device__ __forceinline__ uint16_t* keys() const { return (uint16_t*)lds; }
   __device__ __forceinline__ int n() const { return dense + (gathered + kUnit - 1) / kUnit; }
 };
@@ -65,7 +67,7 @@ __device__ __forceinline__ void plan_rows(RowsPlan& plan, uint64_t* part, int L,
   constexpr int kMost = SPLAT_MAX_L / 32 / THREADS;     // words a thread
   const int words = plan.words, W = (len + 31) >> 5, tid = threadIdx.x;
   uint32_t* const bits = (uint32_t*)plan.lds;
-  int* const cover = (int*)plan.lds + words;
+  int* const cover = (int*)plan.lds + plan.front;
   for (int i = tid; i < W; i += THREADS) bits[i] = 0;
   for (int i = tid; i <= W; i += THREADS) cover[i] = 0;
   __syncthreads();

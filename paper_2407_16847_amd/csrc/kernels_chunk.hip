@@ -340,6 +340,11 @@ struct Ring {
   static constexpr int LDS = 4 * TB;
 };
 
+// log2 of the rows in LDS a unit, for pages of 8 keys and more
+__host__ __device__ constexpr int tiles_sub(int page_shift) {
+  return page_shift < 3 || page_shift > 5 ? 0 : 5 - page_shift;
+}
+
 template <int D>
 __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void k_chunk_tiles(
     const RowRuns* __restrict__ runs, int L, const ChunkArgs x) {
@@ -360,12 +365,12 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void k_chunk_tiles(
   if (splits > 1 && rows <= 0) return;                 // the joining kernel clears the padding
 
   int mine = wave * 32 + qi;                           // this lane's row of the block
-  RowsPlan plan(lds, L);
+  RowsPlan plan(lds, L, tiles_sub(x.page_shift));
   int u0 = 0, u1 = 0;
   RowEnds& row = ends[mine];
   bool dense = true;
   bf16x8_t q[NKS];
-  char* const ring = lds + plan_bytes(L);
+  char* const ring = lds + plan_bytes(L, tiles_sub(x.page_shift));
   if (rows > 0 && !ch.bad && ch.len > 0) {
     const int t0 = r0 / G, t1 = (r0 + rows - 1) / G;
     const int i = r0 + min(mine, rows - 1), t = i / G, g = i - t * G;
@@ -394,11 +399,28 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void k_chunk_tiles(
   bool set = false, found = true;          // the row has a reference; every page was one
 
   // Of unit u's keys this lane loads rows r = RPL * (wave + 4 k) % 32 + lane / CPR, k <
-  // NU.  Their pages are looked up a tile before they are needed (`pages_of`), ahead
-  // of the tile's loads: nothing then waits for those.
+  // NU.  Where 8 keys or more lie in one page, the first row in the cache of each 8, 16 or 32 (a
+  // multiple of as many) and, in its low bits, the last key stand in LDS from here on;
+  // elsewhere pages are looked up a tile before they are needed, ahead of the tile's
+  // loads, so that nothing waits for those.
   constexpr int NU = R::N / 2;             // loads of each a unit
   const int r_lane = lane / R::CPR;
   const int32_t* const table = x.pages + (int64_t)b * x.max_pages;
+  const bool whole_pages = plan.gathered == 0 && x.page_shift >= 3;
+  const int run = min(x.page_shift, 5), low = (1 << run) - 1;
+  uint32_t* const unit_rows = (uint32_t*)lds;          // over the gathered keys
+  if (whole_pages) {
+    for (int k = (u0 << (5 - run)) + (int)threadIdx.x; k < u1 << (5 - run); k += kThreads) {
+      const int u = k >> (5 - run), from = k & ((1 << (5 - run)) - 1);
+      const int word = plan.units()[u] & (int)(kFullUnit - 1);
+      const int kb = min(32 * word + (from << run), (ch.len - 1) & ~low);   // of keys that there are
+      const int page = table[kb >> x.page_shift];
+      const bool ok = page >= 0 && page < x.n_pages;
+      found = found && ok;
+      unit_rows[k] = cache_row(ok ? page : 0, x.heads, kh, x.page_shift, kb) | min(low, ch.len - 1 - kb);
+    }
+    __syncthreads();
+  }
   auto key_of = [&](int u, int k) {        // the key of load k
     const int r = (R::RPL * (wave + 4 * k)) % 32 + r_lane;
     const int j = u < plan.dense ? min(32 * (plan.units()[u] & (int)(kFullUnit - 1)) + r, ch.len - 1)
@@ -406,25 +428,20 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void k_chunk_tiles(
     return dbg::idx(j, L, dbg::kKey);
   };
   auto pages_of = [&](int u, int (&p)[NU]) {
+    if (whole_pages) return;
     u = min(u, u1 - 1);
-    if (u < plan.dense && x.page_shift >= 5) {          // one page
-      p[0] = table[32 * (plan.units()[u] & (int)(kFullUnit - 1)) >> x.page_shift];
-      return;
-    }
 #pragma unroll
     for (int k = 0; k < NU; ++k) p[k] = table[key_of(u, k) >> x.page_shift];
   };
   auto slots_of = [&](int u, const int (&p)[NU], unsigned (&slot)[NU]) {
     u = min(u, u1 - 1);
-    if (u < plan.dense && x.page_shift >= 5) {
-      const int kb = 32 * (__builtin_amdgcn_readfirstlane((int)plan.units()[u]) & (int)(kFullUnit - 1));
-      const int page = __builtin_amdgcn_readfirstlane(p[0]);
-      const bool ok = page >= 0 && page < x.n_pages;
-      found = found && ok;
-      const unsigned first = cache_row(ok ? page : 0, x.heads, kh, x.page_shift, kb);
+    if (whole_pages) {
 #pragma unroll
-      for (int k = 0; k < NU; ++k)
-        slot[k] = first + min((R::RPL * (wave + 4 * k)) % 32 + r_lane, ch.len - 1 - kb);
+      for (int k = 0; k < NU; ++k) {
+        const int r = (R::RPL * (wave + 4 * k)) % 32 + r_lane;
+        const uint32_t e = unit_rows[(u << (5 - run)) + (r >> run)];
+        slot[k] = (e & ~(uint32_t)low) + min((uint32_t)(r & low), e & low);
+      }
       return;
     }
 #pragma unroll
@@ -438,9 +455,9 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void k_chunk_tiles(
 #pragma unroll
     for (int k = 0; k < R::N; ++k) {
       const int bk = wave + 4 * k, r = bk * R::RPL + lane / R::CPR, c = lane % R::CPR;
-      const size_t row = (size_t)slot[k / NU][k % NU] * RB;
-      dma16((const char*)x.K + row + 16 * (c ^ place_k<D>(r)), to + bk * kDmaBlock);
-      dma16((const char*)x.V + row + 16 * (c ^ place_v<D>(r)), to + R::TB + bk * kDmaBlock);
+      const unsigned row = slot[k / NU][k % NU];
+      dma16((const char*)x.K + 16 * (c ^ place_k<D>(r)) + (uint64_t)row * RB, to + bk * kDmaBlock);
+      dma16((const char*)x.V + 16 * (c ^ place_v<D>(r)) + (uint64_t)row * RB, to + R::TB + bk * kDmaBlock);
     }
   };
   unsigned slot[2][NU];
@@ -681,8 +698,8 @@ hipError_t chunk_launch(const DevAcsr& a, const ChunkArgs& x, hipStream_t st) {
   const dim3 grid((unsigned)((int64_t)x.blocks * x.B * x.heads), x.splits);
   if constexpr (sizeof(T) == 2) {
     if (x.tiles)
-      hipLaunchKernelGGL((k_chunk_tiles<D>), grid, dim3(kThreads), plan_bytes(a.L) + Ring<D>::LDS, st,
-                         a.runs, a.L, x);
+      hipLaunchKernelGGL((k_chunk_tiles<D>), grid, dim3(kThreads),
+                         plan_bytes(a.L, tiles_sub(x.page_shift)) + Ring<D>::LDS, st, a.runs, a.L, x);
   }
   if (!x.tiles)
     hipLaunchKernelGGL((k_chunk_slices<T, D>), grid, dim3(kThreads), (plan_bytes(a.L) + kSliceLds<T, D>),
@@ -780,7 +797,7 @@ hipError_t allow_lds() {
 template <int D>
 hipError_t allow_tiles_lds() {
   return hipFuncSetAttribute((const void*)k_chunk_tiles<D>, hipFuncAttributeMaxDynamicSharedMemorySize,
-                             plan_bytes(SPLAT_MAX_L) + Ring<D>::LDS);
+                             plan_bytes(SPLAT_MAX_L, 2) + Ring<D>::LDS);
 }
 
 }  // namespace
