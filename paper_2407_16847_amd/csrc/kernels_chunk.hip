@@ -116,6 +116,15 @@ __device__ __forceinline__ void redo_row(const ChunkArgs& x, const RowRuns* runs
 // and join at the end, and so do workgroups that share out a block's units.
 constexpr int kRows = 32;
 
+// Waits until at most N of this wavefront's loads are on their way.
+template <int N>
+__device__ __forceinline__ void loads_left() {
+  static_assert(N < 64, "vmcnt field");
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | (7 << 4) | (15 << 8));
+  asm volatile("" ::: "memory");
+}
+
 template <typename T, int D>
 constexpr int kStage = kUnit * D * (int)sizeof(T);       // K or V of a unit
 template <typename T, int D>
@@ -169,37 +178,51 @@ __global__ __launch_bounds__(kThreads, sizeof(T) * D > 256 ? 1 : 2) void k_chunk
 
   char* const sk = stage + wave * 2 * kStage<T, D>;
   char* const sv = sk + kStage<T, D>;
-  // the row of the cache that holds this lane's key of unit u, and whether it has one
-  auto slot_of = [&](int u, bool& found) {
-    int j;
-    if (u < plan.dense)
-      j = min(32 * (plan.units()[u] & (kFullUnit - 1)) + qi, ch.len - 1);
-    else
-      j = plan.keys()[min(32 * (u - plan.dense) + qi, plan.gathered - 1)];
-    const int p = page_of(x.pages, b, x.max_pages, x.n_pages, x.page_shift, dbg::idx(j, L, dbg::kKey));
-    found = p >= 0;
-    return cache_row(max(p, 0), x.heads, kh, x.page_shift, j);
+  // A wavefront has one K and one V unit in LDS: the next unit's K is loaded once the
+  // scores are formed, its V once O is, so that loads are always on their way.  Pages
+  // are looked up a unit ahead of that.
+  constexpr int LOADS = kUnit / RPL;
+  const int32_t* const table = x.pages + (int64_t)b * x.max_pages;
+  auto key_of = [&](int u) {
+    const int j = u < plan.dense ? min(32 * (plan.units()[u] & (int)(kFullUnit - 1)) + qi, ch.len - 1)
+                                 : (int)plan.keys()[min(32 * (u - plan.dense) + qi, plan.gathered - 1)];
+    return dbg::idx(j, L, dbg::kKey);
   };
-  int u = u0 + wave;
-  bool found = true;
-  unsigned slot = u < u1 ? slot_of(u, found) : 0;
-  for (; u < u1; u += 4) {
-    wait_lds();   // the unit before it has left the rows that these loads fill
+  auto slot_of = [&](int u, int p, bool& found) {
+    found = p >= 0 && p < x.n_pages;
+    return cache_row(found ? p : 0, x.heads, kh, x.page_shift, key_of(u));
+  };
+  auto issue = [&](const void* from, unsigned slot, char* to) {
 #pragma unroll
-    for (int k = 0; k < kUnit / RPL; ++k) {
+    for (int k = 0; k < LOADS; ++k) {
       const int r = RPL * k + lane / CPR;
       const size_t row = (size_t)(unsigned)__shfl((int)slot, r, 64) * RB;
-      const int c = 16 * ((lane % CPR) ^ swz_row<CPR>(r));
-      dma16((const char*)x.K + row + c, sk + kDmaBlock * k);
-      dma16((const char*)x.V + row + c, sv + kDmaBlock * k);
+      dma16((const char*)from + row + 16 * ((lane % CPR) ^ swz_row<CPR>(r)), to + kDmaBlock * k);
     }
+  };
+  int u = u0 + wave, page = 0;
+  bool found = true, next_found = true;
+  unsigned slot = 0, next = 0;
+  if (u < u1) {
+    slot = slot_of(u, table[key_of(u) >> x.page_shift], found);
+    issue(x.K, slot, sk);
+    if (u + 4 < u1) page = table[key_of(u + 4) >> x.page_shift];
+    issue(x.V, slot, sv);
+  }
+  for (; u < u1; u += 4) {
+    const bool more = u + 4 < u1;
     // which of the unit's keys are the row's: bit r, the key of register r
     const uint32_t mine = register_bits(unit_word(plan, u, runs, row, simple, ch.len), h);
     const uint32_t lost = (uint32_t)__ballot(!found);   // keys without a page
     if (lost) bad = bad || (mine & register_bits(lost, h));
-    if (u + 4 < u1) slot = slot_of(u + 4, found);
-    wait_loads();
+    loads_left<LOADS>();     // K is there
     const f32x16_t sc = dot_staged<T, D>(sk, s, q);
+    if (more) {
+      next = slot_of(u + 4, page, next_found);
+      if (u + 8 < u1) page = table[key_of(u + 8) >> x.page_shift];
+      wait_lds();            // K has been read
+      issue(x.K, next, sk);
+    }
     float p[16], mx = -INFINITY;
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
@@ -223,11 +246,20 @@ __global__ __launch_bounds__(kThreads, sizeof(T) * D > 256 ? 1 : 2) void k_chunk
       p[r] = exp2_hw(p[r] - mu);
       l += p[r];
     }
+    if (more)
+      loads_left<LOADS>();   // V is there
+    else
+      loads_left<0>();
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       typename M::V v;
       load_staged<T, D>(v, sv, s, j);
       M::pv(o, v, p, j);
+    }
+    if (more) {
+      wait_lds();            // V has been read
+      issue(x.V, next, sv);
+      slot = next, found = next_found;
     }
   }
   if (bad) l = NAN;
@@ -814,8 +846,18 @@ hipError_t prepare_chunk() {
   return e;
 }
 
-// As many parts of a block's units as fill the chip with two workgroups a CU while
-// each wavefront keeps two units.
+// Tiles for bf16 blocks of more than 64 rows: 10 tokens of 8 sequences, 4 heads a head of the
+// cache (40 rows), 38.3 us by slices and 35.9 by tiles, but one sequence's 8 tokens, 8
+// heads (64 rows), over 600 keys 13.4 and 19.1.
+//
+// A block's units are shared out among as many workgroups as the chip holds beside
+// each other (more would take a second turn: 4 sequences of 16 fp32 tokens, 12 heads,
+// 36.7 us where 30.7 were to be had) while each wavefront keeps two units, and not
+// at all where joining costs more (about what 14 units of one workgroup take): 300
+// fp32 tokens of 2 sequences under a window of 256, 12 heads, 27.4 us in two
+// parts, 21.2 in one.  One sequence's 32 tokens over 2048 keys, 16 heads: two units a
+// wavefront 13.1 us, four 15.6, eight 20.8; 16 tokens, 32 heads over 8, 8192 keys, d = 128:
+// 23.0, 21.8, 28.5.
 ChunkShape chunk_shape(const DevAcsr& a, int dtype, int B, int H, int heads, int T, int d) {
   ChunkShape s;
   const int64_t rows = (int64_t)T * (H / heads);
@@ -823,9 +865,9 @@ ChunkShape chunk_shape(const DevAcsr& a, int dtype, int B, int H, int heads, int
   const int of = s.tiles ? kTileRows : kRows;
   s.blocks = (int32_t)((rows + of - 1) / of);
   const int64_t units = (std::min(a.max_row_nnz + of, a.L) + kUnit - 1) / kUnit;
-  const int64_t groups = (int64_t)s.blocks * B * heads;
-  const int64_t n = std::min((512 + groups - 1) / groups, (units + 7) / 8);
-  s.splits = (int32_t)std::min<int64_t>(std::max<int64_t>(n, 1), 64);
+  const int64_t groups = (int64_t)s.blocks * B * heads, slots = s.tiles && d == 64 ? 768 : 512;
+  const int64_t n = std::min({std::max<int64_t>(slots / groups, 1), (units + 7) / 8, int64_t(64)});
+  s.splits = units * (n - 1) <= 14 * n ? 1 : (int32_t)n;
   return s;
 }
 

@@ -9,7 +9,7 @@ import paper_2407_16847_amd as splat
 
 @pytest.fixture(scope="module")
 def acsr():
-    return splat.Acsr(splat.Pattern.window(640, 300))
+    return splat.Acsr(splat.Pattern.window(4096, 2000))
 
 
 def test_workspace(acsr):
