@@ -175,29 +175,35 @@ struct RowEnds {
 };
 static_assert(SPLAT_MAX_RUNS == 4 && SPLAT_MAX_L <= 65536, "a run's ends are 16 bits");
 
-// The row's keys of unit u, bit k key k; simple: every run in the wavefront has
-// stride 1.
+// The row's keys among kb .. kb + nk - 1, bit k key kb + k; simple: every run in the
+// wavefront has stride 1.
+__device__ __forceinline__ uint32_t keys_word(const RowRuns* runs, const RowEnds& row, bool simple,
+                                              int kb, int nk) {
+  uint32_t word = 0;
+  if (simple) {
+    const u32x4_t ends = row.ends;
+#pragma unroll
+    for (int k = 0; k < SPLAT_MAX_RUNS; ++k) {
+      const int lo = imax((int)(ends[k] & 0xffff) - kb, 0), hi = imin((int)(ends[k] >> 16) - kb, nk - 1);
+      if (lo <= hi) word |= (~0u << lo) & (~0u >> (31 - hi));
+    }
+  } else {
+    const Run* const r = runs[row.row].r;
+#pragma unroll 1
+    for (int k = 0; k < SPLAT_MAX_RUNS; ++k) word |= (uint32_t)run_tile_bits(r[k], kb, 1, nk);
+  }
+  return word;
+}
+
+// ... of unit u
 __device__ __forceinline__ uint32_t unit_word(const RowsPlan& plan, int u, const RowRuns* runs,
                                               const RowEnds& row, bool simple, int len) {
-  uint32_t word = 0;
   if (u < plan.dense) {
     const uint32_t unit = plan.units()[u];
     if (unit & kFullUnit) return ~0u;
-    const int kb = 32 * unit, nk = imin(32, len - kb);
-    if (simple) {
-      const u32x4_t ends = row.ends;
-#pragma unroll
-      for (int k = 0; k < SPLAT_MAX_RUNS; ++k) {
-        const int lo = imax((int)(ends[k] & 0xffff) - kb, 0), hi = imin((int)(ends[k] >> 16) - kb, nk - 1);
-        if (lo <= hi) word |= (~0u << lo) & (~0u >> (31 - hi));
-      }
-    } else {
-      const Run* const r = runs[row.row].r;
-#pragma unroll 1
-      for (int k = 0; k < SPLAT_MAX_RUNS; ++k) word |= (uint32_t)run_tile_bits(r[k], kb, 1, nk);
-    }
-    return word;
+    return keys_word(runs, row, simple, 32 * unit, imin(32, len - 32 * (int)unit));
   }
+  uint32_t word = 0;
   const uint16_t* const keys = plan.keys() + 32 * (u - plan.dense);
   const int n = imin(32, plan.gathered - 32 * (u - plan.dense));
 #pragma unroll 1

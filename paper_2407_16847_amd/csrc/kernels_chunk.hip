@@ -37,6 +37,16 @@ __device__ __forceinline__ Chunk chunk_of(const ChunkArgs& x, int L, int b) {
   return c;
 }
 
+// i / G and the rest, for i below 2^24: the quotient by a reciprocal is off by one
+// at most.
+__device__ __forceinline__ int divide(int i, int G, float inv, int& rest) {
+  int q = (int)((float)i * inv);
+  rest = i - q * G;
+  if (rest < 0) --q, rest += G;
+  if (rest >= G) ++q, rest -= G;
+  return q;
+}
+
 // The k-th longest sequence (the k-th, of more than 64): workgroups are dealt out in
 // their grid's order, and the long ones had better not come last.
 __device__ __forceinline__ int by_length(const int32_t* lengths, int B, int k) {
@@ -745,82 +755,328 @@ hipError_t chunk_launch(const DevAcsr& a, const ChunkArgs& x, hipStream_t st) {
 
 // ------------------------------------------------------------ weights of keys
 // w_j = decay w_j + sum over the chunk's rows and the group's heads of
-// exp(s_ij - lse_i), the probabilities formed again from the rows' log-sum-exp.  A
-// wavefront has a unit of 32 keys and goes over the rows, 32 at a time; each lane
-// sums its row's 16 keys of the unit, and the lanes' sums meet at the end.
+// exp(s_ij - lse_i), the probabilities formed again from the rows' log-sum-exp: a
+// lane has a row and 16 keys, sums over the rows it sees, and the lanes' sums meet
+// at the end.
+__device__ __forceinline__ void keys_sum(float (&acc)[16], int lane) {
+  // register r's sum over the lanes of a half comes to those whose low bits are r
+  // (picked by bits: the compiler made a selection by index of ?:, 900 instructions)
+#pragma unroll
+  for (int o = 8; o > 0; o >>= 1) {
+    const uint32_t up = lane & o ? ~0u : 0u;
+#pragma unroll
+    for (int r = 0; r < o; ++r) {
+      const uint32_t a = __builtin_bit_cast(uint32_t, acc[r]), b = __builtin_bit_cast(uint32_t, acc[r + o]);
+      const float give = __builtin_bit_cast(float, (a & up) | (b & ~up));
+      acc[r] = __builtin_bit_cast(float, (b & up) | (a & ~up)) + __shfl_xor(give, o, 64);
+    }
+  }
+  acc[0] += __shfl_xor(acc[0], 16, 64);
+}
+// the key, of a unit, whose sum a lane then has
+__device__ __forceinline__ int key_of_lane(int lane) {
+  const int r = lane & 15;
+  return 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3);
+}
+
+// Few rows: the sequences' units of 32 keys are dealt out evenly, whatever the lengths: a
+// workgroup has a contiguous share of those of one head (of 64 sequences at a time), its
+// wavefronts every fourth, the next one's K on its way.  A unit's keys go over the
+// sequence's rows 32 at a time.
 template <typename T, int D>
-__global__ __launch_bounds__(kThreads) void k_weigh(const RowRuns* __restrict__ runs, int L,
-                                                    const WeighArgs x) {
+__global__ __launch_bounds__(kThreads, sizeof(T) * D > 256 ? 1 : 2) void k_weigh(
+    const RowRuns* __restrict__ runs, int L, const WeighArgs x) {
   using M = Mat<T, D>;
-  constexpr int RB = D * (int)sizeof(T), CPR = RB / 16, RPL = 64 / CPR;
-  __shared__ __attribute__((aligned(16))) char lds[4 * kStage<T, D>];
+  constexpr int RB = D * (int)sizeof(T), CPR = RB / 16, RPL = 64 / CPR, LOADS = kUnit / RPL;
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  __shared__ RowEnds ends[4 * kRows];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int qi = lane & 31, h = lane >> 5, G = x.c.group;
-  const int bh = blockIdx.x, kh = bh % x.c.heads, b = bh / x.c.heads;
-  const Chunk ch = chunk_of(x.c, L, b);
-  if (ch.bad) return;
+  const int qi = lane & 31, h = lane >> 5, G = x.c.group, kh = blockIdx.x;
   Slice s;
   s.lane = lane, s.qi = qi, s.h = h;
-  char* const sk = lds + wave * kStage<T, D>;
-  const float sl2 = x.c.scale * kLog2e, fade = ch.n > 0 ? x.decay : 1.f;
-  for (int u = blockIdx.y * 4 + wave; 32 * u < ch.len; u += gridDim.y * 4) {
-    const int kb = 32 * u, nk = min(32, ch.len - kb);
-    const int j = min(kb + qi, ch.len - 1);
-    const int page = page_of(x.c.pages, b, x.c.max_pages, x.c.n_pages, x.c.page_shift, j);
-    const unsigned slot = cache_row(max(page, 0), x.c.heads, kh, x.c.page_shift, j);
-    wait_lds();
+  char* const stage = lds + wave * 2 * kStage<T, D>;
+  const float sl2 = x.c.scale * kLog2e;
+  RowEnds& row = ends[wave * kRows + qi];
+  const int mine = key_of_lane(lane);      // of a unit: the key whose sum this lane writes
+  auto issue = [&](unsigned slot, char* to) {
 #pragma unroll
-    for (int k = 0; k < kUnit / RPL; ++k) {
+    for (int k = 0; k < LOADS; ++k) {
       const int r = RPL * k + lane / CPR;
-      const size_t row = (size_t)(unsigned)__shfl((int)slot, r, 64) * RB;
-      dma16((const char*)x.c.K + row + 16 * ((lane % CPR) ^ swz_row<CPR>(r)), sk + kDmaBlock * k);
+      const size_t at = (size_t)(unsigned)__shfl((int)slot, r, 64) * RB;
+      dma16((const char*)x.c.K + at + 16 * ((lane % CPR) ^ swz_row<CPR>(r)), to + kDmaBlock * k);
     }
-    wait_loads();
-    float acc[16];
-#pragma unroll
-    for (int r = 0; r < 16; ++r) acc[r] = 0.f;
-    for (int r0 = 0; r0 < ch.n * G; r0 += kRows) {
-      const int i = min(r0 + qi, ch.n * G - 1), t = i / G, head = kh * G + i - t * G;
-      const RowRuns rr = runs[dbg::idx(ch.p0 + t, L, dbg::kRow)];
-      const uint32_t word = r0 + qi < ch.n * G ? (uint32_t)tile_row_bits(rr, kb, 1, nk) : 0u;
-      if (!__any(word != 0)) continue;
-      typename M::Row q;
-      load_row<T, D>(q, (const char*)((const T*)x.c.Q + b * x.c.qb + head * x.c.qh + t * x.c.qt), 16u * h);
-      const float lse = x.c.lse[((int64_t)b * x.c.H + head) * x.c.T + t] * kLog2e;
-      const uint32_t mine = lse == -INFINITY ? 0u : register_bits(word, h);
-      const f32x16_t sc = dot_staged<T, D>(sk, s, q);
-#pragma unroll
-      for (int r = 0; r < 16; ++r) acc[r] += mine >> r & 1 ? exp2_hw(sc[r] * sl2 - lse) : 0.f;
+  };
+  for (int b0 = 0; b0 < x.c.B; b0 += 64) {
+    // lane i: sequence b0 + i's length, tokens and the units before it
+    int len = 0, n = 0;
+    if (b0 + lane < x.c.B) {
+      const Chunk c = chunk_of(x.c, L, b0 + lane);
+      len = c.bad ? 0 : c.len, n = c.n;
     }
-    // register r's sum over the rows comes to the lanes whose low bits are r
+    int upto = (len + 31) / 32;
+    const int own = upto;
 #pragma unroll
-    for (int o = 8; o > 0; o >>= 1)
-#pragma unroll
-      for (int r = 0; r < o; ++r) {
-        const bool up = lane & o;
-        const float give = up ? acc[r] : acc[r + o], keep = up ? acc[r + o] : acc[r];
-        acc[r] = keep + __shfl_xor(give, o, 64);
+    for (int o = 1; o < 64; o <<= 1) {
+      const int y = __shfl_up(upto, o, 64);
+      if (lane >= o) upto += y;
+    }
+    const int before = upto - own, all = __builtin_amdgcn_readlane(upto, 63);
+    const int v1 = (int)((int64_t)all * (blockIdx.y + 1) / gridDim.y);
+    int v = (int)((int64_t)all * blockIdx.y / gridDim.y) + wave;
+
+    // unit v: its sequence, number and length there, the place of its key qi
+    struct At {
+      int i, u, len;
+    };
+    auto find = [&](int w) {
+      At a;
+      a.i = __builtin_ctzll(__ballot(upto > w));
+      a.u = w - __builtin_amdgcn_readlane(before, a.i);
+      a.len = __builtin_amdgcn_readlane(len, a.i);
+      return a;
+    };
+    auto page_at = [&](const At& a) {
+      return x.c.pages[(int64_t)(b0 + a.i) * x.c.max_pages + (min(32 * a.u + qi, a.len - 1) >> x.c.page_shift)];
+    };
+    auto slot_of = [&](const At& a, int p, bool& found) {
+      found = p >= 0 && p < x.c.n_pages;
+      return cache_row(found ? p : 0, x.c.heads, kh, x.c.page_shift, min(32 * a.u + qi, a.len - 1));
+    };
+    bool found = false, next_found = false, simple = true;
+    int page = 0, buf = 0, have_i = -1, have_r = -1;
+    unsigned slot = 0, next = 0;
+    At at{0, 0, 0}, ahead{0, 0, 0};
+    typename M::Row q;
+    float lse = 0.f;
+    wait_lds();
+    if (v < v1) {
+      at = find(v);
+      slot = slot_of(at, page_at(at), found);
+      if (v + 4 < v1) ahead = find(v + 4), page = page_at(ahead);
+      issue(slot, stage);
+    }
+    for (; v < v1; v += 4, buf ^= 1) {
+      const int tokens = __builtin_amdgcn_readlane(n, at.i), rows = tokens * G, p0 = at.len - tokens;
+      const int kb = 32 * at.u, b = b0 + at.i;
+      const unsigned to = (unsigned)__shfl((int)slot, mine, 64);
+      const bool writes = __shfl((int)found, mine, 64) && (lane & 16) == 0 && kb + mine < at.len;
+      float old = 0.f;
+      if (writes && kb + mine < p0) old = x.w[to] * (tokens > 0 ? x.decay : 1.f);
+      const At now = at;
+      if (v + 4 < v1) {
+        next = slot_of(ahead, page, next_found);
+        at = ahead;
+        if (v + 8 < v1) ahead = find(v + 8), page = page_at(ahead);
+        wait_lds();              // the unit before has been read
+        issue(next, stage + (buf ^ 1) * kStage<T, D>);
+        loads_left<LOADS>();
+      } else {
+        loads_left<0>();
       }
-    const float sum = acc[0] + __shfl_xor(acc[0], 16, 64);
-    const int r = lane & 15, k = 8 * (r >> 2) + 4 * h + (r & 3);
-    const unsigned at = (unsigned)__shfl((int)slot, k, 64);
-    if (__shfl(page, k, 64) >= 0 && (lane & 16) == 0 && k < nk)
-      x.out[at] = (kb + k < ch.p0 ? x.w[at] * fade : 0.f) + sum;
+      float acc[16];
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[r] = 0.f;
+      for (int r0 = 0; r0 < rows; r0 += kRows) {
+        if (have_i != now.i || have_r != r0) {
+          const int i = min(r0 + qi, rows - 1), t = i / G, head = kh * G + i - t * G;
+          simple = __all(row.open(runs, dbg::idx(p0 + t, L, dbg::kRow)));
+          load_row<T, D>(q, (const char*)((const T*)x.c.Q + b * x.c.qb + head * x.c.qh + t * x.c.qt), 16u * h);
+          lse = x.c.lse[((int64_t)b * x.c.H + head) * x.c.T + t] * kLog2e;
+          have_i = now.i, have_r = r0;
+        }
+        uint32_t word = keys_word(runs, row, simple, kb, min(32, now.len - kb));
+        if (r0 + qi >= rows || lse == -INFINITY) word = 0;
+        if (!__any(word != 0)) continue;
+        const uint32_t bits = register_bits(word, h);
+        const f32x16_t sc = dot_staged<T, D>(stage + buf * kStage<T, D>, s, q);
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          acc[r] += exp2_hw(keep_if_bit(fmaf(sc[r], sl2, -lse), bits, r));
+      }
+      keys_sum(acc, lane);
+      if (writes) x.out[to] = old + acc[0];
+      slot = next, found = next_found;
+    }
   }
+}
+
+// bf16, many rows: a workgroup has 64 keys, whose K stays in its wavefronts'
+// registers, and goes over the rows that see any of them, 128 at a time through a two-slot
+// LDS ring, 32 a wavefront.  A lane forms its row's word of one of the two units.
+template <int D>
+__global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void k_weigh_tiles(
+    const RowRuns* __restrict__ runs, int L, const WeighArgs x) {
+  constexpr int NKS = D / 16, RB = 2 * D, CPR = RB / 16, RPL = 64 / CPR, N = kTileRows / RPL / 4;
+  extern __shared__ __attribute__((aligned(16))) char ring[];
+  __shared__ float sums[4][2][32];
+  __shared__ int span[2];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int qi = lane & 31, h = lane >> 5, G = x.c.group;
+  const int kh = blockIdx.x % x.c.heads, b = by_length(x.c.lengths, x.c.B, blockIdx.x / x.c.heads);
+  const Chunk ch = chunk_of(x.c, L, b);
+  const int kb0 = 64 * blockIdx.y;
+  if (ch.bad || kb0 >= ch.len) return;
+  const int rows = ch.n * G, kb = kb0 + 32 * h, nk = min(32, ch.len - kb);   // of the lane's words
+  // the tokens that see a key of the workgroup's: from, to
+  if (threadIdx.x == 0) span[0] = ch.n, span[1] = -1;
+  __syncthreads();
+  int from = ch.n, to = -1;
+  for (int t = threadIdx.x; t < ch.n; t += kThreads) {
+    const Run* const r = runs[dbg::idx(ch.p0 + t, L, dbg::kRow)].r;
+    bool sees = false;
+#pragma unroll
+    for (int k = 0; k < SPLAT_MAX_RUNS; ++k)
+      sees = sees || (r[k].count > 0 && r[k].start < kb0 + 64 && r[k].start + r[k].stride * (r[k].count - 1) >= kb0);
+    if (sees) from = min(from, t), to = max(to, t);
+  }
+  if (to >= 0) atomicMin(&span[0], from), atomicMax(&span[1], to);
+  // K operand: key qi of each unit, chunk 2 ks + h
+  auto slot_of = [&](int j, bool& found) {
+    const int p = page_of(x.c.pages, b, x.c.max_pages, x.c.n_pages, x.c.page_shift, j);
+    found = p >= 0;
+    return cache_row(max(p, 0), x.c.heads, kh, x.c.page_shift, j);
+  };
+  bf16x8_t ka[2][NKS];
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    bool found;
+    const unsigned slot = slot_of(min(kb0 + 32 * e + qi, ch.len - 1), found);
+#pragma unroll
+    for (int ks = 0; ks < NKS; ++ks)
+      ka[e][ks] = *(const bf16x8_t*)((const char*)x.c.K + (size_t)slot * RB + 32 * ks + 16 * h);
+  }
+  __syncthreads();
+  const int s0 = span[0] * G / kTileRows, s1 = span[1] < 0 ? s0 : (span[1] * G + G - 1) / kTileRows + 1;
+
+  // row r of a stage: its token and head
+  const float inv_G = 1.f / G;
+  auto token_of = [&](int st, int r, int& g) {
+    return divide(min(st * kTileRows + r, rows - 1), G, inv_G, g);
+  };
+  auto issue = [&](int st, char* at) {
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      const int bk = wave + 4 * k, r = bk * RPL + lane / CPR;
+      int g;
+      const int t = token_of(st, r, g);
+      const __bf16* const q = (const __bf16*)x.c.Q + b * x.c.qb + (kh * G + g) * x.c.qh + t * x.c.qt;
+      dma16((const char*)q + 16 * ((lane % CPR) ^ place_k<D>(r)), at + bk * kDmaBlock);
+    }
+  };
+  struct Row {
+    RowRuns rr;
+    float lse;
+  };
+  auto fetch = [&](int st) {               // this lane's row of the wavefront's 32
+    int g;
+    const int t = token_of(st, 32 * wave + qi, g);
+    return Row{runs[dbg::idx(ch.p0 + t, L, dbg::kRow)],
+               x.c.lse[((int64_t)b * x.c.H + kh * G + g) * x.c.T + t] * kLog2e};
+  };
+  auto word_of = [&](int st, const Row& w) {
+    uint32_t word = 0;
+    if (st * kTileRows + 32 * wave + qi >= rows || w.lse == -INFINITY || nk <= 0) return word;
+#pragma unroll
+    for (int k = 0; k < SPLAT_MAX_RUNS; ++k) {
+      const Run& r = w.rr.r[k];
+      if (r.count <= 0) continue;
+      if (r.stride == 1) {
+        const int lo = max(r.start - kb, 0), hi = min(r.start + r.count - 1 - kb, nk - 1);
+        if (lo <= hi) word |= (~0u << lo) & (~0u >> (31 - hi));
+      } else {
+        word |= (uint32_t)run_tile_bits(r, kb, 1, nk);
+      }
+    }
+    return word;
+  };
+
+  float acc[2][16];
+#pragma unroll
+  for (int e = 0; e < 2; ++e)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) acc[e][r] = 0.f;
+  const float sl2 = x.c.scale * kLog2e;
+  const int koff = (32 * wave + qi) * RB + 16 * (h ^ place_k<D>(qi));
+  if (s0 < s1) {
+    Row w = fetch(s0);
+    uint32_t word = word_of(s0, w);
+    float lse = w.lse;
+    w = fetch(min(s0 + 1, s1 - 1));
+    issue(s0, ring);
+    ring_sync<0>();
+    for (int st = s0; st < s1; ++st) {
+      const char* const sq = ring + ((st - s0) & 1) * kTileRows * RB;
+      // the next stage's words, and the loads of the one after, ahead of its rows'
+      const uint32_t next_word = word_of(st + 1, w);
+      const float next_lse = w.lse;
+      w = fetch(min(st + 2, s1 - 1));
+      if (st + 1 < s1) issue(st + 1, ring + (~(st - s0) & 1) * kTileRows * RB);
+      if (__any(word != 0)) {
+        const uint32_t other = __builtin_bit_cast(uint32_t, lane_xor32(__builtin_bit_cast(float, word)));
+        bf16x8_t qb[NKS];
+#pragma unroll
+        for (int ks = 0; ks < NKS; ++ks) qb[ks] = *(const bf16x8_t*)(sq + (koff ^ (32 * ks)));
+        const bool whole = __all(word == ~0u);
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          f32x16_t s;
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[r] = 0.f;
+#pragma unroll
+          for (int ks = 0; ks < NKS; ++ks) s = mfma32(ka[e][ks], qb[ks], s);
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], sl2, -lse);
+          if (!whole) {
+            const uint32_t bits = register_bits(e == h ? word : other, h);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[r] = keep_if_bit(s[r], bits, r);
+          }
+#pragma unroll
+          for (int r = 0; r < 16; ++r) acc[e][r] += exp2_hw(s[r]);
+        }
+      }
+      word = next_word, lse = next_lse;
+      ring_sync<0>();
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    keys_sum(acc[e], lane);
+    if ((lane & 16) == 0) sums[wave][e][key_of_lane(lane)] = acc[e][0];
+  }
+  __syncthreads();
+  const int j = kb0 + (int)threadIdx.x;
+  if (threadIdx.x >= 64 || j >= ch.len) return;
+  bool found;
+  const unsigned at = slot_of(j, found);
+  if (!found) return;
+  const int e = threadIdx.x >> 5, k = threadIdx.x & 31;
+  const float old = j < ch.p0 ? x.w[at] * (ch.n > 0 ? x.decay : 1.f) : 0.f;
+  x.out[at] = old + ((sums[0][e][k] + sums[1][e][k]) + (sums[2][e][k] + sums[3][e][k]));
 }
 
 template <typename T, int D>
 hipError_t weigh_launch(const DevAcsr& a, const WeighArgs& x, hipStream_t st) {
   const int64_t room = std::min<int64_t>((int64_t)x.c.max_pages << x.c.page_shift, a.L);
-  const int64_t groups = (int64_t)x.c.B * x.c.heads;
-  const int64_t parts = std::min((room + 4 * kUnit - 1) / (4 * kUnit), (4096 + groups - 1) / groups);
-  hipLaunchKernelGGL((k_weigh<T, D>), dim3((unsigned)groups, (unsigned)parts), dim3(kThreads), 0, st,
-                     a.runs, a.L, x);
+  const int64_t heads = x.c.heads, groups = x.c.B * heads;
+  if constexpr (sizeof(T) == 2) {
+    if (x.c.T * x.c.group > 64) {
+      hipLaunchKernelGGL((k_weigh_tiles<D>), dim3((unsigned)groups, (unsigned)((room + 63) / 64)),
+                         dim3(kThreads), (2 * kTileRows * 2 * D), st, a.runs, a.L, x);
+      return hipGetLastError();
+    }
+  }
+  const int64_t parts = std::min((room + 4 * kUnit - 1) / (4 * kUnit) * x.c.B, (1024 + heads - 1) / heads);
+  hipLaunchKernelGGL((k_weigh<T, D>), dim3((unsigned)heads, (unsigned)parts), dim3(kThreads),
+                     (8 * kStage<T, D>), st, a.runs, a.L, x);
   return hipGetLastError();
 }
 
 template <typename T, int D>
 hipError_t allow_lds() {
+  const hipError_t e = hipFuncSetAttribute(
+      (const void*)k_weigh<T, D>, hipFuncAttributeMaxDynamicSharedMemorySize, 8 * kStage<T, D>);
+  if (e != hipSuccess) return e;
   return hipFuncSetAttribute((const void*)k_chunk_slices<T, D>,
                              hipFuncAttributeMaxDynamicSharedMemorySize,
                              plan_bytes(SPLAT_MAX_L) + kSliceLds<T, D>);
@@ -828,6 +1084,9 @@ hipError_t allow_lds() {
 
 template <int D>
 hipError_t allow_tiles_lds() {
+  const hipError_t e = hipFuncSetAttribute(
+      (const void*)k_weigh_tiles<D>, hipFuncAttributeMaxDynamicSharedMemorySize, 2 * kTileRows * 2 * D);
+  if (e != hipSuccess) return e;
   return hipFuncSetAttribute((const void*)k_chunk_tiles<D>, hipFuncAttributeMaxDynamicSharedMemorySize,
                              plan_bytes(SPLAT_MAX_L, 2) + Ring<D>::LDS);
 }
