@@ -905,16 +905,18 @@ __global__ __launch_bounds__(kThreads, sizeof(T) * D > 256 ? 1 : 2) void k_weigh
 // LDS ring, 32 a wavefront.  A lane forms its row's word of one of the two units.
 template <int D>
 __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void k_weigh_tiles(
-    const RowRuns* __restrict__ runs, int L, const WeighArgs x) {
+    const RowRuns* __restrict__ runs, int L, const WeighArgs x, int blocks) {
   constexpr int NKS = D / 16, RB = 2 * D, CPR = RB / 16, RPL = 64 / CPR, N = kTileRows / RPL / 4;
   extern __shared__ __attribute__((aligned(16))) char ring[];
   __shared__ float sums[4][2][32];
   __shared__ int span[2];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int qi = lane & 31, h = lane >> 5, G = x.c.group;
-  const int kh = blockIdx.x % x.c.heads, b = by_length(x.c.lengths, x.c.B, blockIdx.x / x.c.heads);
+  // a sequence's blocks of keys in a row, so that they lie on all of the chip's dies;
+  // the longest sequence first
+  const int bh = blockIdx.x / blocks, kb0 = 64 * (blockIdx.x - bh * blocks);
+  const int kh = bh % x.c.heads, b = by_length(x.c.lengths, x.c.B, bh / x.c.heads);
   const Chunk ch = chunk_of(x.c, L, b);
-  const int kb0 = 64 * blockIdx.y;
   if (ch.bad || kb0 >= ch.len) return;
   const int rows = ch.n * G, kb = kb0 + 32 * h, nk = min(32, ch.len - kb);   // of the lane's words
   // the tokens that see a key of the workgroup's: from, to
@@ -1061,8 +1063,9 @@ hipError_t weigh_launch(const DevAcsr& a, const WeighArgs& x, hipStream_t st) {
   const int64_t heads = x.c.heads, groups = x.c.B * heads;
   if constexpr (sizeof(T) == 2) {
     if (x.c.T * x.c.group > 64) {
-      hipLaunchKernelGGL((k_weigh_tiles<D>), dim3((unsigned)groups, (unsigned)((room + 63) / 64)),
-                         dim3(kThreads), (2 * kTileRows * 2 * D), st, a.runs, a.L, x);
+      const int blocks = (int)((room + 63) / 64);
+      hipLaunchKernelGGL((k_weigh_tiles<D>), dim3((unsigned)(groups * blocks)), dim3(kThreads),
+                         (2 * kTileRows * 2 * D), st, a.runs, a.L, x, blocks);
       return hipGetLastError();
     }
   }
