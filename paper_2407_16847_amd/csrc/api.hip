@@ -1192,7 +1192,8 @@ splat_status splat_sparse_mhsa_chunk(splat_acsr_t h, splat_dtype dtype, int32_t 
   x.B = B, x.H = H, x.heads = heads, x.group = H / heads, x.T = T;
   x.max_pages = (int32_t)cache->max_pages, x.n_pages = (int32_t)cache->n_pages;
   x.page_shift = log2_of(cache->page);
-  x.tiles = s.tiles, x.blocks = s.blocks, x.splits = s.splits, x.scale = scale, x.ws = (float*)workspace;
+  x.tiles = s.tiles, x.blocks = s.blocks, x.splits = s.splits, x.cap = s.cap, x.most = s.most;
+  x.scale = scale, x.ws = (float*)workspace;
   return launched(splat::launch_chunk(h->dev, dtype, d, x, (hipStream_t)stream), "sparse_mhsa_chunk");
 }
 

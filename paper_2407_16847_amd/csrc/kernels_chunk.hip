@@ -61,6 +61,44 @@ __device__ __forceinline__ int by_length(const int32_t* lengths, int B, int k) {
   return __builtin_ctzll(__ballot(lane < B && rank == k));
 }
 
+// Where a block's units are shared out, B * splits workgroups share out those of all
+// sequences: each sequence has parts by its length (`splits` of them where there is one, or
+// more than 64), at most x.cap.
+struct Parts {
+  int n, before;      // lane b: sequence b's parts, and those of the sequences before
+};
+__device__ __forceinline__ bool parts_vary(const ChunkArgs& x) { return x.cap != x.splits; }
+__device__ __forceinline__ Parts parts_of(const ChunkArgs& x) {
+  const int lane = threadIdx.x & 63;
+  const int units = lane < x.B ? (min(max(x.lengths[lane], 1), x.most) + 31) / 32 : 0;
+  int sum = units;
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
+  Parts p;
+  p.n = lane < x.B ? min(1 + units * (x.B * (x.splits - 1)) / sum, x.cap) : 0;
+  int upto = p.n;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int y = __shfl_up(upto, o, 64);
+    if (lane >= o) upto += y;
+  }
+  p.before = upto - p.n;
+  return p;
+}
+// workgroup k of B * splits: its sequence (-1: none), part and how many of them
+__device__ __forceinline__ int part_of(const ChunkArgs& x, int k, int& split, int& splits) {
+  if (!parts_vary(x)) {
+    splits = x.splits, split = k % splits;
+    return k / splits;
+  }
+  const Parts p = parts_of(x);
+  const uint64_t here = __ballot(k >= p.before && k < p.before + p.n);
+  if (!here) return -1;
+  const int b = __builtin_ctzll(here);
+  splits = __builtin_amdgcn_readlane(p.n, b), split = k - __builtin_amdgcn_readlane(p.before, b);
+  return b;
+}
+
 // O and lse of one row by one wavefront, from the row's own keys alone.
 template <typename T, int D>
 __device__ __forceinline__ void row_alone(const ChunkArgs& x, const RowRuns& rr, int b, int kh, int len,
@@ -153,12 +191,15 @@ __global__ __launch_bounds__(kThreads, sizeof(T) * D > 256 ? 1 : 2) void k_chunk
   __shared__ RowEnds ends[4 * kRows];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int qi = lane & 31, h = lane >> 5;
-  const int bh = blockIdx.x % (x.B * x.heads), block = x.blocks - 1 - blockIdx.x / (x.B * x.heads);
-  const int kh = bh % x.heads, b = bh / x.heads;
-  const int split = blockIdx.y, splits = x.splits, G = x.group;
+  // workgroups of one sequence and head share its keys: neighbours on a die
+  const int kh = blockIdx.x % x.heads, rest = blockIdx.x / x.heads, shares = x.B * x.splits;
+  const int block = x.blocks - 1 - rest / shares, G = x.group;
+  int split, splits;
+  const int b = part_of(x, rest % shares, split, splits);
+  if (b < 0) return;
   const Chunk ch = chunk_of(x, L, b);
   const int r0 = block * kRows, rows = min(kRows, ch.n * G - r0);   // rows that count
-  if (splits > 1 && rows <= 0) return;                 // the joining kernel clears the padding
+  if (x.splits > 1 && rows <= 0) return;                 // the joining kernel clears the padding
 
   const int i = r0 + min(qi, max(rows - 1, 0)), t = i / G, g = i - t * G;
   RowsPlan plan(lds, L);
@@ -303,9 +344,9 @@ __global__ __launch_bounds__(kThreads, sizeof(T) * D > 256 ? 1 : 2) void k_chunk
     lt += stat[w * 64 + 32 + r] * (mw == -INFINITY ? 1.f : f[w]);
   }
   const int64_t head = (int64_t)b * x.H + kh * G + rg;
-  if (splits > 1) {
+  if (x.splits > 1) {
     if (r >= rows) return;
-    float* const to = x.ws + ((head * x.T + rt) * splits + split) * (D + 2);
+    float* const to = x.ws + ((head * x.T + rt) * x.cap + split) * (D + 2);
 #pragma unroll
     for (int k = 0; k < NB; ++k) {
       const int c = 4 * (threadIdx.x & 7) + 32 * k;
@@ -399,12 +440,17 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void k_chunk_tiles(
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int qi = lane & 31, h = lane >> 5;
   // the longest sequence's blocks first, of each the last (longest) first
-  const int kh = blockIdx.x % x.heads, rest = blockIdx.x / x.heads;
-  const int block = x.blocks - 1 - rest % x.blocks, b = by_length(x.lengths, x.B, rest / x.blocks);
-  const int split = blockIdx.y, splits = x.splits, G = x.group;
+  const int kh = blockIdx.x % x.heads, rest = blockIdx.x / x.heads, G = x.group;
+  const int block = x.blocks - 1 - rest % x.blocks;
+  int split = 0, splits = 1, b;
+  if (x.splits > 1)
+    b = part_of(x, rest / x.blocks, split, splits);
+  else
+    b = by_length(x.lengths, x.B, rest / x.blocks);
+  if (b < 0) return;
   const Chunk ch = chunk_of(x, L, b);
   const int r0 = block * kTileRows, rows = min(kTileRows, ch.n * G - r0);   // rows that count
-  if (splits > 1 && rows <= 0) return;                 // the joining kernel clears the padding
+  if (x.splits > 1 && rows <= 0) return;                 // the joining kernel clears the padding
 
   int mine = wave * 32 + qi;                           // this lane's row of the block
   RowsPlan plan(lds, L, tiles_sub(x.page_shift));
@@ -625,9 +671,9 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void k_chunk_tiles(
   const bool counts = mine < rows;
   const int ri = r0 + mine, rt = ri / G;
   const int64_t place = ((int64_t)b * x.H + kh * G + ri - rt * G) * x.T + rt;   // of lse
-  if (splits > 1) {
+  if (x.splits > 1) {
     if (!counts) return;
-    float* const to = x.ws + (place * splits + split) * (D + 2);
+    float* const to = x.ws + (place * x.cap + split) * (D + 2);
     if (h == 0) *(f32x2_t*)to = f32x2_t{set ? m : -INFINITY, l};
 #pragma unroll
     for (int c = 0; c < NDB; ++c)
@@ -682,7 +728,7 @@ template <typename T, int D>
 __global__ __launch_bounds__(64) void k_chunk_join(const RowRuns* __restrict__ runs, int L,
                                                    const ChunkArgs x) {
   constexpr int STEP = 8;
-  const int lane = threadIdx.x, splits = x.splits;
+  const int lane = threadIdx.x;
   const int64_t row = blockIdx.x;
   const int t = (int)(row % x.T), head = (int)(row / x.T % x.H), b = (int)(row / x.T / x.H);
   const Chunk ch = chunk_of(x, L, b);
@@ -693,7 +739,8 @@ __global__ __launch_bounds__(64) void k_chunk_join(const RowRuns* __restrict__ r
     if (lane == 0) x.lse[row] = -INFINITY;
     return;
   }
-  const float* const part = x.ws + row * splits * (D + 2);
+  const int splits = parts_vary(x) ? __builtin_amdgcn_readlane(parts_of(x).n, b) : x.splits;
+  const float* const part = x.ws + row * x.cap * (D + 2);
   float m = -INFINITY, l = 0.f;
   if (lane < splits) {
     const f32x2_t ml = *(const f32x2_t*)(part + lane * (D + 2));
@@ -737,7 +784,7 @@ __global__ __launch_bounds__(64) void k_chunk_join(const RowRuns* __restrict__ r
 
 template <typename T, int D>
 hipError_t chunk_launch(const DevAcsr& a, const ChunkArgs& x, hipStream_t st) {
-  const dim3 grid((unsigned)((int64_t)x.blocks * x.B * x.heads), x.splits);
+  const dim3 grid((unsigned)((int64_t)x.blocks * x.B * x.heads * x.splits));
   if constexpr (sizeof(T) == 2) {
     if (x.tiles)
       hipLaunchKernelGGL((k_chunk_tiles<D>), grid, dim3(kThreads),
@@ -1130,11 +1177,13 @@ ChunkShape chunk_shape(const DevAcsr& a, int dtype, int B, int H, int heads, int
   const int64_t groups = (int64_t)s.blocks * B * heads, slots = s.tiles && d == 64 ? 768 : 512;
   const int64_t n = std::min({std::max<int64_t>(slots / groups, 1), (units + 7) / 8, int64_t(64)});
   s.splits = units * (n - 1) <= 14 * n ? 1 : (int32_t)n;
+  s.cap = s.splits == 1 || B == 1 || B > 64 ? s.splits : std::min(2 * s.splits, 64);
+  s.most = (int32_t)std::min(a.max_row_nnz + of, a.L);
   return s;
 }
 
 int64_t chunk_workspace(const ChunkShape& s, int B, int H, int T, int d) {
-  return s.splits == 1 ? 0 : (int64_t)B * H * T * s.splits * (d + 2);
+  return s.splits == 1 ? 0 : (int64_t)B * H * T * s.cap * (d + 2);
 }
 
 hipError_t launch_chunk(const DevAcsr& a, int dtype, int d, const ChunkArgs& x, hipStream_t st) {

@@ -164,13 +164,15 @@ struct ChunkArgs {
   int64_t qb, qh, qt, ob, oh, ot;
   int32_t B, H, heads, group, T, max_pages, n_pages, page_shift;
   bool tiles;                 // blocks of 128 rows, not 32
-  int32_t blocks, splits;     // of a (sequence, head of the cache)'s rows, of a block's keys
+  // of a (sequence, head of the cache)'s rows; of a block's keys, on average and at most;
+  // the keys that a block may have
+  int32_t blocks, splits, cap, most;
   float scale;
   float* ws;
 };
 struct ChunkShape {
   bool tiles;
-  int32_t blocks, splits;
+  int32_t blocks, splits, cap, most;
 };
 ChunkShape chunk_shape(const DevAcsr& a, int dtype, int B, int H, int heads, int T, int d);
 int64_t chunk_workspace(const ChunkShape& s, int B, int H, int T, int d);   // floats
