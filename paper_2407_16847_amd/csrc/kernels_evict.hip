@@ -17,10 +17,10 @@ using mfma::u32x4_t;
 
 // ------------------------------------------------------------- which keys stay
 // One workgroup per (sequence, head of the cache).  The weights, as integers in the
-// same order, stay in registers; the K-th largest of them is found bit by bit from
-// the top, each step counting the weights that are no smaller than a trial value.
-// Equal weights at that value stay from the lowest place on.  Bound by the latency
-// of 32 counts over the workgroup.
+// same order, stay in registers; the K-th largest of them is found 8 bits at a time from
+// the top, by histograms of those that agree with it so far.  Equal weights at that value
+// stay from the lowest place on.  Bound by latency: pages and weights one behind the other, two
+// barriers and a scan a digit, two scans for the places.
 constexpr int kSelThreads = 1024, kSelWaves = kSelThreads / 64;
 
 // The weights' order as that of unsigned integers: a NaN is the largest, -0 is 0.
@@ -52,7 +52,7 @@ __device__ __forceinline__ void scan(int* x, int n, int* wave_sums) {
 
 template <int V>
 __global__ __launch_bounds__(kSelThreads) void k_evict_select(const EvictArgs x) {
-  __shared__ int part[V * kSelWaves], sums[kSelWaves], counts[2][kSelWaves];
+  __shared__ int part[V * kSelWaves], sums[kSelWaves], hist[256], found[3];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int b = blockIdx.x / x.heads, h = blockIdx.x - b * x.heads;
@@ -67,50 +67,63 @@ __global__ __launch_bounds__(kSelThreads) void k_evict_select(const EvictArgs x)
   // place v * kSelThreads + tid of the sequence; the middle ones compete for `room`
   const int last = n - x.recent, room = x.budget - x.first - x.recent;
   uint32_t key[V];
+  constexpr int STEP = V < 16 ? V : 16;    // pages' and weights' loads in flight
 #pragma unroll
-  for (int v = 0; v < V; ++v) {
-    const int j = v * kSelThreads + tid;
-    key[v] = 0;       // a place without a page goes first
-    if (j < n) {
-      const int p = page_of(x.pages, b, x.max_pages, x.n_pages, x.page_shift, j);
-      if (p >= 0) key[v] = order_of(x.w[cache_row(p, x.heads, h, x.page_shift, j)]);
+  for (int v0 = 0; v0 < V; v0 += STEP) {
+    if (v0 * kSelThreads >= n) break;
+    int page[STEP];
+#pragma unroll
+    for (int v = 0; v < STEP; ++v)
+      page[v] = x.pages[(int64_t)b * x.max_pages +
+                        (min((v0 + v) * kSelThreads + tid, n - 1) >> x.page_shift)];
+#pragma unroll
+    for (int v = 0; v < STEP; ++v) {
+      const bool ok = page[v] >= 0 && page[v] < x.n_pages;
+      const int j = min((v0 + v) * kSelThreads + tid, n - 1);
+      const float w = x.w[cache_row(ok ? page[v] : 0, x.heads, h, x.page_shift, j)];
+      key[v0 + v] = ok ? order_of(w) : 0;  // a place without a page goes first
     }
   }
   auto middle = [&](int v) {
     const int j = v * kSelThreads + tid;
     return j >= x.first && j < last;
   };
+  // `least`: the room-th largest of the middle ones, or a value that as many reach;
+  // `above`: how many surely stay; ties: more equal it than may stay
   uint32_t least = 0;
   int above = 0;
-  if (room > 0) {
-    // the largest `least` that `room` of the middle weights reach
-    for (int bit = 31; bit >= 0; --bit) {
-      const uint32_t trial = least | 1u << bit;
-      int c = 0;
-#pragma unroll
-      for (int v = 0; v < V; ++v) {
-        if (v * kSelThreads >= n) break;
-        c += __popcll(__ballot(middle(v) && key[v] >= trial));
-      }
-      int* const to = counts[bit & 1];
-      if (lane == 0) to[wave] = c;
-      __syncthreads();
-      int all = 0;
-#pragma unroll
-      for (int w = 0; w < kSelWaves; ++w) all += to[w];
-      if (all >= room) least = trial;
-    }
-    int c = 0;
+  bool ties = false;
+  for (int shift = 24; room > 0 && shift >= 0; shift -= 8) {
+    if (tid < 256) hist[tid] = 0;
+    __syncthreads();
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       if (v * kSelThreads >= n) break;
-      c += __popcll(__ballot(middle(v) && key[v] > least));
+      if (middle(v) && (uint64_t)(key[v] ^ least) >> (shift + 8) == 0) atomicAdd(&hist[key[v] >> shift & 255], 1);
     }
     __syncthreads();
-    if (lane == 0) counts[0][wave] = c;
-    __syncthreads();
+    if (wave == 0) {                       // lane l: digits 255 - 4 l and the three below
+      int c[4], own = 0;
 #pragma unroll
-    for (int w = 0; w < kSelWaves; ++w) above += counts[0][w];
+      for (int e = 0; e < 4; ++e) c[e] = hist[255 - 4 * lane - e], own += c[e];
+      int upto = own;
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const int y = __shfl_up(upto, o, 64);
+        if (lane >= o) upto += y;
+      }
+      int before = above + upto - own;
+      if (before < room && before + own >= room)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          if (before < room && before + c[e] >= room) found[0] = 255 - 4 * lane - e, found[1] = before, found[2] = c[e];
+          before += c[e];
+        }
+    }
+    __syncthreads();
+    least |= (uint32_t)found[0] << shift, above = found[1];
+    ties = above + found[2] > room;
+    if (!ties) break;                      // all that begin so stay
   }
   // places in order: 64 at a time by (v, wave)
   const uint64_t before = ((uint64_t)1 << lane) - 1;
@@ -127,15 +140,17 @@ __global__ __launch_bounds__(kSelThreads) void k_evict_select(const EvictArgs x)
     scan(part, V * kSelWaves, sums);
   };
   auto equal = [&](int v) { return middle(v) && key[v] == least; };
-  ranks(equal);
+  if (ties) ranks(equal);
   uint64_t keep = 0;        // bit v: the place stays
 #pragma unroll
   for (int v = 0; v < V; ++v) {
     if (v * kSelThreads >= n) break;
     const int j = v * kSelThreads + tid;
-    const int rank = part[v * kSelWaves + wave] + __popcll(__ballot(equal(v)) & before);
-    const bool stays = middle(v) ? room > 0 && (key[v] > least || (equal(v) && rank < room - above))
-                                 : j < n;
+    bool stays = middle(v) ? room > 0 && key[v] >= least : j < n;
+    if (ties) {
+      const int rank = part[v * kSelWaves + wave] + __popcll(__ballot(equal(v)) & before);
+      stays = stays && !(equal(v) && rank >= room - above);
+    }
     keep |= (uint64_t)stays << v;
   }
   __syncthreads();
