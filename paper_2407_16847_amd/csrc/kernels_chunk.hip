@@ -575,6 +575,7 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void k_chunk_tiles(
     if (u + h < u1) word = unit_word(plan, u + h, runs, row, simple, ch.len);
     const uint32_t other = __builtin_bit_cast(uint32_t, lane_xor32(__builtin_bit_cast(float, word)));
     if (__any(word != 0)) {
+      __builtin_amdgcn_s_setprio(1);
       const bool whole = __all(word == ~0u);
       f32x16_t s[2];
 #pragma unroll
@@ -588,6 +589,7 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void k_chunk_tiles(
 #pragma unroll
         for (int ks = 0; ks < NKS; ++ks) s[half] = mfma32(ka[ks], q[ks], s[half]);
       }
+      __builtin_amdgcn_s_setprio(0);
       // against the row's reference, in powers of 2
 #pragma unroll
       for (int half = 0; half < 2; ++half)
@@ -642,6 +644,7 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void k_chunk_tiles(
         lt = exps();
       }
       l += lt;
+      __builtin_amdgcn_s_setprio(1);
       // V^T a block of 32 features at a time, the next one's reads in flight where
       // registers allow (d = 64 has four wavefronts a SIMD instead)
       const unsigned sv = lds_addr(sk + R::TB);
@@ -659,6 +662,7 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void k_chunk_tiles(
 #pragma unroll
         for (int j = 0; j < 4; ++j) o[c] = mfma32(va[c % N][j], pf[j], o[c]);
       }
+      __builtin_amdgcn_s_setprio(0);
     }
     ring_sync<0>();
   }
