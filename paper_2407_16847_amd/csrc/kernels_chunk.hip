@@ -399,10 +399,25 @@ __global__ __launch_bounds__(kThreads, sizeof(T) * D > 256 ? 1 : 2) void k_chunk
 constexpr int kTileRows = 128;
 constexpr float kSumLimit = 4096.f;
 
-// Waits until at most N of this wavefront's LDS reads are on their way; the operands
-// of a block read before them depend on it.
+// V^T of a tile's keys 16 J .. 16 (J + NJ) - 1 and one block of 32 features (the transposing
+// reads of read_v_block).
+template <int D, int J, int NJ, int K = 0>
+__device__ __forceinline__ void read_v_part(unsigned at, bf16x8_t (&v)[NJ]) {
+  constexpr int RB = 2 * D;
+  if constexpr (K < NJ) {
+    v[K] = __builtin_shufflevector(tr16_async_at<16 * (J + K) * RB>(at),
+                                   tr16_async_at<16 * (J + K) * RB + 8 * RB>(at), 0, 1, 2, 3, 4, 5, 6, 7);
+    read_v_part<D, J, NJ, K + 1>(at, v);
+  }
+}
+// Waits until at most N of this wavefront's LDS reads are on their way; what was read
+// before them depends on it.
 template <int N>
-__device__ __forceinline__ void block_wait(bf16x8_t (&v)[4]) {
+__device__ __forceinline__ void part_wait(bf16x8_t (&v)[2]) {
+  asm volatile("s_waitcnt lgkmcnt(%2)" : "+v"(v[0]), "+v"(v[1]) : "n"(N));
+}
+template <int N>
+__device__ __forceinline__ void part_wait(bf16x8_t (&v)[4]) {
   asm volatile("s_waitcnt lgkmcnt(%4)" : "+v"(v[0]), "+v"(v[1]), "+v"(v[2]), "+v"(v[3]) : "n"(N));
 }
 
@@ -429,7 +444,7 @@ __host__ __device__ constexpr int tiles_sub(int page_shift) {
 }
 
 template <int D>
-__global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void k_chunk_tiles(
+__global__ __launch_bounds__(kThreads, D == 64 ? 4 : 2) void k_chunk_tiles(
     const RowRuns* __restrict__ runs, int L, const ChunkArgs x) {
   using R = Ring<D>;
   constexpr int NKS = D / 16, NDB = D / 32, RB = R::RB;
@@ -574,39 +589,44 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void k_chunk_tiles(
     uint32_t word = 0;
     if (u + h < u1) word = unit_word(plan, u + h, runs, row, simple, ch.len);
     const uint32_t other = __builtin_bit_cast(uint32_t, lane_xor32(__builtin_bit_cast(float, word)));
-    if (__any(word != 0)) {
+    // ... one unit after the other, or (d = 128) both at once
+    auto pass = [&](auto FIRST) {
+      constexpr int E = FIRST, NE = D == 64 ? 1 : 2;      // units E .. E + NE - 1
+      const uint32_t seen = NE == 2 ? word | other : (h == E ? word : other);
+      if (!__any(seen != 0)) return;
+      const bool whole = NE == 2 ? __all(word == ~0u) : __all(seen == ~0u);
       __builtin_amdgcn_s_setprio(1);
-      const bool whole = __all(word == ~0u);
-      f32x16_t s[2];
+      f32x16_t s[NE];
 #pragma unroll
-      for (int half = 0; half < 2; ++half) {
+      for (int e = 0; e < NE; ++e) {
         bf16x8_t ka[NKS];
 #pragma unroll
-        for (int ks = 0; ks < NKS; ++ks) 
-          ka[ks] = *(const bf16x8_t*)(sk + (koff ^ (32 * ks)) + half * 32 * RB);
+        for (int ks = 0; ks < NKS; ++ks)
+          ka[ks] = *(const bf16x8_t*)(sk + (koff ^ (32 * ks)) + (E + e) * 32 * RB);
 #pragma unroll
-        for (int r = 0; r < 16; ++r) s[half][r] = 0.f;
+        for (int r = 0; r < 16; ++r) s[e][r] = 0.f;
 #pragma unroll
-        for (int ks = 0; ks < NKS; ++ks) s[half] = mfma32(ka[ks], q[ks], s[half]);
+        for (int ks = 0; ks < NKS; ++ks) s[e] = mfma32(ka[ks], q[ks], s[e]);
       }
       __builtin_amdgcn_s_setprio(0);
       // against the row's reference, in powers of 2
 #pragma unroll
-      for (int half = 0; half < 2; ++half)
+      for (int e = 0; e < NE; ++e)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) s[half][r] = fmaf(s[half][r], sl2, -m);
+        for (int r = 0; r < 16; ++r) s[e][r] = fmaf(s[e][r], sl2, -m);
       if (!whole) {
-        const uint32_t bits = register_bits(h ? other : word, h) | register_bits(h ? word : other, h) << 16;
 #pragma unroll
-        for (int half = 0; half < 2; ++half)
+        for (int e = 0; e < NE; ++e) {
+          const uint32_t bits = register_bits(h == E + e ? word : other, h);
 #pragma unroll
-          for (int r = 0; r < 16; ++r) s[half][r] = keep_if_bit(s[half][r], bits, 16 * half + r);
+          for (int r = 0; r < 16; ++r) s[e][r] = keep_if_bit(s[e][r], bits, r);
+        }
       }
-      bf16x8_t pf[4];
+      bf16x8_t pf[2 * NE];
       auto exps = [&]() {
         float l0 = 0.f, l1 = 0.f;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        for (int j = 0; j < 2 * NE; ++j) {
           float e8[8];
 #pragma unroll
           for (int e = 0; e < 8; ++e) e8[e] = exp2_hw(s[j >> 1][(j & 1) * 8 + e]);
@@ -620,12 +640,12 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void k_chunk_tiles(
       float lt = exps();
       // (both halves of the lanes decide alike: a row's sum and its keys are theirs together)
       const float both = lt + lane_xor32(lt);
-      if (__any(!(both <= kSumLimit) || (!set && (word | other) != 0))) {
+      if (__any(!(both <= kSumLimit) || (!set && seen != 0))) {
         float mx = -INFINITY;
 #pragma unroll
-        for (int half = 0; half < 2; ++half)
+        for (int e = 0; e < NE; ++e)
 #pragma unroll
-          for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[half][r]);
+          for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[e][r]);
         mx = fmaxf(mx, lane_xor32(mx));
         // a row without weight has no reference yet
         const float up = !set ? (mx == -INFINITY ? 0.f : mx) : fmaxf(0.f, mx);
@@ -638,32 +658,32 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void k_chunk_tiles(
         set = set || mx != -INFINITY;
         m += up;
 #pragma unroll
-        for (int half = 0; half < 2; ++half)
+        for (int e = 0; e < NE; ++e)
 #pragma unroll
-          for (int r = 0; r < 16; ++r) s[half][r] -= up;
+          for (int r = 0; r < 16; ++r) s[e][r] -= up;
         lt = exps();
       }
       l += lt;
       __builtin_amdgcn_s_setprio(1);
-      // V^T a block of 32 features at a time, the next one's reads in flight where
-      // registers allow (d = 64 has four wavefronts a SIMD instead)
+      // V^T a block of 32 features at a time, the next one's reads in flight
       const unsigned sv = lds_addr(sk + R::TB);
-      constexpr int AHEAD = D == 64 ? 0 : 1;
-      bf16x8_t va[AHEAD + 1][4];
-      if (AHEAD) read_v_block<D>(sv + voff, va[0]);
+      bf16x8_t va[2][2 * NE];
+      read_v_part<D, 2 * E, 2 * NE>(sv + voff, va[0]);
 #pragma unroll
       for (int c = 0; c < NDB; ++c) {
-        constexpr int N = AHEAD + 1;
-        if (c + AHEAD < NDB) read_v_block<D>(sv + (voff ^ (64 * (c + AHEAD))), va[(c + AHEAD) % N]);
-        if (AHEAD && c + 1 < NDB)
-          block_wait<8>(va[c % N]);
-        else
-          block_wait<0>(va[c % N]);
+        if (c + 1 < NDB) {
+          read_v_part<D, 2 * E, 2 * NE>(sv + (voff ^ (64 * (c + 1))), va[(c + 1) & 1]);
+          part_wait<4 * NE>(va[c & 1]);
+        } else {
+          part_wait<0>(va[c & 1]);
+        }
 #pragma unroll
-        for (int j = 0; j < 4; ++j) o[c] = mfma32(va[c % N][j], pf[j], o[c]);
+        for (int j = 0; j < 2 * NE; ++j) o[c] = mfma32(va[c & 1][j], pf[j], o[c]);
       }
       __builtin_amdgcn_s_setprio(0);
-    }
+    };
+    pass(std::integral_constant<int, 0>());
+    if constexpr (D == 64) pass(std::integral_constant<int, 1>());
     ring_sync<0>();
   }
   l += lane_xor32(l);
@@ -1178,7 +1198,7 @@ ChunkShape chunk_shape(const DevAcsr& a, int dtype, int B, int H, int heads, int
   const int of = s.tiles ? kTileRows : kRows;
   s.blocks = (int32_t)((rows + of - 1) / of);
   const int64_t units = (std::min(a.max_row_nnz + of, a.L) + kUnit - 1) / kUnit;
-  const int64_t groups = (int64_t)s.blocks * B * heads, slots = s.tiles && d == 64 ? 768 : 512;
+  const int64_t groups = (int64_t)s.blocks * B * heads, slots = s.tiles && d == 64 ? 1024 : 512;
   const int64_t n = std::min({std::max<int64_t>(slots / groups, 1), (units + 7) / 8, int64_t(64)});
   s.splits = units * (n - 1) <= 14 * n ? 1 : (int32_t)n;
   s.cap = s.splits == 1 || B == 1 || B > 64 ? s.splits : std::min(2 * s.splits, 64);
