@@ -1003,48 +1003,62 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void k_weigh_tiles(
     if (sees) from = min(from, t), to = max(to, t);
   }
   if (to >= 0) atomicMin(&span[0], from), atomicMax(&span[1], to);
-  // K operand: key qi of each unit, chunk 2 ks + h
   auto slot_of = [&](int j, bool& found) {
     const int p = page_of(x.c.pages, b, x.c.max_pages, x.c.n_pages, x.c.page_shift, j);
     found = p >= 0;
     return cache_row(max(p, 0), x.c.heads, kh, x.c.page_shift, j);
   };
-  bf16x8_t ka[2][NKS];
-#pragma unroll
-  for (int e = 0; e < 2; ++e) {
-    bool found;
-    const unsigned slot = slot_of(min(kb0 + 32 * e + qi, ch.len - 1), found);
-#pragma unroll
-    for (int ks = 0; ks < NKS; ++ks)
-      ka[e][ks] = *(const bf16x8_t*)((const char*)x.c.K + (size_t)slot * RB + 32 * ks + 16 * h);
-  }
   __syncthreads();
   const int s0 = span[0] * G / kTileRows, s1 = span[1] < 0 ? s0 : (span[1] * G + G - 1) / kTileRows + 1;
+  // K operand: key qi of each unit, chunk 2 ks + h
+  bf16x8_t ka[2][NKS];
+  if (s0 < s1) {
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      bool found;
+      const unsigned slot = slot_of(min(kb0 + 32 * e + qi, ch.len - 1), found);
+#pragma unroll
+      for (int ks = 0; ks < NKS; ++ks)
+        ka[e][ks] = *(const bf16x8_t*)((const char*)x.c.K + (size_t)slot * RB + 32 * ks + 16 * h);
+    }
+  }
 
-  // row r of a stage: its token and head
-  const float inv_G = 1.f / G;
-  auto token_of = [&](int st, int r, int& g) {
-    return divide(min(st * kTileRows + r, rows - 1), G, inv_G, g);
-  };
-  auto issue = [&](int st, char* at) {
+  // Rows are walked without divisions: R rows further are R / G tokens and R % G heads,
+  // and a token more, G heads less, where the heads run over.
+  const int64_t wrap = 2 * (x.c.qt - G * x.c.qh);
+  // Q: this lane's row of each load, 4 RPL rows from one to the next, through all stages
+  constexpr int RS = 4 * RPL;
+  int qg;
+  const int qr = s0 * kTileRows + wave * RPL + lane / CPR;
+  const int qtok = divide(qr, G, 1.f / G, qg);
+  const char* const q0 = (const char*)((const __bf16*)x.c.Q + b * x.c.qb + kh * G * x.c.qh);
+  int64_t q_at = 2 * (qtok * x.c.qt + qg * x.c.qh);
+  const int q_dg = RS % G;
+  const int64_t q_step = 2 * (RS / G * x.c.qt + q_dg * x.c.qh);
+  auto issue = [&](int st, char* at) {     // called for s0, s0 + 1, ..
 #pragma unroll
     for (int k = 0; k < N; ++k) {
       const int bk = wave + 4 * k, r = bk * RPL + lane / CPR;
-      int g;
-      const int t = token_of(st, r, g);
-      const __bf16* const q = (const __bf16*)x.c.Q + b * x.c.qb + (kh * G + g) * x.c.qh + t * x.c.qt;
-      dma16((const char*)q + 16 * ((lane % CPR) ^ place_k<D>(r)), at + bk * kDmaBlock);
+      const bool in = st * kTileRows + r < rows;
+      dma16(q0 + (in ? q_at : 0) + 16 * ((lane % CPR) ^ place_k<D>(r)), at + bk * kDmaBlock);
+      q_at += q_step, qg += q_dg;
+      if (qg >= G) qg -= G, q_at += wrap;
     }
   };
+  // ... and this lane's row of the wavefront's 32 of a stage, in the mask and of lse
   struct Row {
     RowRuns rr;
     float lse;
   };
-  auto fetch = [&](int st) {               // this lane's row of the wavefront's 32
-    int g;
-    const int t = token_of(st, 32 * wave + qi, g);
-    return Row{runs[dbg::idx(ch.p0 + t, L, dbg::kRow)],
-               x.c.lse[((int64_t)b * x.c.H + kh * G + g) * x.c.T + t] * kLog2e};
+  int rg, rt = divide(min(s0 * kTileRows + 32 * wave + qi, rows - 1), G, 1.f / G, rg);
+  const int r_dt = kTileRows / G, r_dg = kTileRows % G;
+  const float* const lse0 = x.c.lse + ((int64_t)b * x.c.H + kh * G) * x.c.T;
+  auto fetch = [&]() {                     // of s0, then of each one after
+    const Row w{runs[dbg::idx(ch.p0 + rt, L, dbg::kRow)], lse0[(int64_t)rg * x.c.T + rt] * kLog2e};
+    rt += r_dt, rg += r_dg;
+    if (rg >= G) rg -= G, ++rt;
+    if (rt >= ch.n) rt = ch.n - 1, rg = G - 1;
+    return w;
   };
   auto word_of = [&](int st, const Row& w) {
     uint32_t word = 0;
@@ -1071,10 +1085,10 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void k_weigh_tiles(
   const float sl2 = x.c.scale * kLog2e;
   const int koff = (32 * wave + qi) * RB + 16 * (h ^ place_k<D>(qi));
   if (s0 < s1) {
-    Row w = fetch(s0);
+    Row w = fetch();
     uint32_t word = word_of(s0, w);
     float lse = w.lse;
-    w = fetch(min(s0 + 1, s1 - 1));
+    w = fetch();
     issue(s0, ring);
     ring_sync<0>();
     for (int st = s0; st < s1; ++st) {
@@ -1082,7 +1096,7 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void k_weigh_tiles(
       // the next stage's words, and the loads of the one after, ahead of its rows'
       const uint32_t next_word = word_of(st + 1, w);
       const float next_lse = w.lse;
-      w = fetch(min(st + 2, s1 - 1));
+      w = fetch();
       if (st + 1 < s1) issue(st + 1, ring + (~(st - s0) & 1) * kTileRows * RB);
       if (__any(word != 0)) {
         const uint32_t other = __builtin_bit_cast(uint32_t, lane_xor32(__builtin_bit_cast(float, word)));
