@@ -674,8 +674,8 @@ splat_status splat_cache_weights(splat_acsr_t h, splat_dtype dtype, int32_t B, i
  * last.  left: int32 [B], the new lengths.
  * to: int32 [B, max_to], the pages that the tokens move to, of the same cache; none of
  * them is a page that the call's tables name in `table` or name twice (shared pages
- * stay as they were).  NULL: in place, and then no two sequences share a page below
- * their lengths.  A token without a page in either table is not moved, and its weight counts as
+ * stay as they were).  NULL: in place, and then no page below the lengths may be named
+ * twice, by one sequence or by two.  A token without a page in either table is not moved, and its weight counts as
  * less than any other; NaN counts as the largest.  A length outside [0, SPLAT_MAX_L] or past the
  * table: nothing moves, left = -1.  Bits are moved, not rounded.  The weights, kept and left share no
  * memory with another argument (INVALID_ARG).
@@ -735,6 +735,15 @@ splat_status splat_debug_route(splat_acsr_t h, int32_t call, splat_dtype dtype, 
  */
 splat_status splat_debug_bwd_shared(splat_acsr_t h, splat_dtype dtype, int32_t B, int32_t H, int32_t d,
                                     int32_t shared[2]);
+
+/*
+ * splat_debug_chunk -- how splat_sparse_mhsa_chunk would go about a launch: shape[0] 1 for
+ * tiles of 128 rows and 0 for slices of 32, shape[1] the parts that a block's keys
+ * are shared out in (on average; 1: not).  Host only, for tests of the choice, which may
+ * change between versions.
+ */
+splat_status splat_debug_chunk(splat_acsr_t h, splat_dtype dtype, int32_t B, int32_t H, int32_t heads,
+                               int32_t T, int32_t d, int32_t shape[2]);
 
 /* Message of the calling thread's last non-OK status ("" if none). */
 const char* splat_last_error(void);

@@ -171,6 +171,7 @@ def _open(path: str) -> ctypes.CDLL:
                                       P(i32), vp],
         "splat_debug_route": [vp, i32, i32, i32, i32, i32, P(i32), P(i32)],
         "splat_debug_bwd_shared": [vp, i32, i32, i32, i32, P(i32)],
+        "splat_debug_chunk": [vp, i32, i32, i32, i32, i32, i32, P(i32)],
         "splat_debug_bounds": [P(ctypes.c_uint32), i32],
         "splat_debug_bounds_probe": [i32, i32, i32, P(i32)],
     }
@@ -427,6 +428,14 @@ def bwd_shared(acsr: Acsr, dtype: torch.dtype, B: int, H: int, d: int) -> Tuple[
                                             _int32(d, "d"), n))
     return n[0], n[1]
 
+
+def chunk_route(acsr: Acsr, dtype: torch.dtype, B: int, H: int, heads: int, T: int, d: int) -> Tuple[str, int]:
+    """("tiles" or "slices", parts of a block's keys) that sparse_mhsa_chunk takes
+    (splat_debug_chunk): for tests; needs no GPU."""
+    n = (ctypes.c_int32 * 2)()
+    _check(acsr._lib.splat_debug_chunk(acsr.handle, _DT[dtype], _int32(B, "B"), _int32(H, "H"),
+                                       _int32(heads, "heads"), _int32(T, "T"), _int32(d, "d"), n))
+    return ("slices", "tiles")[n[0]], n[1]
 
 
 def _dense(x: torch.Tensor, name: str, acsr: Acsr, d: Optional[int] = None):

@@ -1356,6 +1356,16 @@ splat_status splat_debug_bwd_shared(splat_acsr_t h, splat_dtype dtype, int32_t B
   return ok();
 }
 
+splat_status splat_debug_chunk(splat_acsr_t h, splat_dtype dtype, int32_t B, int32_t H, int32_t heads,
+                               int32_t T, int32_t d, int32_t shape[2]) {
+  if (!shape) return fail(SPLAT_ERR_INVALID_ARG, "shape must be non-NULL");
+  int64_t bytes = 0;
+  CHECK(splat_chunk_workspace(h, dtype, B, H, heads, T, d, &bytes));
+  const splat::ChunkShape s = splat::chunk_shape(h->dev, dtype, B, H, heads, T, d);
+  shape[0] = s.tiles, shape[1] = s.splits;
+  return ok();
+}
+
 splat_status splat_debug_bounds(uint32_t* flags, int32_t clear) {
   CHECK(check_ptr(flags, "flags"));
 #ifndef SPLAT_DEBUG_BOUNDS

@@ -1196,9 +1196,13 @@ hipError_t prepare_chunk() {
   return e;
 }
 
-// Tiles for bf16 blocks of more than 64 rows: 10 tokens of 8 sequences, 4 heads a head of the
-// cache (40 rows), 38.3 us by slices and 35.9 by tiles, but one sequence's 8 tokens, 8
-// heads (64 rows), over 600 keys 13.4 and 19.1.
+// Tiles for bf16 launches of more than 32 rows a head of the cache whose slices would
+// have many units in all (tiles take a third of the time a row and key, but four wavefronts
+// share one block's where slices have a unit each).  300 tokens under a window of 256, 24 heads
+// (2400 units), d = 64: tiles 19.8 us, slices 12.2; 1000 tokens (7680) 27.1 and 22.2; 1000 over 32
+// heads on 8, B = 4 (12160) 25.6 and 34.4; every key of 4096, 300 tokens of 24 heads (30720) 38.7 and
+// 47.9.  d = 128: 2400 units 24.1 and 15.6, 6400 33.7 and 34.9, 7680 34.0 and 40.6, 10000 28.7
+// and 44.3.
 //
 // A block's units are shared out among as many workgroups as the chip holds beside
 // each other (more would take a second turn: 4 sequences of 16 fp32 tokens, 12 heads,
@@ -1211,7 +1215,9 @@ hipError_t prepare_chunk() {
 ChunkShape chunk_shape(const DevAcsr& a, int dtype, int B, int H, int heads, int T, int d) {
   ChunkShape s;
   const int64_t rows = (int64_t)T * (H / heads);
-  s.tiles = dtype == 1 && rows > 64;
+  const int64_t slices = (rows + kRows - 1) / kRows * B * heads;
+  const int64_t slice_units = (std::min(a.max_row_nnz + kRows, a.L) + kUnit - 1) / kUnit;
+  s.tiles = dtype == 1 && rows > 32 && slices * slice_units > (d == 64 ? 9000 : 6000);
   const int of = s.tiles ? kTileRows : kRows;
   s.blocks = (int32_t)((rows + of - 1) / of);
   const int64_t units = (std::min(a.max_row_nnz + of, a.L) + kUnit - 1) / kUnit;
