@@ -82,7 +82,7 @@ def test_new_places_start_from_zero(gpu_lib):
     reach anything; rows of lse -inf add nothing; NaN reaches its row's keys alone."""
     splat = gpu_lib
     a, M = make(splat, "window", {"w": 20}, 300)
-    for T in (2, 60):
+    for T in (2, 60, 140):
         lengths, counts, page = [300, 170], [T, T - 1], 16
         kc, _, table = paged(lengths, page, 19, 2, 64, torch.float32, 3)
         Q = torch.randn((2, 4, T, 64), generator=torch.Generator().manual_seed(1))
