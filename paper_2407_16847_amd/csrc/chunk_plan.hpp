@@ -5,7 +5,9 @@
 // counted by their two ends and summed up, and leaves bits in the two at its rims; a strided run leaves
 // bits.  A word is then empty, full (every row has all its keys), partial, or, with at
 // most kSparseKeys bits and no whole cover, sparse.  Where that saves half of them at least,
-// the sparse words' keys are gathered into units of 32.
+// the sparse words' keys are gathered into units of 32.  Every workgroup plans for
+// itself, some 2 us: a launch for it beforehand would cost as much, and the lengths
+// are not known to the host.
 #pragma once
 
 #include "../../include/splat.h"

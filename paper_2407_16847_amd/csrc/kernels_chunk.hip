@@ -161,7 +161,13 @@ __device__ __forceinline__ void redo_row(const ChunkArgs& x, const RowRuns* runs
 
 // ------------------------------------------------------------------ slices
 // A workgroup per 32 rows; its wavefronts take every fourth unit of the rows' keys
-// and join at the end, and so do workgroups that share out a block's units.
+// and join at the end, and so do workgroups that share out a block's units.  Each
+// wavefront keeps a softmax of its own (running maximum, sum, O): one pass over the
+// keys.  Bound by HBM where sequences are long: 5 tokens of 16 sequences of 1000 .. 8192 keys, 32
+// heads over 8, d = 128, bf16 59 us, 5.1 TB/s, what a copy of 1 GiB reaches, and 5 to join;
+// else by the chain length, rows' runs, plan, pages, keys, products, some 8 us: 8 tokens of one
+// sequence under window 512 + 64 global 8.8 us and 4.0 to join.  fp32, where each unit
+// takes the matrix cores 2 us at d = 64: 300 tokens under a window of 256, 21.5 us.
 constexpr int kRows = 32;
 
 // Waits until at most N of this wavefront's loads are on their way.
@@ -396,6 +402,12 @@ __global__ __launch_bounds__(kThreads, sizeof(T) * D > 256 ? 1 : 2) void k_chunk
 // taken from the score registers.  A row's reference m stays while its tiles' sums
 // stay below kSumLimit, without a look at the maximum: a tile past it (and a row's first)
 // takes the exact maximum and rescales.
+// Bound by the matrix cores and the vector ALUs in turn, and by the longest blocks: 1024
+// tokens of 4 sequences over 2048 .. 8192 keys, 32 heads over 8, d = 128 314 us, 883
+// TFLOP/s (1232 in a product of 8192^3); 2048 tokens of 4 sequences under window 512 + 64 global,
+// 16 heads, d = 64 59.6 us, 462 TFLOP/s, a third of the time in tiles that the window cuts.
+// One 16-key step's products straight behind its exponentials, instead of a tile's behind all
+// of them: 10% slower.  Without priority for the products: 318 us.
 constexpr int kTileRows = 128;
 constexpr float kSumLimit = 4096.f;
 
@@ -853,7 +865,9 @@ __device__ __forceinline__ int key_of_lane(int lane) {
 // Few rows: the sequences' units of 32 keys are dealt out evenly, whatever the lengths: a
 // workgroup has a contiguous share of those of one head (of 64 sequences at a time), its
 // wavefronts every fourth, the next one's K on its way.  A unit's keys go over the
-// sequence's rows 32 at a time.
+// sequence's rows 32 at a time.  Bound by HBM: a token of 32 sequences of 1000 .. 8192
+// keys, 32 heads over 8, d = 128, bf16 73 us, 4.2 TB/s; shares by sequence instead of by
+// length 119.
 template <typename T, int D>
 __global__ __launch_bounds__(kThreads, sizeof(T) * D > 256 ? 1 : 2) void k_weigh(
     const RowRuns* __restrict__ runs, int L, const WeighArgs x) {
@@ -974,6 +988,9 @@ __global__ __launch_bounds__(kThreads, sizeof(T) * D > 256 ? 1 : 2) void k_weigh
 // bf16, many rows: a workgroup has 64 keys, whose K stays in its wavefronts'
 // registers, and goes over the rows that see any of them, 128 at a time through a two-slot
 // LDS ring, 32 a wavefront.  A lane forms its row's word of one of the two units.
+// 512 tokens of 4 sequences of 600 .. 4096 keys, 16 heads over 4, d = 64: 35 us, 229
+// TFLOP/s: two to three workgroups a CU, each with some 8 us until its first products and
+// 16 stages of exponentials (16 cycles each) behind half as many cycles of products.
 template <int D>
 __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void k_weigh_tiles(
     const RowRuns* __restrict__ runs, int L, const WeighArgs x, int blocks) {
@@ -1202,7 +1219,7 @@ hipError_t prepare_chunk() {
 // have many units in all (tiles take a third of the time a row and key, but four wavefronts
 // share one block's where slices have a unit each).  300 tokens under a window of 256, 24 heads
 // (2400 units), d = 64: tiles 19.8 us, slices 12.2; 1000 tokens (7680) 27.1 and 22.2; 1000 over 32
-// heads on 8, B = 4 (12160) 25.6 and 34.4; every key of 4096, 300 tokens of 24 heads (30720) 38.7 and
+// heads on 8, B = 4 (12160) 25.6 and 34.4; every key of 4096, 300 tokens of 24 heads (31 thousand) 38.7 and
 // 47.9.  d = 128: 2400 units 24.1 and 15.6, 6400 33.7 and 34.9, 7680 34.0 and 40.6, 10000 28.7
 // and 44.3.
 //

@@ -20,7 +20,8 @@ using mfma::u32x4_t;
 // same order, stay in registers; the K-th largest of them is found 8 bits at a time from
 // the top, by histograms of those that agree with it so far.  Equal weights at that value
 // stay from the lowest place on.  Bound by latency: pages and weights one behind the other, two
-// barriers and a scan a digit, two scans for the places.
+// barriers and a scan a digit, two scans for the places: 8.8 us for 4096 weights a head,
+// 15 for 8192 (bit by bit, 32 counts over the workgroup: 20 and 32).
 constexpr int kSelThreads = 1024, kSelWaves = kSelThreads / 64;
 
 // The weights' order as that of unsigned integers: a NaN is the largest, -0 is 0.
@@ -166,6 +167,7 @@ __global__ __launch_bounds__(kSelThreads) void k_evict_select(const EvictArgs x)
 
 // ------------------------------------------------------------ where they move
 // To pages of their own: a thread has a 16-byte chunk of kMoveRows rows of K and of V.
+// Bound by HBM: 4096 rows of 256 bytes of K and V, 8 heads, 16 sequences 92 us, 5.3 TB/s.
 constexpr int kMoveThreads = 256, kMoveRows = 4;
 
 template <int RB>
@@ -207,7 +209,9 @@ __global__ __launch_bounds__(kMoveThreads) void k_evict_move(const EvictArgs x) 
 // In place: the rows' order makes a row's new place never come after its old one.  A
 // workgroup has 64 bytes of every row of K or V (or the weights) of one (sequence, head) and
 // takes the rows in batches: once a batch is read its places may be written, since
-// what later batches read lies behind them.
+// what later batches read lies behind them.  16 sequences of 2000 .. 8192 tokens to 4096, 8
+// heads, d = 128, bf16: 139 us with the selection, to pages of their own 116; one of
+// 4096 to 2048, 16 heads, d = 64 45 us and 15: batches of 256 rows one after the other.
 constexpr int kSlab = 64;
 
 template <typename T, int LPR>
