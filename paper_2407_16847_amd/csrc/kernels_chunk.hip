@@ -993,7 +993,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) * D > 256 ? 1 : 2) void k_weigh
 // 16 stages of exponentials (16 cycles each) behind half as many cycles of products.
 template <int D>
 __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void k_weigh_tiles(
-    const RowRuns* __restrict__ runs, int L, const WeighArgs x, int blocks) {
+    const RowRuns* __restrict__ runs, int L, const WeighArgs x) {
   constexpr int NKS = D / 16, RB = 2 * D, CPR = RB / 16, RPL = 64 / CPR, N = kTileRows / RPL / 4;
   extern __shared__ __attribute__((aligned(16))) char ring[];
   __shared__ float sums[4][2][32];
@@ -1001,8 +1001,8 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void k_weigh_tiles(
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int qi = lane & 31, h = lane >> 5, G = x.c.group;
   // a sequence's blocks of keys in a row, so that they lie on all of the chip's dies;
-  // the longest sequence first
-  const int bh = blockIdx.x / blocks, kb0 = 64 * (blockIdx.x - bh * blocks);
+  // the longest sequence first; two dimensions, since 2^32 threads in one are refused
+  const int bh = blockIdx.y, kb0 = 64 * blockIdx.x;
   const int kh = bh % x.c.heads, b = by_length(x.c.lengths, x.c.B, bh / x.c.heads);
   const Chunk ch = chunk_of(x.c, L, b);
   if (ch.bad || kb0 >= ch.len) return;
@@ -1167,9 +1167,8 @@ hipError_t weigh_launch(const DevAcsr& a, const WeighArgs& x, hipStream_t st) {
     // d = 64, every key of 4096, 24 heads: 70 rows 25.3 us and 14.9 with a wavefront's units
     // in turn, 300 rows 33.6 and 39.9; 1200 rows of 32 heads 71 and 121, 280 of them 42 and 35
     if (x.c.T * x.c.group > 256) {
-      const int blocks = (int)((room + 63) / 64);
-      hipLaunchKernelGGL((k_weigh_tiles<D>), dim3((unsigned)(groups * blocks)), dim3(kThreads),
-                         (2 * kTileRows * 2 * D), st, a.runs, a.L, x, blocks);
+      hipLaunchKernelGGL((k_weigh_tiles<D>), dim3((unsigned)((room + 63) / 64), (unsigned)groups),
+                         dim3(kThreads), (2 * kTileRows * 2 * D), st, a.runs, a.L, x);
       return hipGetLastError();
     }
   }

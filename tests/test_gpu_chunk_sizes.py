@@ -67,6 +67,35 @@ def test_many_sequences(gpu_lib, B, T, L, dtype):
     both(gpu_lib, a, M, Q, kc, vc, table, lengths, counts, 0.125)
 
 
+@pytest.mark.parametrize("T", [17, 257])
+def test_most_blocks(gpu_lib, T):
+    """16384 heads of sequences that may have 65536 keys each: more blocks of keys than
+    a grid's first dimension takes in threads."""
+    splat, L, B, heads, page, scale = gpu_lib, 65536, 1024, 16, 512, 0.125
+    a = splat.Acsr(splat.Pattern.from_terms(L, [dict(lo_i=1, lo_c=-40, hi_i=1)]))
+    g = torch.Generator(device="cuda").manual_seed(T)
+    kc, vc = (torch.randn((B, heads, page, 64), generator=g, device="cuda").bfloat16() for _ in range(2))
+    Q = torch.randn((B, heads, T, 64), generator=g, device="cuda").bfloat16()
+    table = torch.zeros((B, L // page), dtype=torch.int32)
+    table[:, 0] = torch.randperm(B, generator=torch.Generator().manual_seed(1)).int()
+    lengths = [T + (37 * b) % (page - T) for b in range(B)]
+    w = torch.rand((B, heads, page), generator=g, device="cuda")
+    O, lse = splat.sparse_mhsa_chunk(a, Q, kc, vc, table.cuda(), ints(lengths), scale)
+    got = splat.cache_weights(a, Q, lse, kc, table.cuda(), ints(lengths), w, scale, decay=0.5, out=torch.empty_like(w))
+    torch.cuda.synchronize()
+    M = Rows(lambda i, j: (j <= i) & (j >= i - 40))
+    some = [0, 1, 511, 512, 1022, 1023]
+    at = table[some, 0].long()
+    one = torch.arange(len(some), dtype=torch.int32)[:, None]
+    n, c = [lengths[b] for b in some], [T] * len(some)
+    small = [x[at.cuda()].cpu() for x in (kc, vc, w, got)]
+    q, l = Q[some].cpu(), lse[some].cpu()
+    check((O[some], l), chunk64(q, *small[:2], one, n, c, M, scale))
+    want, bound = weights64(q, l, small[0], one, n, c, M, scale, small[2], 0.5)
+    for k, length in enumerate(n):
+        assert ((small[3][k].double() - want[k]).abs() <= bound[k])[:, :length].all()
+
+
 class Rows:
     """Rows of a mask of 65536 positions, as chunk64 asks for them."""
 
