@@ -713,8 +713,28 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 4 : 2) void k_chunk_tiles(
   l += lane_xor32(l), lx += lane_xor32(lx);
   if (__any(!found)) lost = 1;
   __syncthreads();
-  // a page that is none: every row of the block is formed again from its own keys
-  if (ch.bad || lost) l = lx = NAN;
+  // pages that are none, among those of the units' keys: the rows that have a key there are
+  // NaN, and no others (a cache may have given up the pages behind its window, and a unit of the
+  // window's first keys reach into them).  Bit k: key k of the unit.
+  bool gone = ch.bad;
+  if (lost) {
+    uint32_t* const none = (uint32_t*)ring;
+    for (int k0 = 0; k0 < 32 * (u1 - u0); k0 += kThreads) {
+      const int u = min(u0 + (k0 + (int)threadIdx.x) / 32, u1 - 1);
+      const int j = u < plan.dense ? min(32 * (plan.units()[u] & (int)(kFullUnit - 1)) + qi, ch.len - 1)
+                                   : (int)plan.keys()[min(32 * (u - plan.dense) + qi, plan.gathered - 1)];
+      const int p = table[dbg::idx(j, L, dbg::kKey) >> x.page_shift];
+      const uint64_t out = __ballot(p < 0 || p >= x.n_pages);
+      if (qi == 0) none[u - u0] = (uint32_t)(h == 0 ? out : out >> 32);
+    }
+    __syncthreads();
+    for (int u = u0; u < u1; ++u) {
+      const uint32_t bits = none[u - u0];
+      if (bits) gone = gone || (unit_word(plan, u, runs, row, simple, ch.len) & bits);
+    }
+    __syncthreads();
+  }
+  if (gone) l = lx = NAN;
   asm volatile("" : "+v"(mine));     // formed again, not kept through the loop
   const bool counts = mine < rows;
   const int ri = r0 + mine, rt = ri / G;
@@ -752,7 +772,7 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 4 : 2) void k_chunk_tiles(
       }
       store4<__bf16>((__bf16*)(stage + qi * OS) + 32 * c + 8 * k + 4 * h, v[0], v[1], v[2], v[3]);
     }
-  const uint64_t again = __ballot(counts && !ch.bad && !fine);
+  const uint64_t again = __ballot(counts && !gone && !fine);
   if (lane == 0) redo[wave] = (uint32_t)again | (uint32_t)(again >> 32);
   if (h == 0 && ri < x.T * G)
     x.lse[place] = !counts || l == 0.f ? -INFINITY : kLn2 * (m + log2f(lx));
