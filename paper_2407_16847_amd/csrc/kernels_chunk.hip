@@ -640,9 +640,10 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 4 : 2) void k_chunk_tiles(
           for (int r = 0; r < 16; ++r) s[e][r] = keep_if_bit(s[e][r], bits, r);
         }
       }
-      uint32_t pf[2 * NE][4];    // P^T, bf16 pairs
+      bf16x8_t pf[2 * NE];
+      float lt, lxt;
       auto exps = [&]() {
-        float x0 = 0.f, x1 = 0.f;
+        float l0 = 0.f, l1 = 0.f, x0 = 0.f, x1 = 0.f;
 #pragma unroll
         for (int j = 0; j < 2 * NE; ++j) {
           float e8[8];
@@ -650,12 +651,17 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 4 : 2) void k_chunk_tiles(
           for (int e = 0; e < 8; ++e) e8[e] = exp2_hw(s[j >> 1][(j & 1) * 8 + e]);
           x0 += (e8[0] + e8[1]) + (e8[2] + e8[3]);
           x1 += (e8[4] + e8[5]) + (e8[6] + e8[7]);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) pf[j][e] = pack_bf16_rn(e8[2 * e], e8[2 * e + 1]);
+          const unsigned v0 = pack_bf16_rn(e8[0], e8[1]), v1 = pack_bf16_rn(e8[2], e8[3]);
+          const unsigned v2 = pack_bf16_rn(e8[4], e8[5]), v3 = pack_bf16_rn(e8[6], e8[7]);
+          l0 = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(mfma::bf16x2_t, v0), mfma::kOnes2, l0, false);
+          l1 = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(mfma::bf16x2_t, v1), mfma::kOnes2, l1, false);
+          l0 = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(mfma::bf16x2_t, v2), mfma::kOnes2, l0, false);
+          l1 = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(mfma::bf16x2_t, v3), mfma::kOnes2, l1, false);
+          pf[j] = __builtin_bit_cast(bf16x8_t, u32x4_t{v0, v1, v2, v3});
         }
-        return x0 + x1;
+        lt = l0 + l1, lxt = x0 + x1;
       };
-      float lxt = exps();
+      exps();
       // (both halves of the lanes decide alike: a row's sum and its keys are theirs together)
       const float both = lxt + lane_xor32(lxt);
       if (__any(!(both <= kSumLimit) || (!set && seen != 0))) {
@@ -679,25 +685,14 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 4 : 2) void k_chunk_tiles(
         for (int e = 0; e < NE; ++e)
 #pragma unroll
           for (int r = 0; r < 16; ++r) s[e][r] -= up;
-        lxt = exps();
+        exps();
       }
-      lx += lxt;
+      l += lt, lx += lxt;
       __builtin_amdgcn_s_setprio(1);
       // V^T a block of 32 features at a time, the next one's reads in flight
       const unsigned sv = lds_addr(sk + R::TB);
       bf16x8_t va[2][2 * NE];
       read_v_part<D, 2 * E, 2 * NE>(sv + voff, va[0]);
-      // meanwhile the rounded weights' sum (of the pairs as scalars: taken out of a vector, the
-      // compiler made them one and the same)
-      float l0 = 0.f, l1 = 0.f;
-#pragma unroll
-      for (int j = 0; j < 2 * NE; ++j)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          float& sum = e & 1 ? l1 : l0;
-          sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(mfma::bf16x2_t, pf[j][e]), mfma::kOnes2, sum, false);
-        }
-      l += l0 + l1;
 #pragma unroll
       for (int c = 0; c < NDB; ++c) {
         if (c + 1 < NDB) {
@@ -707,8 +702,7 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 4 : 2) void k_chunk_tiles(
           part_wait<0>(va[c & 1]);
         }
 #pragma unroll
-        for (int j = 0; j < 2 * NE; ++j)
-          o[c] = mfma32(va[c & 1][j], __builtin_bit_cast(bf16x8_t, u32x4_t{pf[j][0], pf[j][1], pf[j][2], pf[j][3]}), o[c]);
+        for (int j = 0; j < 2 * NE; ++j) o[c] = mfma32(va[c & 1][j], pf[j], o[c]);
       }
       __builtin_amdgcn_s_setprio(0);
     };
