@@ -629,8 +629,7 @@ splat_status splat_sparse_mhsa_decode(splat_acsr_t h, splat_dtype dtype, int32_t
  * with a key whose page lies outside [0, n_pages): NaN.  Only a row's own keys
  * count, whatever the others hold; a row whose scores are all -inf gets NaN (and lse -inf).
  * Scores, softmax and sums in fp32 in a fixed order, one rounding of O; for blocks of
- * many bf16 rows the probabilities are rounded to nearest even bf16 before they meet V,
- * and their sum as rounded divides O.
+ * many bf16 rows the probabilities are rounded to nearest even bf16 before they meet V.
  * O and lse share no memory with the inputs or each other (INVALID_ARG).
  * workspace: splat_chunk_workspace() bytes, 16-byte aligned, that the call writes
  * and reads (calls that may run at the same time need one each); NULL if 0.

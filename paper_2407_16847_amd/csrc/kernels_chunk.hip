@@ -402,13 +402,15 @@ __global__ __launch_bounds__(kThreads, sizeof(T) * D > 256 ? 1 : 2) void k_chunk
 // taken from the score registers.  A row's reference m stays while its tiles' sums
 // stay below kSumLimit, without a look at the maximum: a tile past it (and a row's first)
 // takes the exact maximum and rescales.
-// P^T is rounded to bf16, as in the fused forward; O is divided by the sum of the rounded
-// weights, so that their roundings cancel in what a row's values share, and the log-sum-exp
-// adds the weights before.  A second product with what the rounding left brings O's error from 0.0023
-// of its size to its own rounding's, 0.0017, at 413 us for 316 and 80 for 67 of the cases below.
+// P^T is rounded to bf16 as in the fused forward, which leaves an error of O of 0.0023 of its
+// size where its own rounding leaves 0.0017.  A second product with what the rounding left brings that
+// to 0.0017, at 413 us for 311 and 80 for 64 of the cases below.  O is divided by the sum of the weights
+// before the rounding, so a feature is off by at most 2^-8 of the row's sum of w |v|; by the
+// sum of the rounded ones it would be of w |v - O|: none where values are equal, but up to twice as
+// much where they have both signs, at 2 to 3% more time.
 // Bound by the matrix cores and the vector ALUs in turn, and by the longest blocks: 1024
-// tokens of 4 sequences over 2048 .. 8192 keys, 32 heads over 8, d = 128 316 us, 877
-// TFLOP/s (1232 in a product of 8192^3; 311 us without the second sum); 2048 tokens of 4 sequences under window 512 + 64 global,
+// tokens of 4 sequences over 2048 .. 8192 keys, 32 heads over 8, d = 128 314 us, 883
+// TFLOP/s (1232 in a product of 8192^3); 2048 tokens of 4 sequences under window 512 + 64 global,
 // 16 heads, d = 64 59.6 us, 462 TFLOP/s, a third of the time in tiles that the window cuts.
 // One 16-key step's products straight behind its exponentials, instead of a tile's behind all
 // of them: 10% slower.  Without priority for the products: 318 us.
@@ -514,9 +516,7 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 4 : 2) void k_chunk_tiles(
 #pragma unroll
     for (int r = 0; r < 16; ++r) o[c][r] = 0.f;
   const float sl2 = x.scale * kLog2e;
-  // l: the sum of the rounded p, which the products take, and which divides O; lx: of the p
-  // before, for the log-sum-exp
-  float m = 0.f, l = 0.f, lx = 0.f;
+  float m = 0.f, l = 0.f;
   bool set = false, found = true;          // the row has a reference; every page was one
 
   // Of unit u's keys this lane loads rows r = RPL * (wave + 4 k) % 32 + lane / CPR, k <
@@ -641,29 +641,23 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 4 : 2) void k_chunk_tiles(
         }
       }
       bf16x8_t pf[2 * NE];
-      float lt, lxt;
       auto exps = [&]() {
-        float l0 = 0.f, l1 = 0.f, x0 = 0.f, x1 = 0.f;
+        float l0 = 0.f, l1 = 0.f;
 #pragma unroll
         for (int j = 0; j < 2 * NE; ++j) {
           float e8[8];
 #pragma unroll
           for (int e = 0; e < 8; ++e) e8[e] = exp2_hw(s[j >> 1][(j & 1) * 8 + e]);
-          x0 += (e8[0] + e8[1]) + (e8[2] + e8[3]);
-          x1 += (e8[4] + e8[5]) + (e8[6] + e8[7]);
-          const unsigned v0 = pack_bf16_rn(e8[0], e8[1]), v1 = pack_bf16_rn(e8[2], e8[3]);
-          const unsigned v2 = pack_bf16_rn(e8[4], e8[5]), v3 = pack_bf16_rn(e8[6], e8[7]);
-          l0 = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(mfma::bf16x2_t, v0), mfma::kOnes2, l0, false);
-          l1 = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(mfma::bf16x2_t, v1), mfma::kOnes2, l1, false);
-          l0 = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(mfma::bf16x2_t, v2), mfma::kOnes2, l0, false);
-          l1 = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(mfma::bf16x2_t, v3), mfma::kOnes2, l1, false);
-          pf[j] = __builtin_bit_cast(bf16x8_t, u32x4_t{v0, v1, v2, v3});
+          l0 += (e8[0] + e8[1]) + (e8[2] + e8[3]);
+          l1 += (e8[4] + e8[5]) + (e8[6] + e8[7]);
+          pf[j] = __builtin_bit_cast(bf16x8_t, u32x4_t{pack_bf16_rn(e8[0], e8[1]), pack_bf16_rn(e8[2], e8[3]),
+                                                       pack_bf16_rn(e8[4], e8[5]), pack_bf16_rn(e8[6], e8[7])});
         }
-        lt = l0 + l1, lxt = x0 + x1;
+        return l0 + l1;
       };
-      exps();
+      float lt = exps();
       // (both halves of the lanes decide alike: a row's sum and its keys are theirs together)
-      const float both = lxt + lane_xor32(lxt);
+      const float both = lt + lane_xor32(lt);
       if (__any(!(both <= kSumLimit) || (!set && seen != 0))) {
         float mx = -INFINITY;
 #pragma unroll
@@ -674,7 +668,7 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 4 : 2) void k_chunk_tiles(
         // a row without weight has no reference yet
         const float up = !set ? (mx == -INFINITY ? 0.f : mx) : fmaxf(0.f, mx);
         const float alpha = set ? exp2_hw(-up) : 0.f;
-        l *= alpha, lx *= alpha;
+        l *= alpha;
 #pragma unroll
         for (int c = 0; c < NDB; ++c)
 #pragma unroll
@@ -685,9 +679,9 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 4 : 2) void k_chunk_tiles(
         for (int e = 0; e < NE; ++e)
 #pragma unroll
           for (int r = 0; r < 16; ++r) s[e][r] -= up;
-        exps();
+        lt = exps();
       }
-      l += lt, lx += lxt;
+      l += lt;
       __builtin_amdgcn_s_setprio(1);
       // V^T a block of 32 features at a time, the next one's reads in flight
       const unsigned sv = lds_addr(sk + R::TB);
@@ -710,7 +704,7 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 4 : 2) void k_chunk_tiles(
     if constexpr (D == 64) pass(std::integral_constant<int, 1>());
     ring_sync<0>();
   }
-  l += lane_xor32(l), lx += lane_xor32(lx);
+  l += lane_xor32(l);
   if (__any(!found)) lost = 1;
   __syncthreads();
   // pages that are none, among those of the units' keys: the rows that have a key there are
@@ -734,7 +728,7 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 4 : 2) void k_chunk_tiles(
     }
     __syncthreads();
   }
-  if (gone) l = lx = NAN;
+  if (gone) l = NAN;
   asm volatile("" : "+v"(mine));     // formed again, not kept through the loop
   const bool counts = mine < rows;
   const int ri = r0 + mine, rt = ri / G;
@@ -742,16 +736,14 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 4 : 2) void k_chunk_tiles(
   if (x.splits > 1) {
     if (!counts) return;
     float* const to = x.ws + (place * x.cap + split) * (D + 2);
-    // a part's O belongs to its l, and is joined by its lx
-    const float ratio = l == 0.f ? 1.f : lx / l;
-    if (h == 0) *(f32x2_t*)to = f32x2_t{set ? m : -INFINITY, lx};
+    if (h == 0) *(f32x2_t*)to = f32x2_t{set ? m : -INFINITY, l};
 #pragma unroll
     for (int c = 0; c < NDB; ++c)
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         float* const at = to + 2 + 32 * c + 8 * k + 4 * h;
-        *(f32x2_t*)at = f32x2_t{o[c][4 * k] * ratio, o[c][4 * k + 1] * ratio};
-        *(f32x2_t*)(at + 2) = f32x2_t{o[c][4 * k + 2] * ratio, o[c][4 * k + 3] * ratio};
+        *(f32x2_t*)at = f32x2_t{o[c][4 * k], o[c][4 * k + 1]};
+        *(f32x2_t*)(at + 2) = f32x2_t{o[c][4 * k + 2], o[c][4 * k + 3]};
       }
     return;
   }
@@ -775,7 +767,7 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 4 : 2) void k_chunk_tiles(
   const uint64_t again = __ballot(counts && !gone && !fine);
   if (lane == 0) redo[wave] = (uint32_t)again | (uint32_t)(again >> 32);
   if (h == 0 && ri < x.T * G)
-    x.lse[place] = !counts || l == 0.f ? -INFINITY : kLn2 * (m + log2f(lx));
+    x.lse[place] = !counts || l == 0.f ? -INFINITY : kLn2 * (m + log2f(l));
   __syncthreads();
 #pragma unroll
   for (int k = 0; k < 32 / R::RPL; ++k) {
