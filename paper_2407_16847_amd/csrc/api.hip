@@ -55,6 +55,20 @@ void plan_sizes(splat_acsr* h) {
   h->dev.L = a.L;
   h->dev.nnz = a.nnz;
   h->dev.max_row_nnz = a.max_row_nnz;
+  std::vector<int32_t> all, past;
+  for (int32_t i = 0; i < a.L; ++i)
+    if (a.row_ptr[i + 1] > a.row_ptr[i]) {
+      all.push_back(a.row_ptr[i + 1] - a.row_ptr[i]);
+      past.push_back(splat::count_lt(a.runs[i], i + 1));
+    }
+  auto most = [](std::vector<int32_t>& n) {
+    if (n.empty()) return 0;
+    const auto at = n.begin() + (n.size() - 1 - n.size() / 16);
+    std::nth_element(n.begin(), at, n.end());
+    const int32_t longest = *std::max_element(at, n.end());
+    return longest - *at <= *at / 8 ? longest : *at;
+  };
+  h->dev.row_keys = most(all), h->dev.past_keys = most(past);
   h->dev.n_groups = (int32_t)a.groups.size();
   h->dev.computed = a.computed;
   h->dev.max_slice_tiles = 0;

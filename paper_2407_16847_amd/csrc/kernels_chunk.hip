@@ -1240,13 +1240,19 @@ hipError_t prepare_chunk() {
   return e;
 }
 
-// Tiles for bf16 launches of more than 32 rows a head of the cache whose slices would
-// have many units in all (tiles take a third of the time a row and key, but four wavefronts
-// share one block's where slices have a unit each).  300 tokens under a window of 256, 24 heads
-// (2400 units), d = 64: tiles 19.8 us, slices 12.2; 1000 tokens (7680) 27.1 and 22.2; 1000 over 32
-// heads on 8, B = 4 (12160) 25.6 and 34.4; every key of 4096, 300 tokens of 24 heads (31 thousand) 38.7 and
-// 47.9.  d = 128: 2400 units 24.1 and 15.6, 6400 33.7 and 34.9, 7680 34.0 and 40.6, 10000 28.7
-// and 44.3.
+// Sizes are those of a chunk's rows, which see the keys up to their own and the chunk's newer
+// ones; a few global rows of the mask (DevAcsr) do not count, 300 tokens of 24 heads under a
+// symmetric window of 255 with 4 global tokens 14.8 us, 26.3 counted by the longest row.
+//
+// Tiles for bf16 launches of more than 32 rows a head of the cache that are more slices than
+// the chip takes nearly at once, whatever their keys: d = 64, 720 slices of 14 units tiles 32.3 us,
+// slices 23.7, 816 of 2 20.0 and 16.9, 984 of 4 19.7 and 24.7, 1216 of 8 24.7 and 29.8; d = 128,
+// 456 of 8 23.9 and 20.6, 640 of 8 29.4 and 29.2, 768 of 4 25.6 and 31.7, 984 of 4 20.6 and 30.8.  Fewer
+// slices where they are long: tiles take a third of the time a row and key, but four wavefronts
+// share one block's where slices have a unit each.  d = 64, 240 slices of 58 units 32.0 and 31.5, of
+// 111 39.3 and 42.6, 416 of 58 41.5 and 36.7, of 111 50.4 and 59.5; d = 128, 240 of 33 32.5 and 33.0, of 58
+// 38.3 and 40.5, 416 of 33 41.6 and 34.6, of 58 48.7 and 51.7.  And of those only launches of many units in
+// all: d = 64, 48 of 111 23.9 and 21.7, 96 of 111 26.7 and 28.7; d = 128, 28.5 and 27.1, 33.4 and 37.1.
 //
 // A block's units are shared out among as many workgroups as the chip holds beside
 // each other (more would take a second turn: 4 sequences of 16 fp32 tokens, 12 heads,
@@ -1255,21 +1261,31 @@ hipError_t prepare_chunk() {
 // fp32 tokens of 2 sequences under a window of 256, 12 heads, 27.4 us in two
 // parts, 21.2 in one.  One sequence's 32 tokens over 2048 keys, 16 heads: two units a
 // wavefront 13.1 us, four 15.6, eight 20.8; 16 tokens, 32 heads over 8, 8192 keys, d = 128:
-// 23.0, 21.8, 28.5.
+// 23.0, 21.8, 28.5.  Few short blocks, a workgroup or less a CU in all, take one unit a wavefront:
+// 8 tokens of one sequence, 16 heads, d = 64, 19 units, one part / two units / one unit a
+// wavefront 13.8 / 14.0 / 12.3 us in bf16, 23.2 / 17.2 / 14.2 in fp32; 14 units 12.6 / 14.1 / 12.8 and
+// 20.2 / 16.7 / 14.3, 7 units 10.1 / - / 12.3 and 17.6 / - / 17.2; d = 128 in fp32, 7 units 25.2 / - / 21.9.
 ChunkShape chunk_shape(const DevAcsr& a, int dtype, int B, int H, int heads, int T, int d) {
   ChunkShape s;
   const int64_t rows = (int64_t)T * (H / heads);
   const int64_t slices = (rows + kRows - 1) / kRows * B * heads;
-  const int64_t slice_units = (std::min(a.max_row_nnz + kRows, a.L) + kUnit - 1) / kUnit;
-  s.tiles = dtype == 1 && rows > 32 && slices * slice_units > (d == 64 ? 9000 : 6000);
+  auto keys = [&](int of) {      // that a block of so many rows has
+    return std::min<int64_t>(std::min((int64_t)a.row_keys, (int64_t)a.past_keys + T) + of, a.L);
+  };
+  const int64_t slice_units = (keys(kRows) + kUnit - 1) / kUnit;
+  const bool is_many = slices > (d == 64 ? 900 : 640);
+  const bool is_long = slice_units >= (d == 64 ? 79 : 45) && slices * slice_units > (d == 64 ? 9000 : 6000);
+  s.tiles = dtype == 1 && rows > 32 && (is_many || is_long);
   const int of = s.tiles ? kTileRows : kRows;
   s.blocks = (int32_t)((rows + of - 1) / of);
-  const int64_t units = (std::min(a.max_row_nnz + of, a.L) + kUnit - 1) / kUnit;
+  const int64_t units = (keys(of) + kUnit - 1) / kUnit;
   const int64_t groups = (int64_t)s.blocks * B * heads, slots = s.tiles && d == 64 ? 1024 : 512;
   const int64_t n = std::min({std::max<int64_t>(slots / groups, 1), (units + 7) / 8, int64_t(64)});
   s.splits = units * (n - 1) <= 14 * n ? 1 : (int32_t)n;
+  const int64_t each = (units + 3) / 4;
+  if (!s.tiles && each > (dtype == 1 ? 4 : d == 64 ? 2 : 1) && each <= 16 && groups * each <= 256) s.splits = (int32_t)each;
   s.cap = s.splits == 1 || B == 1 || B > 64 ? s.splits : std::min(2 * s.splits, 64);
-  s.most = (int32_t)std::min(a.max_row_nnz + of, a.L);
+  s.most = (int32_t)keys(of);
   return s;
 }
 

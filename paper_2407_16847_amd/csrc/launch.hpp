@@ -18,6 +18,9 @@ struct DevAcsr {
   int32_t L;
   int64_t nnz;
   int32_t max_row_nnz;
+  // keys of a row, and those among them up to the row's own position: the most that a row has,
+  // but where a sixteenth of the rows or fewer have far more than the others, what those have
+  int32_t row_keys, past_keys;
   int32_t n_groups;
   int64_t computed;         // rows x keys of the non-empty wavefront tiles
   int32_t max_slice_tiles;  // non-empty tiles of the 32 rows that have the most
