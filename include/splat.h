@@ -745,6 +745,15 @@ splat_status splat_debug_bwd_shared(splat_acsr_t h, splat_dtype dtype, int32_t B
 splat_status splat_debug_chunk(splat_acsr_t h, splat_dtype dtype, int32_t B, int32_t H, int32_t heads,
                                int32_t T, int32_t d, int32_t shape[2]);
 
+/*
+ * splat_debug_weights -- how splat_cache_weights would go about a launch over tables of
+ * `room` keys: shape[0] 1 for blocks of 64 keys and 0 for units of 32 dealt out, then
+ * among shape[1] workgroups a head.  Host only, for tests of the choice, which may change
+ * between versions.
+ */
+splat_status splat_debug_weights(splat_acsr_t h, splat_dtype dtype, int32_t B, int32_t H, int32_t heads,
+                                 int32_t T, int32_t d, int32_t room, int32_t shape[2]);
+
 /* Message of the calling thread's last non-OK status ("" if none). */
 const char* splat_last_error(void);
 

@@ -172,6 +172,7 @@ def _open(path: str) -> ctypes.CDLL:
         "splat_debug_route": [vp, i32, i32, i32, i32, i32, P(i32), P(i32)],
         "splat_debug_bwd_shared": [vp, i32, i32, i32, i32, P(i32)],
         "splat_debug_chunk": [vp, i32, i32, i32, i32, i32, i32, P(i32)],
+        "splat_debug_weights": [vp, i32, i32, i32, i32, i32, i32, i32, P(i32)],
         "splat_debug_bounds": [P(ctypes.c_uint32), i32],
         "splat_debug_bounds_probe": [i32, i32, i32, P(i32)],
     }
@@ -436,6 +437,17 @@ def chunk_route(acsr: Acsr, dtype: torch.dtype, B: int, H: int, heads: int, T: i
     _check(acsr._lib.splat_debug_chunk(acsr.handle, _DT[dtype], _int32(B, "B"), _int32(H, "H"),
                                        _int32(heads, "heads"), _int32(T, "T"), _int32(d, "d"), n))
     return ("slices", "tiles")[n[0]], n[1]
+
+
+def weights_route(acsr: Acsr, dtype: torch.dtype, B: int, H: int, heads: int, T: int, d: int,
+                  room: int) -> Tuple[str, int]:
+    """("tiles" or "units", workgroups that share out a head's units) that cache_weights
+    takes over tables of `room` keys (splat_debug_weights): for tests; needs no GPU."""
+    n = (ctypes.c_int32 * 2)()
+    _check(acsr._lib.splat_debug_weights(acsr.handle, _DT[dtype], _int32(B, "B"), _int32(H, "H"),
+                                         _int32(heads, "heads"), _int32(T, "T"), _int32(d, "d"),
+                                         _int32(room, "room"), n))
+    return ("units", "tiles")[n[0]], n[1]
 
 
 def _dense(x: torch.Tensor, name: str, acsr: Acsr, d: Optional[int] = None):

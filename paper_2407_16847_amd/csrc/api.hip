@@ -1380,6 +1380,18 @@ splat_status splat_debug_chunk(splat_acsr_t h, splat_dtype dtype, int32_t B, int
   return ok();
 }
 
+splat_status splat_debug_weights(splat_acsr_t h, splat_dtype dtype, int32_t B, int32_t H, int32_t heads,
+                                 int32_t T, int32_t d, int32_t room, int32_t shape[2]) {
+  if (!shape) return fail(SPLAT_ERR_INVALID_ARG, "shape must be non-NULL");
+  if (room < 1) return fail(SPLAT_ERR_INVALID_ARG, "room must be 1 or more, got %d", room);
+  int64_t bytes = 0;
+  CHECK(splat_chunk_workspace(h, dtype, B, H, heads, T, d, &bytes));
+  const splat::WeighShape s =
+      splat::weigh_shape(h->dev, dtype, B, H, heads, T, d, std::min<int64_t>(room, h->dev.L));
+  shape[0] = s.tiles, shape[1] = (int32_t)s.parts;
+  return ok();
+}
+
 splat_status splat_debug_bounds(uint32_t* flags, int32_t clear) {
   CHECK(check_ptr(flags, "flags"));
 #ifndef SPLAT_DEBUG_BOUNDS

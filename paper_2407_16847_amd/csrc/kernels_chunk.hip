@@ -1188,21 +1188,15 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void k_weigh_tiles(
 template <typename T, int D>
 hipError_t weigh_launch(const DevAcsr& a, const WeighArgs& x, hipStream_t st) {
   const int64_t room = std::min<int64_t>((int64_t)x.c.max_pages << x.c.page_shift, a.L);
-  const int64_t heads = x.c.heads, groups = x.c.B * heads;
+  const WeighShape s = weigh_shape(a, sizeof(T) == 2, x.c.B, x.c.H, x.c.heads, x.c.T, D, room);
   if constexpr (sizeof(T) == 2) {
-    // d = 64, every key of 4096, 24 heads: 70 rows 25.3 us and 14.9 with a wavefront's units
-    // in turn, 300 rows 33.6 and 39.9; 1200 rows of 32 heads 71 and 121, 280 of them 42 and 35
-    if (x.c.T * x.c.group > 256) {
-      hipLaunchKernelGGL((k_weigh_tiles<D>), dim3((unsigned)((room + 63) / 64), (unsigned)groups),
+    if (s.tiles) {
+      hipLaunchKernelGGL((k_weigh_tiles<D>), dim3((unsigned)((room + 63) / 64), (unsigned)(x.c.B * x.c.heads)),
                          dim3(kThreads), (2 * kTileRows * 2 * D), st, a.runs, a.L, x);
       return hipGetLastError();
     }
   }
-  // what the chip holds at a time: the shares are even.  32 sequences' tokens 78.2 us, with
-  // twice as many workgroups 81.5, four times 90.7
-  constexpr int kHeld = sizeof(T) * D > 256 ? 256 : 512;
-  const int64_t parts = std::min((room + 4 * kUnit - 1) / (4 * kUnit) * x.c.B, (kHeld + heads - 1) / heads);
-  hipLaunchKernelGGL((k_weigh<T, D>), dim3((unsigned)heads, (unsigned)parts), dim3(kThreads),
+  hipLaunchKernelGGL((k_weigh<T, D>), dim3((unsigned)x.c.heads, (unsigned)s.parts), dim3(kThreads),
                      (8 * kStage<T, D>), st, a.runs, a.L, x);
   return hipGetLastError();
 }
@@ -1291,6 +1285,20 @@ ChunkShape chunk_shape(const DevAcsr& a, int dtype, int B, int H, int heads, int
 
 int64_t chunk_workspace(const ChunkShape& s, int B, int H, int T, int d) {
   return s.splits == 1 ? 0 : (int64_t)B * H * T * s.cap * (d + 2);
+}
+
+// parts: what the chip holds at a time by the workgroups' LDS, and no more, so that the shares are
+// even: 32 sequences' tokens, 8 heads, d = 128 78.2 us, with twice as many workgroups 81.5, four times
+// 90.7; 128 rows of 24 heads over 4096 keys 23.9 with 21 parts, 37.5 with 22, of which some
+// take a second turn; d = 64 14.2 with 42, 18.4 with 21, 20.9 with 22.
+WeighShape weigh_shape(const DevAcsr& a, int dtype, int B, int H, int heads, int T, int d, int64_t room) {
+  const int64_t held = (1 << 17) / (d * (dtype == 1 ? 2 : 4));
+  WeighShape s;
+  // d = 64, every key of 4096, 24 heads: 70 rows 25.3 us and 14.9 with a wavefront's units
+  // in turn, 300 rows 33.6 and 39.9; 1200 rows of 32 heads 71 and 121, 280 of them 42 and 35
+  s.tiles = dtype == 1 && (int64_t)T * (H / heads) > 256;
+  s.parts = std::min((room + 4 * kUnit - 1) / (4 * kUnit) * B, std::max(held / heads, int64_t(1)));
+  return s;
 }
 
 hipError_t launch_chunk(const DevAcsr& a, int dtype, int d, const ChunkArgs& x, hipStream_t st) {

@@ -189,6 +189,12 @@ struct WeighArgs {
   float* out;                 // the same, or w itself
   float decay;
 };
+struct WeighShape {
+  bool tiles;                 // blocks of 64 keys, not units of 32 dealt out
+  int64_t parts;              // workgroups that share out a head's units
+};
+// room: the keys that a sequence may have
+WeighShape weigh_shape(const DevAcsr& a, int dtype, int B, int H, int heads, int T, int d, int64_t room);
 hipError_t launch_weigh(const DevAcsr& a, int dtype, int d, const WeighArgs& x, hipStream_t st);
 
 // A cache brought back to a budget.  to: the pages that the kept keys move to, or
