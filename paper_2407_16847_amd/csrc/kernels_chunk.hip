@@ -1291,12 +1291,21 @@ int64_t chunk_workspace(const ChunkShape& s, int B, int H, int T, int d) {
 // even: 32 sequences' tokens, 8 heads, d = 128 78.2 us, with twice as many workgroups 81.5, four times
 // 90.7; 128 rows of 24 heads over 4096 keys 23.9 with 21 parts, 37.5 with 22, of which some
 // take a second turn; d = 64 14.2 with 42, 18.4 with 21, 20.9 with 22.
+//
+// tiles: from how many rows on it pays to pass them through LDS for the keys' sake depends on whether
+// all blocks of 64 keys are there at a time, and else on whether the mask has most keys (blocks
+// skip the rows that see none of theirs).  us, units / tiles: d = 64, 4 heads of 4096 keys, 160 rows
+// 10.7 / 11.3, 192 12.0 / 11.3, 256 14.7 / 11.5; 16 heads, every key, 320 rows 22.8 / 27.5, 448 29.6 / 30.2,
+// 512 33.1 / 31.1, window 256, 192 rows 16.2 / 17.1, 256 19.9 / 18.1; 16 heads of 8 sequences, every
+// key, 384 rows 134 / 155, 512 174 / 172.  d = 128, 4 heads, 128 rows 11.8 / 11.4, 192 15.7 / 12.7;
+// 16 heads, every key, 320 rows 31.7 / 34.3, 384 36.7 / 34.8; 24 heads, window 256, 160 rows 30.3 / 32.0, 192
+// 35.1 / 32.5.
 WeighShape weigh_shape(const DevAcsr& a, int dtype, int B, int H, int heads, int T, int d, int64_t room) {
   const int64_t held = (1 << 17) / (d * (dtype == 1 ? 2 : 4));
   WeighShape s;
-  // d = 64, every key of 4096, 24 heads: 70 rows 25.3 us and 14.9 with a wavefront's units
-  // in turn, 300 rows 33.6 and 39.9; 1200 rows of 32 heads 71 and 121, 280 of them 42 and 35
-  s.tiles = dtype == 1 && (int64_t)T * (H / heads) > 256;
+  const int64_t rows = (int64_t)T * (H / heads), blocks = (int64_t)B * heads * ((room + 63) / 64);
+  const bool at_once = blocks <= (d == 64 ? 768 : 512), most = 2 * (int64_t)a.row_keys >= room;
+  s.tiles = dtype == 1 && rows >= (at_once ? (d == 64 ? 192 : 144) : most ? (d == 64 ? 448 : 352) : d == 64 ? 240 : 192);
   s.parts = std::min((room + 4 * kUnit - 1) / (4 * kUnit) * B, std::max(held / heads, int64_t(1)));
   return s;
 }

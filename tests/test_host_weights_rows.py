@@ -31,3 +31,17 @@ def test_refusals():
         with pytest.raises(splat.SplatError):
             splat.weights_route(a, BF16, *args)
     assert splat.load().splat_debug_weights(a.handle, 1, 1, 4, 4, 1, 64, 100, None) == 1
+
+
+def test_faster_side():
+    """Measured launches on both sides of the choice, over tables of the masks' length."""
+    window = lambda L, w: splat.Acsr(splat.Pattern.from_terms(L, [dict(lo_i=1, lo_c=-w, hi_i=1)]))
+    for a, B, heads, d, units, tiles in (
+            (causal(4096), 1, 4, 64, 160, 256), (causal(4096), 1, 16, 64, 384, 512), (causal(4096), 1, 32, 64, 320, 448),
+            (causal(4096), 8, 16, 64, 384, 512), (causal(1024), 1, 32, 64, 160, 256), (window(4096, 256), 1, 16, 64, 192, 256),
+            (window(4096, 1500), 1, 24, 64, 192, 256), (causal(4096), 1, 4, 128, 96, 192), (causal(4096), 1, 16, 128, 320, 384),
+            (causal(4096), 8, 16, 128, 256, 448), (window(4096, 256), 1, 24, 128, 160, 192), (causal(1024), 1, 12, 128, 96, 160)):
+        room = a._info["L"]
+        assert splat.weights_route(a, BF16, B, heads, heads, units, d, room)[0] == "units", (B, heads, d, units)
+        assert splat.weights_route(a, BF16, B, heads, heads, tiles, d, room)[0] == "tiles", (B, heads, d, tiles)
+        assert splat.weights_route(a, F32, B, heads, heads, tiles, d, room)[0] == "units"
