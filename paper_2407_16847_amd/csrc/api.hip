@@ -1407,6 +1407,7 @@ splat_status splat_debug_bounds(uint32_t* flags, int32_t clear) {
   if (e == hipSuccess) e = splat::bounds_collect_grad_tiles(&bits, clear != 0);
   if (e == hipSuccess) e = splat::bounds_collect_serve(&bits, clear != 0);
   if (e == hipSuccess) e = splat::bounds_collect_chunk(&bits, clear != 0);
+  if (e == hipSuccess) e = splat::bounds_collect_evict(&bits, clear != 0);
   if (e != hipSuccess) return fail(SPLAT_ERR_HIP, "splat_debug_bounds: %s", hipGetErrorString(e));
   *flags = bits;
   return SPLAT_OK;

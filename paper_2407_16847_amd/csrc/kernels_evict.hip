@@ -31,6 +31,12 @@ __device__ __forceinline__ uint32_t order_of(float w) {
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
+// A row of the cache, checked against its size in a checked build.
+__device__ __forceinline__ uint32_t row_of(const EvictArgs& x, int page, int h, int j) {
+  return dbg::idx(cache_row(page, x.heads, h, x.page_shift, j),
+                  ((uint32_t)x.n_pages * (uint32_t)x.heads) << x.page_shift, dbg::kKey);
+}
+
 // Exclusive prefix sums of n values in LDS (n <= kSelThreads), all of which
 // every thread sees afterwards.
 __device__ __forceinline__ void scan(int* x, int n, int* wave_sums) {
@@ -76,12 +82,12 @@ __global__ __launch_bounds__(kSelThreads) void k_evict_select(const EvictArgs x)
 #pragma unroll
     for (int v = 0; v < STEP; ++v)
       page[v] = x.pages[(int64_t)b * x.max_pages +
-                        (min((v0 + v) * kSelThreads + tid, n - 1) >> x.page_shift)];
+                        dbg::idx(min((v0 + v) * kSelThreads + tid, n - 1) >> x.page_shift, x.max_pages, dbg::kRow)];
 #pragma unroll
     for (int v = 0; v < STEP; ++v) {
       const bool ok = page[v] >= 0 && page[v] < x.n_pages;
       const int j = min((v0 + v) * kSelThreads + tid, n - 1);
-      const float w = x.w[cache_row(ok ? page[v] : 0, x.heads, h, x.page_shift, j)];
+      const float w = x.w[row_of(x, ok ? page[v] : 0, h, j)];
       key[v0 + v] = ok ? order_of(w) : 0;  // a place without a page goes first
     }
   }
@@ -161,7 +167,7 @@ __global__ __launch_bounds__(kSelThreads) void k_evict_select(const EvictArgs x)
     if (v * kSelThreads >= n) break;
     const bool stays = keep >> v & 1;
     const int rank = part[v * kSelWaves + wave] + __popcll(__ballot(stays) & before);
-    if (stays) kept[rank] = v * kSelThreads + tid;
+    if (stays) kept[dbg::idx(rank, x.budget, dbg::kValue)] = v * kSelThreads + tid;
   }
 }
 
@@ -187,8 +193,8 @@ __global__ __launch_bounds__(kMoveThreads) void k_evict_move(const EvictArgs x) 
     const int p = j < 0 ? -1 : page_of(x.pages, b, x.max_pages, x.n_pages, x.page_shift, j);
     const int q = j < 0 ? -1 : page_of(x.to, b, x.max_to, x.n_pages, x.page_shift, i);
     moves[r] = p >= 0 && q >= 0;
-    src[r] = cache_row(max(p, 0), x.heads, h, x.page_shift, j);
-    dst[r] = cache_row(max(q, 0), x.heads, h, x.page_shift, i);
+    src[r] = moves[r] ? row_of(x, p, h, j) : 0;
+    dst[r] = moves[r] ? row_of(x, q, h, i) : 0;
   }
 #pragma unroll
   for (int r = 0; r < kMoveRows; ++r) {
@@ -232,8 +238,8 @@ __device__ __forceinline__ void move_in_place(const EvictArgs& x, int b, int h, 
       const int p = page_of(x.pages, b, x.max_pages, x.n_pages, x.page_shift, j);
       const int q = page_of(x.pages, b, x.max_pages, x.n_pages, x.page_shift, i);
       if (j == i || p < 0 || q < 0) continue;
-      v[r] = *(const T*)(base + (size_t)cache_row(p, x.heads, h, x.page_shift, j) * RB + at);
-      to[r] = base + (size_t)cache_row(q, x.heads, h, x.page_shift, i) * RB + at;
+      v[r] = *(const T*)(base + (size_t)row_of(x, p, h, j) * RB + at);
+      to[r] = base + (size_t)row_of(x, q, h, i) * RB + at;
     }
     // the whole batch is in registers before any of its places is written
     asm volatile("" ::: "memory");
@@ -266,6 +272,8 @@ void move_launch(const EvictArgs& x, hipStream_t st) {
 }
 
 }  // namespace
+
+hipError_t bounds_collect_evict(uint32_t* bits, bool clear) { return dbg::collect(bits, clear); }
 
 hipError_t launch_evict(const EvictArgs& x, int row_bytes, hipStream_t st) {
   const int64_t room = std::min<int64_t>((int64_t)x.max_pages << x.page_shift, SPLAT_MAX_L);

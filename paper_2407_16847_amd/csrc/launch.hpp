@@ -224,6 +224,7 @@ hipError_t bounds_collect_grad(uint32_t* bits, bool clear);
 hipError_t bounds_collect_grad_tiles(uint32_t* bits, bool clear);
 hipError_t bounds_collect_serve(uint32_t* bits, bool clear);
 hipError_t bounds_collect_chunk(uint32_t* bits, bool clear);
+hipError_t bounds_collect_evict(uint32_t* bits, bool clear);
 // One check of `index` against [0, n) as kind `kind`, run on the device
 // (allocates and frees one int); *result = the checked index.
 hipError_t bounds_probe(int kind, int index, int n, int* result);
