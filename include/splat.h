@@ -515,8 +515,8 @@ splat_status splat_rotary_build(const splat_rotary_desc* desc, splat_rotary_t* o
  * have pairs left.  The frequency of pair t is base^(-2t/rot_dim) as with one axis,
  * or (restart) that of its number k among its axis's `pairs`, base^(-k/pairs); it is
  * scaled as with one axis.  Calls with such a handle take positions [axes, B, T],
- * one axis after the other, and need them (INVALID_ARG); a position outside the
- * table gives NaN in that axis's pairs alone.
+ * one axis after the other, and where it has two axes or more they need them
+ * (INVALID_ARG); a position outside the table gives NaN in that axis's pairs alone.
  *
  * splat_rotary_build_axes -- axes NULL: one axis, as splat_rotary_build.
  */

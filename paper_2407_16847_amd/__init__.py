@@ -658,7 +658,8 @@ class Rotary:
         axes: how many of the rot_dim/2 pairs turn by each of 1 to 4 axes of
         positions (time, row, column), one axis's pairs after the other's or
         (cyclic) the axes in turn; restart gives each axis frequencies from base^0
-        on.  Positions are then [axes, B, T]."""
+        on.  Positions are then [axes, B, T] (of one axis also [B, T]), and must be
+        given where there are two axes or more."""
         lo, hi = (0.0, 0.0) if ramp is None else ramp
         self.desc = RotaryDesc(_int32(int(max_len), "max_len"), _int32(int(rot_dim), "rot_dim"),
                                int(bool(interleaved)), _int32(int(original_len), "original_len"),

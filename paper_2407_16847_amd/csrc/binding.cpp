@@ -118,10 +118,11 @@ struct Call {
   const int32_t* ints(const Tensor& x, const char* name, at::IntArrayRef sizes) const {
     return (const int32_t*)want(x, name, at::kInt, sizes);
   }
-  // of the tokens of x [B, heads, T, d], as the rotation's axes ask for
+  // of the tokens of x [B, heads, T, d], as the rotation's axes ask for; those of one axis
+  // may have its dimension
   const int32_t* positions(const Opt& p, int64_t axes, at::IntArrayRef x) const {
     if (!p) return nullptr;
-    return axes > 1 ? ints(*p, "positions", {axes, x[0], x[2]}) : ints(*p, "positions", {x[0], x[2]});
+    return axes > 1 || p->dim() == 3 ? ints(*p, "positions", {axes, x[0], x[2]}) : ints(*p, "positions", {x[0], x[2]});
   }
   splat_cache cache(const Tensor& k, const Tensor& v, const Tensor& table, int64_t B, int64_t d) const {
     on_gpu(k, "k_cache");
