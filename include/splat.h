@@ -631,6 +631,7 @@ splat_status splat_sparse_mhsa_decode(splat_acsr_t h, splat_dtype dtype, int32_t
  * Scores, softmax and sums in fp32 in a fixed order, one rounding of O; for blocks of
  * many bf16 rows the probabilities are rounded to nearest even bf16 before they meet V.
  * O and lse share no memory with the inputs or each other (INVALID_ARG).
+ * B*H*T <= 2^24 (UNSUPPORTED; rows of padding count).
  * workspace: splat_chunk_workspace() bytes, 16-byte aligned, that the call writes
  * and reads (calls that may run at the same time need one each); NULL if 0.
  */
@@ -656,7 +657,7 @@ splat_status splat_sparse_mhsa_chunk(splat_acsr_t h, splat_dtype dtype, int32_t 
  * nothing, one of NaN makes its keys' weights NaN.  A place without a page is not
  * written; a sequence of bad length (as there) is left out.  No two sequences share a page
  * below their lengths in out.  fp32 arithmetic in a fixed order.  cache->v is not read.  out
- * otherwise shares no memory with the inputs (INVALID_ARG).
+ * otherwise shares no memory with the inputs (INVALID_ARG).  B*H*T <= 2^24 (UNSUPPORTED).
  */
 splat_status splat_cache_weights(splat_acsr_t h, splat_dtype dtype, int32_t B, int32_t T, int32_t d,
                                  const splat_heads* q, const float* lse, const splat_cache* cache,

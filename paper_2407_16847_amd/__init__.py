@@ -750,7 +750,7 @@ def sparse_mhsa_decode(acsr: Acsr, Q: torch.Tensor, k_cache: torch.Tensor, v_cac
 
 
 def chunk_workspace(acsr: Acsr, dtype: torch.dtype, B: int, H: int, heads: int, T: int, d: int) -> int:
-    """Bytes of workspace that sparse_mhsa_chunk takes (0: none)."""
+    """Bytes of workspace that sparse_mhsa_chunk takes (0: none); B*H*T at most 2^24."""
     n = ctypes.c_int64()
     _check(acsr._lib.splat_chunk_workspace(acsr.handle, _DT[dtype], _int32(B, "B"), _int32(H, "H"),
                                            _int32(heads, "heads"), _int32(T, "T"), _int32(d, "d"),
@@ -768,8 +768,8 @@ def sparse_mhsa_chunk(acsr: Acsr, Q: torch.Tensor, k_cache: torch.Tensor, v_cach
     (default T; int32 [B]) of sequence b's lengths[b] tokens are the chunk's, token t
     of them has the mask's row lengths[b] - counts[b] + t, its columns below
     lengths[b].  The cache's heads divide H.  Returns (O in the inputs' dtype, lse
-    fp32 [B, H, T]); rows of padding have 0 and -inf.  workspace: at least
-    chunk_workspace() bytes, made by the call unless given."""
+    fp32 [B, H, T]); rows of padding have 0 and -inf.  B*H*T is at most 2^24.  workspace:
+    at least chunk_workspace() bytes, made by the call unless given."""
     return native().chunk(acsr.handle.value, Q, k_cache, v_cache, table, lengths, scale, counts, O, lse,
                           workspace, *_where())
 
@@ -781,7 +781,8 @@ def cache_weights(acsr: Acsr, Q: torch.Tensor, lse: torch.Tensor, k_cache: torch
     """Adds the attention weight that each cached key took from a chunk's queries to
     `weights` (fp32 [pages, heads, page]), after decaying it; the chunk's own keys
     start from 0.  Q, table, lengths, counts and scale as given to
-    sparse_mhsa_chunk, lse as it returned it.  In place, or into out."""
+    sparse_mhsa_chunk, lse as it returned it; B*H*T at most 2^24 as there.  In place, or
+    into out."""
     return native().cache_weights(acsr.handle.value, Q, lse, k_cache, table, lengths, weights, scale, counts,
                                   decay, out, *_where())
 
