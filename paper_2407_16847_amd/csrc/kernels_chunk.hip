@@ -99,6 +99,14 @@ __device__ __forceinline__ int part_of(const ChunkArgs& x, int k, int& split, in
   return b;
 }
 
+// What is read in the place of a key without a page, and then has no part in any row: the
+// sequence's newest key, whose values are a token's where an unused page may hold anything
+// (a NaN there would have every row formed again).
+__device__ __forceinline__ unsigned spare_row(const ChunkArgs& x, int b, int kh, int len) {
+  const int p = page_of(x.pages, b, x.max_pages, x.n_pages, x.page_shift, len - 1);
+  return p < 0 ? 0u : cache_row(p, x.heads, kh, x.page_shift, len - 1);
+}
+
 // O and lse of one row by one wavefront, from the row's own keys alone.
 template <typename T, int D>
 __device__ __forceinline__ void row_alone(const ChunkArgs& x, const RowRuns& rr, int b, int kh, int len,
@@ -213,11 +221,13 @@ __global__ __launch_bounds__(kThreads, sizeof(T) * D > 256 ? 1 : 2) void k_chunk
   int u0 = 0, u1 = 0;
   RowEnds& row = ends[wave * kRows + qi];
   bool dense = true;
+  unsigned spare = 0;
   typename M::Row q;
   if (rows > 0 && !ch.bad && ch.len > 0) {
     const int t0 = r0 / G, t1 = (r0 + rows - 1) / G;
     dense = row.open(runs, dbg::idx(ch.p0 + t, L, dbg::kRow));
     load_row<T, D>(q, (const char*)((const T*)x.Q + b * x.qb + (kh * G + g) * x.qh + t * x.qt), 16u * h);
+    spare = spare_row(x, b, kh, ch.len);
     plan_rows<kThreads>(plan, part, L, runs, ch.p0 + t0, t1 - t0 + 1, ch.len);
     u0 = (int)((int64_t)plan.n() * split / splits), u1 = (int)((int64_t)plan.n() * (split + 1) / splits);
   }
@@ -247,7 +257,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) * D > 256 ? 1 : 2) void k_chunk
   };
   auto slot_of = [&](int u, int p, bool& found) {
     found = p >= 0 && p < x.n_pages;
-    return cache_row(found ? p : 0, x.heads, kh, x.page_shift, key_of(u));
+    return found ? cache_row(p, x.heads, kh, x.page_shift, key_of(u)) : spare;
   };
   auto issue = [&](const void* from, unsigned slot, char* to) {
 #pragma unroll
@@ -490,6 +500,7 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 4 : 2) void k_chunk_tiles(
   int u0 = 0, u1 = 0;
   RowEnds& row = ends[mine];
   bool dense = true;
+  unsigned spare = 0;
   bf16x8_t q[NKS];
   char* const ring = lds + plan_bytes(L, tiles_sub(x.page_shift));
   if (rows > 0 && !ch.bad && ch.len > 0) {
@@ -499,6 +510,7 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 4 : 2) void k_chunk_tiles(
 #pragma unroll
     for (int k = 0; k < NKS; ++k) q[k] = *(const bf16x8_t*)(from + 16 * k + 8 * h);
     dense = row.open(runs, dbg::idx(ch.p0 + t, L, dbg::kRow));
+    spare = spare_row(x, b, kh, ch.len);
     plan_rows<kThreads>(plan, part, L, runs, ch.p0 + t0, t1 - t0 + 1, ch.len);
     u0 = (int)((int64_t)plan.n() * split / splits), u1 = (int)((int64_t)plan.n() * (split + 1) / splits);
   }
@@ -538,7 +550,7 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 4 : 2) void k_chunk_tiles(
       const int page = table[kb >> x.page_shift];
       const bool ok = page >= 0 && page < x.n_pages;
       found = found && ok;
-      unit_rows[k] = cache_row(ok ? page : 0, x.heads, kh, x.page_shift, kb) | min(low, ch.len - 1 - kb);
+      unit_rows[k] = ok ? cache_row(page, x.heads, kh, x.page_shift, kb) | min(low, ch.len - 1 - kb) : spare & ~(unsigned)low;
     }
     __syncthreads();
   }
@@ -569,7 +581,7 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 4 : 2) void k_chunk_tiles(
     for (int k = 0; k < NU; ++k) {
       const bool ok = p[k] >= 0 && p[k] < x.n_pages;
       found = found && ok;
-      slot[k] = cache_row(ok ? p[k] : 0, x.heads, kh, x.page_shift, key_of(u, k));
+      slot[k] = ok ? cache_row(p[k], x.heads, kh, x.page_shift, key_of(u, k)) : spare;
     }
   };
   auto issue = [&](char* to, const unsigned (&slot)[2][NU]) {

@@ -102,3 +102,31 @@ def test_pages_given_up_in_many_parts(gpu_lib):
     rows = torch.from_numpy(M[2990 - T:2990, j:j + page].any(1)).cuda()
     assert torch.isnan(O[0][:, rows]).all() and torch.equal(O[0][:, ~rows], want[0][0][:, ~rows])
     check((want[0][:, :2], want[1][:, :2]), chunk64(Q[:, :2], kc[:, :2], vc[:, :2], table, lengths, [T], M, 0.09))
+
+
+@pytest.mark.parametrize("tiles", [True, False])
+@pytest.mark.parametrize("page", [2, 16, 64])
+def test_unused_pages_hold_anything(gpu_lib, page, tiles):
+    """... NaN and infinities in the pages given up, the cache's first among them."""
+    splat, L, d = gpu_lib, 900, 64
+    for kind, params, T, lengths in (("sliding", {"w": 70, "n_global": 4}, 200, [893, 611]), ("dilated", {"w": 30, "dilation": 3}, 150, [877, 600])):
+        a, M = make(splat, kind, params, L)
+        heads = heads_for_tiles(splat, a, 2, 1, T, d) if tiles else 2
+        kc, vc, table = paged(lengths, page, -(-L // page), heads, d, torch.bfloat16, L)
+        Q = torch.randn((2, heads, T, d), generator=torch.Generator().manual_seed(T)).bfloat16()
+        run = lambda k, v, t: splat.sparse_mhsa_chunk(a, Q.cuda(), k.cuda(), v.cuda(), t.cuda(), ints(lengths), 0.125)
+        want = run(kc, vc, table)
+        few = freed(table, lengths, [T, T], M, page)
+        # a page given up becomes the cache's first
+        gone = int(table[0][(few[0] < 0) & (table[0] >= 0)][0])
+        swap = torch.arange(kc.shape[0])
+        swap[0], swap[gone] = gone, 0
+        few = torch.where(few >= 0, swap.int()[few.clamp(min=0).long()], few)
+        k, v = kc[swap].clone(), vc[swap].clone()
+        unused = torch.ones(k.shape[0], dtype=torch.bool)
+        unused[few[few >= 0].long()] = False
+        assert unused[0]
+        k[unused], v[unused] = math.nan, math.inf
+        got = run(k, v, few)
+        torch.cuda.synchronize()
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
