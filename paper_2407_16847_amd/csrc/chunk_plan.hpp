@@ -6,8 +6,9 @@
 // bits.  A word is then empty, full (every row has all its keys), partial, or, with at
 // most kSparseKeys bits and no whole cover, sparse.  Where that saves half of them at least,
 // the sparse words' keys are gathered into units of 32.  Every workgroup plans for
-// itself, some 2 us: a launch for it beforehand would cost as much, and the lengths
-// are not known to the host.
+// itself, some 2 us under windows: a launch for it beforehand would cost as much, and the
+// lengths are not known to the host.  4 tokens over every second key of 8192 / 65536, 8 heads,
+// bf16: 21 / 46 us (every key 16 / 36; strided runs by one thread each, key by key: 213 / 1760).
 #pragma once
 
 #include "../../include/splat.h"
@@ -72,6 +73,9 @@ __device__ __forceinline__ void plan_rows(RowsPlan& plan, uint64_t* part, int L,
   int* const cover = (int*)plan.lds + plan.front;
   for (int i = tid; i < W; i += THREADS) bits[i] = 0;
   for (int i = tid; i <= W; i += THREADS) cover[i] = 0;
+  // whether any run is strided; written again behind the barrier of the first sum
+  uint64_t& strided = part[2 * THREADS / 64 - 1];
+  if (tid == 0) strided = 0;
   __syncthreads();
   for (int k = tid; k < nt * SPLAT_MAX_RUNS; k += THREADS) {
     const int row = dbg::idx(p0 + k / SPLAT_MAX_RUNS, L, dbg::kRow), slot = k % SPLAT_MAX_RUNS;
@@ -89,24 +93,38 @@ __device__ __forceinline__ void plan_rows(RowsPlan& plan, uint64_t* part, int L,
       }
       continue;
     }
-    // a run that the next row's continues is that one's to mark
-    if (row + 1 < p0 + nt) {
-      const Run q = runs[row + 1].r[slot];
-      if (q.start == r.start && q.stride == r.stride && q.count >= r.count) continue;
-    }
-    const int last = imin(r.start + r.stride * (r.count - 1), len - 1);
-    int word = r.start >> 5;
-    uint32_t have = 0;
-    for (int j = r.start; j <= last; j += r.stride) {
-      if (j >> 5 != word) {
-        atomicOr(&bits[word], have);
-        word = j >> 5, have = 0;
-      }
-      have |= 1u << (j & 31);
-    }
-    atomicOr(&bits[word], have);
+    strided = 1;
   }
   __syncthreads();
+  // Strided runs, a word a lane: each wavefront looks 64 runs over and takes every
+  // (THREADS / 64)-th 64 words of them.  A row's run that the next row's continues is that one's.
+  if (strided) {
+    const int lane = tid & 63, wave = tid >> 6;
+    for (int k0 = 0; k0 < nt * SPLAT_MAX_RUNS; k0 += 64) {
+      const int k = min(k0 + lane, nt * SPLAT_MAX_RUNS - 1);
+      const int row = dbg::idx(p0 + k / SPLAT_MAX_RUNS, L, dbg::kRow), slot = k % SPLAT_MAX_RUNS;
+      Run r = runs[row].r[slot];
+      bool marks = k0 + lane < nt * SPLAT_MAX_RUNS && r.count > 1 && r.stride != 1 && r.start < len;
+      if (marks && row + 1 < p0 + nt) {
+        const Run q = runs[row + 1].r[slot];
+        marks = !(q.start == r.start && q.stride == r.stride && q.count >= r.count);
+      }
+      int turn = wave;
+      for (uint64_t left = __ballot(marks); left; left &= left - 1) {
+        const int from = __builtin_ctzll(left);
+        const Run run{__builtin_amdgcn_readlane(r.start, from), __builtin_amdgcn_readlane(r.stride, from),
+                      __builtin_amdgcn_readlane(r.count, from), 0};
+        const int w0 = run.start >> 5, n = imin(run.start + run.stride * (run.count - 1), len - 1) / 32 - w0 + 1;
+        for (int b = 0; b < n; b += 64, turn = (turn + 1) % (THREADS / 64)) {
+          if (turn || b + lane >= n) continue;
+          const int word = w0 + b + lane;
+          const uint32_t have = (uint32_t)run_tile_bits(run, 32 * word, 1, imin(32, len - 32 * word));
+          if (have) atomicOr(&bits[word], have);
+        }
+      }
+    }
+    __syncthreads();
+  }
   // this thread's words
   const int per = (W + THREADS - 1) / THREADS, w0 = tid * per;
   uint32_t b[kMost];
