@@ -172,10 +172,10 @@ __device__ __forceinline__ void redo_row(const ChunkArgs& x, const RowRuns* runs
 // and join at the end, and so do workgroups that share out a block's units.  Each
 // wavefront keeps a softmax of its own (running maximum, sum, O): one pass over the
 // keys.  Bound by HBM where sequences are long: 5 tokens of 16 sequences of 1000 .. 8192 keys, 32
-// heads over 8, d = 128, bf16 59 us, 5.1 TB/s, what a copy of 1 GiB reaches, and 5 to join;
+// heads over 8, d = 128, bf16 59.6 us, 5.1 TB/s, what a copy of 1 GiB reaches, and 5.5 to join;
 // else by the chain length, rows' runs, plan, pages, keys, products, some 8 us: 8 tokens of one
-// sequence under window 512 + 64 global 8.8 us and 4.0 to join.  fp32, where each unit
-// takes the matrix cores 2 us at d = 64: 300 tokens under a window of 256, 21.5 us.
+// sequence, 16 heads, under window 512 + 64 global, in five parts, 11.6 us with the joining launch.
+// fp32, where each unit takes the matrix cores 2 us at d = 64: 300 tokens under a window of 256, 21.8 us.
 constexpr int kRows = 32;
 
 // Waits until at most N of this wavefront's loads are on their way.
@@ -419,11 +419,12 @@ __global__ __launch_bounds__(kThreads, sizeof(T) * D > 256 ? 1 : 2) void k_chunk
 // sum of the rounded ones it would be of w |v - O|: none where values are equal, but up to twice as
 // much where they have both signs, at 2 to 3% more time.
 // Bound by the matrix cores and the vector ALUs in turn, and by the longest blocks: 1024
-// tokens of 4 sequences over 2048 .. 8192 keys, 32 heads over 8, d = 128 314 us, 883
-// TFLOP/s (1232 in a product of 8192^3); 2048 tokens of 4 sequences under window 512 + 64 global,
-// 16 heads, d = 64 59.6 us, 462 TFLOP/s, a third of the time in tiles that the window cuts.
+// tokens of 4 sequences over 2048 .. 8192 keys, 32 heads over 8, d = 128 317 us, 875
+// TFLOP/s (1232 in a product of 8192^3), the matrix cores 39% and the vector ALUs 41% busy; 2048
+// tokens of 4 sequences under window 512 + 64 global, 16 heads, d = 64 60.5 us, 455 TFLOP/s: one
+// uneven turn of 832 blocks, 2.2 of 4 wavefronts a SIMD.
 // One 16-key step's products straight behind its exponentials, instead of a tile's behind all
-// of them: 10% slower.  Without priority for the products: 318 us.
+// of them: 10% slower.  Without priority for the products: 4% slower.
 constexpr int kTileRows = 128;
 constexpr float kSumLimit = 4096.f;
 
@@ -903,9 +904,10 @@ __device__ __forceinline__ int key_of_lane(int lane) {
 // Few rows: the sequences' units of 32 keys are dealt out evenly, whatever the lengths: a
 // workgroup has a contiguous share of those of one head (of 64 sequences at a time), its
 // wavefronts every fourth, the next one's K on its way.  A unit's keys go over the
-// sequence's rows 32 at a time.  Bound by HBM: a token of 32 sequences of 1000 .. 8192
-// keys, 32 heads over 8, d = 128, bf16 73 us, 4.2 TB/s; shares by sequence instead of by
-// length 119.
+// sequence's rows 32 at a time, of those that see any.  K of every unit is read, also of one
+// that no row sees: a window saves products, not bytes.  Bound by HBM: a token of 32 sequences of
+// 1000 .. 8192 keys, 32 heads over 8, d = 128, bf16 72 us, 4.3 TB/s (77 with the launch);
+// shares by sequence instead of by length 119.
 template <typename T, int D>
 __global__ __launch_bounds__(kThreads, sizeof(T) * D > 256 ? 1 : 2) void k_weigh(
     const RowRuns* __restrict__ runs, int L, const WeighArgs x) {
@@ -1300,8 +1302,8 @@ int64_t chunk_workspace(const ChunkShape& s, int B, int H, int T, int d) {
 }
 
 // parts: what the chip holds at a time by the workgroups' LDS, and no more, so that the shares are
-// even: 32 sequences' tokens, 8 heads, d = 128 78.2 us, with twice as many workgroups 81.5, four times
-// 90.7; 128 rows of 24 heads over 4096 keys 23.9 with 21 parts, 37.5 with 22, of which some
+// even: 32 sequences' tokens, 8 heads, d = 128, with twice as many workgroups 4% more time, four times
+// 16%; 128 rows of 24 heads over 4096 keys 23.9 with 21 parts, 37.5 with 22, of which some
 // take a second turn; d = 64 14.2 with 42, 18.4 with 21, 20.9 with 22.
 //
 // tiles: from how many rows on it pays to pass them through LDS for the keys' sake depends on whether
